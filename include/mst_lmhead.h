@@ -82,7 +82,9 @@ enum {
   MST_ERR_WORKSPACE = -4,      /* workspace NULL or smaller than required          */
   MST_ERR_ALIGNMENT = -5,      /* a pointer is not aligned as required             */
   MST_ERR_LAUNCH = -6,         /* the HIP runtime refused a launch                 */
-  MST_ERR_NO_DEVICE = -7       /* no current device, or not a whole 256-CU gfx950  */
+  MST_ERR_NO_DEVICE = -7,      /* no current device, or not a whole 256-CU gfx950  */
+  MST_ERR_BAD_ARGUMENT = -8    /* a value out of range, pointers that exclude or need
+                                  each other, overlapping memory (mst_norm.h)      */
 };
 
 /* Human-readable text for a status code (host; static storage). */

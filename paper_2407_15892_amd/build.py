@@ -1,4 +1,4 @@
-"""Builds libmst_lmhead.so and libmst_mlp.so (HIP, gfx950) in-tree with hipcc."""
+"""Builds libmst_lmhead.so, libmst_mlp.so and libmst_norm.so (HIP, gfx950) in-tree with hipcc."""
 from __future__ import annotations
 
 import os
@@ -9,6 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libmst_lmhead.so")
 MLP_LIB_PATH = os.path.join(HERE, "libmst_mlp.so")
+NORM_LIB_PATH = os.path.join(HERE, "libmst_norm.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -40,8 +41,9 @@ def _compile(src_name: str, lib_path: str, verbose: bool) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/mst_api.hip into libmst_lmhead.so and csrc/mst_mlp_api.hip into libmst_mlp.so;
-    returns the path of the LM-head library."""
+    """Compile csrc/mst_api.hip into libmst_lmhead.so, csrc/mst_mlp_api.hip into libmst_mlp.so and csrc/mst_norm_api.hip
+    into libmst_norm.so; returns the path of the LM-head library."""
+    _compile("mst_norm_api.hip", NORM_LIB_PATH, verbose)
     _compile("mst_mlp_api.hip", MLP_LIB_PATH, verbose)
     return _compile("mst_api.hip", LIB_PATH, verbose)
 

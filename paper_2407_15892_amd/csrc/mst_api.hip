@@ -796,6 +796,7 @@ const char* mst_strerror(mst_status s) {
     case MST_ERR_ALIGNMENT: return "pointer alignment: H, W, dH, dW 16 bytes; workspace 256 bytes; n_valid 8 bytes; labels, lse, loss 4 bytes";
     case MST_ERR_LAUNCH: return "the HIP runtime refused a kernel launch or attribute";
     case MST_ERR_NO_DEVICE: return "no current HIP device, or it is not a whole 256-CU gfx950 chip";
+    case MST_ERR_BAD_ARGUMENT: return "bad argument: a value out of range, pointers that exclude or need each other, or overlapping memory";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,446 @@
+// Host side of the norm, residual and checkpoint calls: argument validation, workspace carving, launches.
+#include "../../include/mst_norm.h"
+#include "host_util.hpp"
+#include "mst_norm_kernels.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using namespace mst;
+using mst_host::misaligned;
+
+constexpr int kNumCu = 256;
+
+mst_status check_launch() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
+
+mst_status check_shape(int64_t S, int64_t d) {
+  if (S < 1 || S >= (int64_t(1) << 30) || d < 8 || d % 8 != 0 || d > MST_NORM_MAX_D) return MST_ERR_BAD_SHAPE;
+  return MST_OK;
+}
+
+int64_t tail_blocks(int64_t d) { return (d + 31) / 32; }
+
+// The tensors of a call, to be checked in one go.
+struct Operands {
+  struct Range { uintptr_t at; size_t bytes; int entry; bool out, whole; };
+  Range r[24];
+  int n = 0;
+  bool aligned = true;
+  // entry: bytes of an entry; whole: one entry for each row and column
+  void add(const void* p, int64_t entries, int entry, bool out, bool whole, size_t alignment = 16) {
+    if (!p) return;
+    if (misaligned(p, alignment)) aligned = false;
+    r[n++] = {reinterpret_cast<uintptr_t>(p), (size_t)entries * entry, entry, out, whole};
+  }
+  mst_status check() const {
+    if (!aligned) return MST_ERR_ALIGNMENT;
+    for (int i = 0; i < n; ++i)
+      for (int j = 0; j < i; ++j) {
+        const Range &a = r[i], &b = r[j];
+        if (!(a.out || b.out) || a.at >= b.at + b.bytes || b.at >= a.at + a.bytes) continue;
+        // a lane reads its entries of an input before it writes the same ones of an output
+        if (a.out == b.out || !a.whole || !b.whole || a.at != b.at || a.entry != b.entry) return MST_ERR_BAD_ARGUMENT;
+      }
+    return MST_OK;
+  }
+};
+
+int type_bytes(int32_t type) { return type == MST_TYPE_FP32 ? 4 : 2; }
+bool good_type(int32_t type) { return type == MST_TYPE_BF16 || type == MST_TYPE_FP32; }
+bool good_norm(float eps, float offset) { return std::isfinite(eps) && eps >= 0x1p-126f && std::isfinite(offset); }
+
+// Gate and scale; rows of the gate in *rows (0 without one).
+mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t S, int64_t* rows) {
+  if (!std::isfinite(scale) || (gate ? gate_rows < 1 : gate_rows != 0)) return MST_ERR_BAD_ARGUMENT;
+  *rows = gate ? (S + std::min(gate_rows, S) - 1) / std::min(gate_rows, S) : 0;
+  return MST_OK;
+}
+
+// How a row is held: chunks of eight columns per lane, lanes (whole waves).
+struct RowPlan {
+  int chunks, threads;
+  explicit RowPlan(int64_t d) {
+    chunks = d <= 8 * 64 * kNormMaxWaves ? 1 : 2;
+    threads = (int)((d + 8 * 64 * chunks - 1) / (8 * 64 * chunks)) * 64;
+  }
+};
+
+constexpr int kFwdRows[2] = {2, 1}, kBwdRows[2] = {2, 1};      // rows at a time with one and with two chunks
+
+// Rows of a workgroup of the backward calls.
+struct BwdPlan {
+  RowPlan row;
+  int rows;
+  int64_t groups;
+  BwdPlan(int64_t S, int64_t d) : row(d) {
+    const int64_t most = kNumCu * std::max(1, 1024 / row.threads);
+    const int at_a_time = kBwdRows[row.chunks - 1];
+    rows = (int)((((S + most - 1) / most) + at_a_time - 1) / at_a_time * at_a_time);
+    groups = (S + rows - 1) / rows;
+  }
+};
+
+size_t workspace_bytes(const BwdPlan& p, int64_t d, int64_t gate_groups) {      // dw_pre, dw_post, two of the gate's rows
+  return p.groups == 1 && gate_groups <= 1 ? 256 : mst_host::align_up((size_t)p.groups * d * 4 * (gate_groups > 1 ? 4 : 2), 256);
+}
+
+template <class T, bool kRes, bool kPre, bool kRebuild, int kNc>
+mst_status launch_fwd_chunks(NormFwd a, int threads, hipStream_t st) {
+  constexpr int kRows = kFwdRows[kNc - 1];
+  const int64_t most = (int64_t(1) << 31) / threads * kRows;      // a launch has fewer than 2^32 lanes
+  for (int64_t r = 0; r < a.S; r += most) {
+    a.row0 = (int)r;
+    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kNc, kRows>), dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)),
+                       dim3(threads), 0, st, a);
+  }
+  return check_launch();
+}
+template <class T, bool kRes, bool kPre, bool kRebuild>
+mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
+  const RowPlan p(a.d);
+  return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p.threads, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p.threads, st);
+}
+
+template <class T, bool kPre, bool kRes, bool kMany>
+mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream_t st) {
+  const BwdPlan p(a.S, a.d);
+  a.rows = p.rows;
+  float* const ws = static_cast<float*>(workspace);
+  const size_t part = (size_t)p.groups * a.d;
+  a.part_pre = ws;
+  a.part_post = ws + part;
+  a.part_gate = ws + 2 * part;
+  const dim3 grid((unsigned)p.groups);
+  if (p.row.chunks == 1)
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 1, kBwdRows[0]>), grid, dim3(p.row.threads), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 2, kBwdRows[1]>), grid, dim3(p.row.threads), 0, st, a);
+  if (p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) {
+    const int64_t items = !kMany ? 0 : a.gate_rows >= a.rows ? gate_groups : p.groups - 1;
+    hipLaunchKernelGGL(k_norm_reduce<kMany>, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + items)), dim3(kReduceThreads), 0, st, a, (int)p.groups);
+  }
+  return check_launch();
+}
+
+template <bool kPre, bool kRes>
+mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_groups, void* workspace, hipStream_t st) {
+  if (kRes && gate_groups > 1)
+    return type == MST_TYPE_FP32 ? launch_bwd<float, kPre, kRes, kRes>(a, gate_groups, workspace, st)
+                                 : launch_bwd<__bf16, kPre, kRes, kRes>(a, gate_groups, workspace, st);
+  return type == MST_TYPE_FP32 ? launch_bwd<float, kPre, kRes, false>(a, gate_groups, workspace, st)
+                               : launch_bwd<__bf16, kPre, kRes, false>(a, gate_groups, workspace, st);
+}
+
+// slots of a checkpoint kernel's launch stay below 2^30: rows of one launch
+int64_t ckpt_rows(int64_t d) { return (int64_t(1) << 30) / (4 * tail_blocks(d)); }
+
+template <class T>
+void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
+  const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
+  for (int64_t r = 0, n; r < S; r += n) {
+    n = std::min(S - r, ckpt_rows(d));
+    const uint32_t slots = (uint32_t)n * per_row.d;
+    hipLaunchKernelGGL(k_ckpt_pack<T>, dim3((slots + kCkptThreads - 1) / kCkptThreads), dim3(kCkptThreads), 0, st,
+                       X + r * d, per_row, slots, (int)d, codes + r * d, exps + r * tail_blocks(d));
+  }
+}
+template <class T>
+void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
+  const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
+  for (int64_t r = 0, n; r < S; r += n) {
+    n = std::min(S - r, ckpt_rows(d));
+    const uint32_t slots = (uint32_t)n * per_row.d;
+    hipLaunchKernelGGL(k_ckpt_unpack<T>, dim3((slots + kCkptThreads - 1) / kCkptThreads), dim3(kCkptThreads), 0, st,
+                       codes + r * d, exps + r * tail_blocks(d), per_row, slots, (int)d, X + r * d);
+  }
+}
+
+mst_status check_device() {
+  int dev = 0;
+  return hipGetDevice(&dev) == hipSuccess ? MST_OK : MST_ERR_NO_DEVICE;
+}
+
+bool both_or_neither(const void* a, const void* b) { return !a == !b; }
+const __bf16* bf(const void* p) { return static_cast<const __bf16*>(p); }
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+
+}  // namespace
+
+extern "C" {
+
+const char* mst_norm_version(void) { return "mst-norm 0.1 (gfx950)"; }
+
+mst_status mst_norm_workspace_bytes(int64_t S, int64_t d, int64_t gate_rows, size_t* bytes) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (gate_rows < 0) return MST_ERR_BAD_ARGUMENT;
+  if (!bytes) return MST_ERR_NULL_POINTER;
+  *bytes = workspace_bytes(BwdPlan(S, d), d, gate_rows ? (S + std::min(gate_rows, S) - 1) / std::min(gate_rows, S) : 0);
+  return MST_OK;
+}
+
+mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t* info) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!info) return MST_ERR_NULL_POINTER;
+  const BwdPlan p(S, d);
+  info[0] = p.row.threads;
+  info[1] = p.rows;
+  info[2] = p.groups;
+  return MST_OK;
+}
+
+mst_status mst_ckpt_pack(const void* X, int32_t type, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!X || !codes || !exps) return MST_ERR_NULL_POINTER;
+  if (!good_type(type)) return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(X, S * d, type_bytes(type), false, true);
+  ops.add(codes, S * d, 1, true, true);
+  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  if (type == MST_TYPE_FP32) launch_pack(static_cast<const float*>(X), S, d, codes, exps, as_stream(stream));
+  else launch_pack(bf(X), S, d, codes, exps, as_stream(stream));
+  return check_launch();
+}
+
+mst_status mst_ckpt_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, void* X, int32_t type, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!X || !codes || !exps) return MST_ERR_NULL_POINTER;
+  if (!good_type(type)) return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(X, S * d, type_bytes(type), true, true);
+  ops.add(codes, S * d, 1, false, true);
+  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  if (type == MST_TYPE_FP32) launch_unpack(codes, exps, S, d, static_cast<float*>(X), as_stream(stream));
+  else launch_unpack(codes, exps, S, d, static_cast<__bf16*>(X), as_stream(stream));
+  return check_launch();
+}
+
+mst_status mst_prenorm_fwd(const void* X, int32_t stream_type, const void* w_pre, float w_offset, float eps,
+                           int64_t S, int64_t d, void* H, int8_t* codes, uint8_t* exps, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!X || !H) return MST_ERR_NULL_POINTER;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps)) return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(X, S * d, type_bytes(stream_type), false, true);
+  ops.add(w_pre, d, 2, false, false);
+  ops.add(H, S * d, 2, true, true);
+  ops.add(codes, S * d, 1, true, true);
+  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormFwd a = {};
+  a.X = X; a.w_pre = bf(w_pre); a.H = static_cast<__bf16*>(H);
+  a.codes_y = codes; a.exps_y = exps;
+  a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d;
+  return stream_type == MST_TYPE_FP32 ? launch_fwd<float, false, true, false>(a, as_stream(stream))
+                                      : launch_fwd<__bf16, false, true, false>(a, as_stream(stream));
+}
+
+mst_status mst_prenorm_rebuild(const int8_t* codes, const uint8_t* exps, const void* w_pre, float w_offset, float eps,
+                               int64_t S, int64_t d, void* H, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!codes || !exps || !H) return MST_ERR_NULL_POINTER;
+  if (!good_norm(eps, w_offset)) return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(codes, S * d, 1, false, true);
+  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(w_pre, d, 2, false, false);
+  ops.add(H, S * d, 2, true, true);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormFwd a = {};
+  a.codes_x = codes; a.exps_x = exps; a.w_pre = bf(w_pre); a.H = static_cast<__bf16*>(H);
+  a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d;
+  return launch_fwd<__bf16, false, true, true>(a, as_stream(stream));
+}
+
+mst_status mst_prenorm_bwd(const void* dH, const void* X, const int8_t* codes, const uint8_t* exps, const void* dres,
+                           int32_t stream_type, const void* w_pre, float w_offset, float eps, int64_t S, int64_t d,
+                           void* workspace, size_t workspace_size, void* dX, float* dw_pre, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!dH || !dX || (!X && !codes && !exps)) return MST_ERR_NULL_POINTER;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps) || (X && codes) || (dw_pre && !w_pre))
+    return MST_ERR_BAD_ARGUMENT;
+  if (w_pre && !dw_pre) return MST_ERR_NULL_POINTER;
+  const size_t need = workspace_bytes(BwdPlan(S, d), d, 0);
+  if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
+  Operands ops;
+  ops.add(dH, S * d, 2, false, true);
+  ops.add(X, S * d, type_bytes(stream_type), false, true);
+  ops.add(codes, S * d, 1, false, true);
+  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(dres, S * d, type_bytes(stream_type), false, true);
+  ops.add(w_pre, d, 2, false, false);
+  ops.add(workspace, (int64_t)need, 1, true, false, 256);
+  ops.add(dX, S * d, type_bytes(stream_type), true, true);
+  ops.add(dw_pre, d, 4, true, false);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormBwd a = {};
+  a.dH = bf(dH); a.dres = dres; a.X = X; a.codes_x = codes; a.exps_x = exps; a.w_pre = bf(w_pre);
+  a.dX = dX; a.dw_pre = dw_pre;
+  a.offset = w_offset; a.eps = eps; a.scale = 1.f; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d;
+  return dispatch_bwd<true, false>(a, stream_type, 0, workspace, as_stream(stream));
+}
+
+mst_status mst_residual_fwd(const void* O, const void* X, int32_t stream_type, int32_t normalize, const void* w_post,
+                            float w_offset, float eps, const void* gate, int64_t gate_rows, float scale,
+                            int64_t S, int64_t d, void* Y, int8_t* codes, uint8_t* exps, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!O || !X || !Y) return MST_ERR_NULL_POINTER;
+  int64_t gate_groups = 0;
+  if ((s = check_gate(gate, gate_rows, scale, S, &gate_groups)) != MST_OK) return s;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps) || (w_post && !normalize)) return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(O, S * d, 2, false, true);
+  ops.add(X, S * d, type_bytes(stream_type), false, true);
+  ops.add(w_post, d, 2, false, false);
+  ops.add(gate, gate_groups * d, 2, false, false);
+  ops.add(Y, S * d, type_bytes(stream_type), true, true);
+  ops.add(codes, S * d, 1, true, true);
+  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormFwd a = {};
+  a.X = X; a.O = bf(O); a.w_post = bf(w_post); a.gate = bf(gate); a.Y = Y;
+  a.codes_o = codes; a.exps_o = exps;
+  a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
+  a.gate_rows = (int)std::min(gate_rows, S);
+  return stream_type == MST_TYPE_FP32 ? launch_fwd<float, true, false, false>(a, as_stream(stream))
+                                      : launch_fwd<__bf16, true, false, false>(a, as_stream(stream));
+}
+
+mst_status mst_residual_bwd(const void* dY, int32_t stream_type, const void* O, const int8_t* codes, const uint8_t* exps,
+                            int32_t normalize, const void* w_post, float w_offset, float eps,
+                            const void* gate, int64_t gate_rows, float scale, int64_t S, int64_t d,
+                            void* workspace, size_t workspace_size, void* dO, float* dw_post, float* dgate, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  int64_t gate_groups = 0;
+  if ((s = check_gate(gate, gate_rows, scale, S, &gate_groups)) != MST_OK) return s;
+  if (!dY || !dO) return MST_ERR_NULL_POINTER;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps) || (O && codes) || (w_post && !normalize) ||
+      (dw_post && !w_post) || (dgate && !gate))
+    return MST_ERR_BAD_ARGUMENT;
+  if ((w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes)) return MST_ERR_NULL_POINTER;
+  const size_t need = workspace_bytes(BwdPlan(S, d), d, gate_groups);
+  if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
+  if (!normalize && !gate) O = nullptr, codes = nullptr, exps = nullptr;
+  Operands ops;
+  ops.add(dY, S * d, type_bytes(stream_type), false, true);
+  ops.add(O, S * d, 2, false, true);
+  ops.add(codes, S * d, 1, false, true);
+  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(w_post, d, 2, false, false);
+  ops.add(gate, gate_groups * d, 2, false, false);
+  ops.add(workspace, (int64_t)need, 1, true, false, 256);
+  ops.add(dO, S * d, 2, true, true);
+  ops.add(dw_post, d, 4, true, false);
+  ops.add(dgate, gate_groups * d, 4, true, false);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormBwd a = {};
+  a.dY = dY; a.O = bf(O); a.codes_o = codes; a.exps_o = exps; a.w_post = bf(w_post); a.gate = bf(gate);
+  a.dO = static_cast<__bf16*>(dO); a.dw_post = dw_post; a.dgate = dgate;
+  a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
+  a.gate_rows = (int)std::min(gate_rows, S);
+  return dispatch_bwd<false, true>(a, stream_type, gate_groups, workspace, as_stream(stream));
+}
+
+mst_status mst_residual_prenorm_fwd(const void* O, const void* X, int32_t stream_type, int32_t normalize, const void* w_post,
+                                    const void* gate, int64_t gate_rows, float scale, const void* w_pre,
+                                    float w_offset, float eps, int64_t S, int64_t d, void* Y, void* H,
+                                    int8_t* codes_o, uint8_t* exps_o, int8_t* codes_y, uint8_t* exps_y, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  if (!O || !X || !Y || !H) return MST_ERR_NULL_POINTER;
+  int64_t gate_groups = 0;
+  if ((s = check_gate(gate, gate_rows, scale, S, &gate_groups)) != MST_OK) return s;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes_o, exps_o) || !both_or_neither(codes_y, exps_y) ||
+      (w_post && !normalize))
+    return MST_ERR_BAD_ARGUMENT;
+  Operands ops;
+  ops.add(O, S * d, 2, false, true);
+  ops.add(X, S * d, type_bytes(stream_type), false, true);
+  ops.add(w_post, d, 2, false, false);
+  ops.add(w_pre, d, 2, false, false);
+  ops.add(gate, gate_groups * d, 2, false, false);
+  ops.add(Y, S * d, type_bytes(stream_type), true, true);
+  ops.add(H, S * d, 2, true, true);
+  ops.add(codes_o, S * d, 1, true, true);
+  ops.add(exps_o, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(codes_y, S * d, 1, true, true);
+  ops.add(exps_y, S * tail_blocks(d), 1, true, false, 1);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormFwd a = {};
+  a.X = X; a.O = bf(O); a.w_post = bf(w_post); a.w_pre = bf(w_pre); a.gate = bf(gate);
+  a.Y = Y; a.H = static_cast<__bf16*>(H);
+  a.codes_o = codes_o; a.exps_o = exps_o; a.codes_y = codes_y; a.exps_y = exps_y;
+  a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
+  a.gate_rows = (int)std::min(gate_rows, S);
+  return stream_type == MST_TYPE_FP32 ? launch_fwd<float, true, true, false>(a, as_stream(stream))
+                                      : launch_fwd<__bf16, true, true, false>(a, as_stream(stream));
+}
+
+mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t stream_type,
+                                    const void* Y, const int8_t* codes_y, const uint8_t* exps_y,
+                                    const void* O, const int8_t* codes_o, const uint8_t* exps_o,
+                                    int32_t normalize, const void* w_post, const void* gate, int64_t gate_rows, float scale,
+                                    const void* w_pre, float w_offset, float eps, int64_t S, int64_t d,
+                                    void* workspace, size_t workspace_size, void* dY, void* dO,
+                                    float* dw_pre, float* dw_post, float* dgate, void* stream) {
+  mst_status s = check_shape(S, d);
+  if (s != MST_OK) return s;
+  int64_t gate_groups = 0;
+  if ((s = check_gate(gate, gate_rows, scale, S, &gate_groups)) != MST_OK) return s;
+  if (!dH || !dY || !dO || (!Y && !codes_y && !exps_y)) return MST_ERR_NULL_POINTER;
+  if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes_o, exps_o) || !both_or_neither(codes_y, exps_y) ||
+      (O && codes_o) || (Y && codes_y) || (w_post && !normalize) || (dw_post && !w_post) || (dgate && !gate) || (dw_pre && !w_pre))
+    return MST_ERR_BAD_ARGUMENT;
+  if ((w_pre && !dw_pre) || (w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes_o)) return MST_ERR_NULL_POINTER;
+  const size_t need = workspace_bytes(BwdPlan(S, d), d, gate_groups);
+  if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
+  if (!normalize && !gate) O = nullptr, codes_o = nullptr, exps_o = nullptr;
+  Operands ops;
+  ops.add(dH, S * d, 2, false, true);
+  ops.add(dres, S * d, type_bytes(stream_type), false, true);
+  ops.add(Y, S * d, type_bytes(stream_type), false, true);
+  ops.add(codes_y, S * d, 1, false, true);
+  ops.add(exps_y, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(O, S * d, 2, false, true);
+  ops.add(codes_o, S * d, 1, false, true);
+  ops.add(exps_o, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(w_post, d, 2, false, false);
+  ops.add(w_pre, d, 2, false, false);
+  ops.add(gate, gate_groups * d, 2, false, false);
+  ops.add(workspace, (int64_t)need, 1, true, false, 256);
+  ops.add(dY, S * d, type_bytes(stream_type), true, true);
+  ops.add(dO, S * d, 2, true, true);
+  ops.add(dw_pre, d, 4, true, false);
+  ops.add(dw_post, d, 4, true, false);
+  ops.add(dgate, gate_groups * d, 4, true, false);
+  if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
+  NormBwd a = {};
+  a.dH = bf(dH); a.dres = dres; a.X = Y; a.codes_x = codes_y; a.exps_x = exps_y;
+  a.O = bf(O); a.codes_o = codes_o; a.exps_o = exps_o;
+  a.w_pre = bf(w_pre); a.w_post = bf(w_post); a.gate = bf(gate);
+  a.dX = dY; a.dO = static_cast<__bf16*>(dO); a.dw_pre = dw_pre; a.dw_post = dw_post; a.dgate = dgate;
+  a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
+  a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
+  a.gate_rows = (int)std::min(gate_rows, S);
+  return dispatch_bwd<true, true>(a, stream_type, gate_groups, workspace, as_stream(stream));
+}
+
+}  // extern "C"
