@@ -160,8 +160,8 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
                                     float* dw_pre, float* dw_post, float* dgate, void* stream);
 
 /*
- * How a backward call goes over the rows (host, pure; a test aid): info = {threads of a workgroup, rows of a
- * workgroup, workgroups}; all three calls alike.
+ * How a backward call goes over the rows (host, pure; a test aid): info = {threads of a workgroup, teams of lanes in it that
+ * hold a row each, rows that a team takes in turn, workgroups}; all three calls alike.
  */
 mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t* info);
 

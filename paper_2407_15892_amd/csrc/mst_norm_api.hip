@@ -58,67 +58,77 @@ mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t 
   return MST_OK;
 }
 
-// How a row is held: chunks of eight columns per lane, lanes (whole waves).
+// How rows are held: chunks of eight columns per lane, and teams of lanes.  A workgroup has as many teams as fit 512 lanes.
 struct RowPlan {
-  int chunks, threads;
+  int chunks, teams;
+  Team team;
   explicit RowPlan(int64_t d) {
     chunks = d <= 8 * 64 * kNormMaxWaves ? 1 : 2;
-    threads = (int)((d + 8 * 64 * chunks - 1) / (8 * 64 * chunks)) * 64;
+    team.lanes = 8;
+    while (team.lanes < 64 && team.lanes * 8 < d) team.lanes *= 2;
+    team.waves = (int)((d + 8 * 64 * chunks - 1) / (8 * 64 * chunks));
+    teams = std::max(1, 512 / (team.lanes * team.waves));
   }
+  int threads() const { return team.lanes * team.waves * teams; }
 };
 
-constexpr int kFwdRows[2] = {2, 1}, kBwdRows[2] = {2, 1};      // rows at a time with one and with two chunks
+constexpr int kFwdRows[2] = {2, 1};      // rows of a team with one and with two chunks
 
-// Rows of a workgroup of the backward calls.
+// Rows of a team of the backward calls.
 struct BwdPlan {
   RowPlan row;
-  int rows;
-  int64_t groups;
+  int rows, teams;                       // of a team; in all
+  int64_t groups;                        // workgroups
   BwdPlan(int64_t S, int64_t d) : row(d) {
-    const int64_t most = kNumCu * std::max(1, 1024 / row.threads);
-    const int at_a_time = kBwdRows[row.chunks - 1];
-    rows = (int)((((S + most - 1) / most) + at_a_time - 1) / at_a_time * at_a_time);
-    groups = (S + rows - 1) / rows;
+    const int64_t most = kNumCu * std::max(1, 1024 / row.threads()) * row.teams;
+    rows = (int)((S + most - 1) / most);
+    const int64_t needed = (S + rows - 1) / rows;
+    groups = (needed + row.teams - 1) / row.teams;
+    teams = (int)(groups * row.teams);
   }
 };
 
-size_t workspace_bytes(const BwdPlan& p, int64_t d, int64_t gate_groups) {      // dw_pre, dw_post, two of the gate's rows
-  return p.groups == 1 && gate_groups <= 1 ? 256 : mst_host::align_up((size_t)p.groups * d * 4 * (gate_groups > 1 ? 4 : 2), 256);
+size_t workspace_bytes(const BwdPlan& p, int64_t d, int64_t gate_groups) {      // dw_pre, dw_post by workgroup, two of the gate's rows by team
+  return mst_host::align_up((size_t)d * 4 * ((p.groups > 1 ? 2 * p.groups : 0) + (gate_groups > 1 ? 2 * p.teams : 0)) + 256, 256);
 }
 
 template <class T, bool kRes, bool kPre, bool kRebuild, int kNc>
-mst_status launch_fwd_chunks(NormFwd a, int threads, hipStream_t st) {
-  constexpr int kRows = kFwdRows[kNc - 1];
-  const int64_t most = (int64_t(1) << 31) / threads * kRows;      // a launch has fewer than 2^32 lanes
+mst_status launch_fwd_chunks(NormFwd a, const RowPlan& p, hipStream_t st) {
+  const int64_t kRows = kFwdRows[kNc - 1] * p.teams;              // of a workgroup
+  const int64_t most = (int64_t(1) << 31) / p.threads() * kRows;  // a launch has fewer than 2^32 lanes
+  a.team = p.team;
   for (int64_t r = 0; r < a.S; r += most) {
     a.row0 = (int)r;
-    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kNc, kRows>), dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)),
-                       dim3(threads), 0, st, a);
+    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kNc, kFwdRows[kNc - 1]>),
+                       dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)), dim3(p.threads()), 0, st, a);
   }
   return check_launch();
 }
 template <class T, bool kRes, bool kPre, bool kRebuild>
 mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   const RowPlan p(a.d);
-  return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p.threads, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p.threads, st);
+  return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p, st);
 }
 
 template <class T, bool kPre, bool kRes, bool kMany>
 mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream_t st) {
   const BwdPlan p(a.S, a.d);
   a.rows = p.rows;
+  a.teams = p.teams;
+  a.team = p.row.team;
   float* const ws = static_cast<float*>(workspace);
-  const size_t part = (size_t)p.groups * a.d;
+  const size_t part = p.groups > 1 ? (size_t)p.groups * a.d : 0;
   a.part_pre = ws;
   a.part_post = ws + part;
   a.part_gate = ws + 2 * part;
-  const dim3 grid((unsigned)p.groups);
+  const dim3 grid((unsigned)p.groups), block(p.row.threads());
+  const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // at most 16 KB
   if (p.row.chunks == 1)
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 1, kBwdRows[0]>), grid, dim3(p.row.threads), 0, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 1>), grid, block, lds, st, a);
   else
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 2, kBwdRows[1]>), grid, dim3(p.row.threads), 0, st, a);
-  if (p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) {
-    const int64_t items = !kMany ? 0 : a.gate_rows >= a.rows ? gate_groups : p.groups - 1;
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 2>), grid, block, lds, st, a);
+  const int64_t items = !kMany || a.rows % a.gate_rows == 0 ? 0 : a.gate_rows >= a.rows ? gate_groups : p.teams - 1;
+  if ((p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) || items) {
     hipLaunchKernelGGL(k_norm_reduce<kMany>, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + items)), dim3(kReduceThreads), 0, st, a, (int)p.groups);
   }
   return check_launch();
@@ -186,9 +196,10 @@ mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t* info) {
   if (s != MST_OK) return s;
   if (!info) return MST_ERR_NULL_POINTER;
   const BwdPlan p(S, d);
-  info[0] = p.row.threads;
-  info[1] = p.rows;
-  info[2] = p.groups;
+  info[0] = p.row.threads();
+  info[1] = p.row.teams;
+  info[2] = p.rows;
+  info[3] = p.groups;
   return MST_OK;
 }
 

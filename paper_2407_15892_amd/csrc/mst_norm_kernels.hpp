@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace mst {
 
 typedef float norm_f32x4 __attribute__((ext_vector_type(4)));
@@ -182,38 +184,64 @@ __global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* code
 
 // ---- sums over a row -----------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float wave_sum(float x) {      // of all 64 lanes, in all of them, in one order
-  x += dpp_f32<kQuadSwap1>(x);
-  x += dpp_f32<kQuadSwap2>(x);
-  x += dpp_f32<kHalfMirror>(x);
-  x += dpp_f32<kMirror>(x);
-  const int b = __float_as_int(x);
-  return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
-         (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+// Lanes that hold a row together (a team): 8, 16 or 32 of a wave for short rows, else `waves` whole waves.
+struct Team {
+  int lanes, waves;        // lanes: of one wave
+  __device__ int threads() const { return lanes * waves; }
+};
+
+template <int kN> __device__ __forceinline__ void add_all(float (&v)[kN], const float (&o)[kN]) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] += o[i];
 }
+template <int kCtrl, int kN> __device__ __forceinline__ void add_dpp(float (&v)[kN]) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] += dpp_f32<kCtrl>(v[i]);
+}
+__device__ __forceinline__ float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
 
 constexpr int kNormMaxWaves = 16;
 
-// Sums of kN values over the workgroup, in every lane.  Two buffers in turn: one barrier a sum.
+// A barrier that waits for this wave's LDS accesses, but not for global loads that are on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Sums of kN values over a team, in every one of its lanes, always in the same order.  All of the workgroup calls it.  Two
+// buffers in turn: one barrier a sum, none where a team is within a wave.
 template <int kN> struct RowSums {
   float (*lds)[kNormMaxWaves][kN];       // [2]
+  const Team team;
   int turn = 0;
-  __device__ explicit RowSums(float (*buffers)[kNormMaxWaves][kN]) : lds(buffers) {}
+  __device__ RowSums(float (*buffers)[kNormMaxWaves][kN], Team t) : lds(buffers), team(t) {}
   __device__ __forceinline__ void operator()(float (&v)[kN]) {
+    add_dpp<kQuadSwap1>(v);
+    add_dpp<kQuadSwap2>(v);
+    add_dpp<kHalfMirror>(v);
+    if (team.lanes == 8) return;
+    add_dpp<kMirror>(v);
+    if (team.lanes == 16) return;
+    if (team.lanes == 32) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = wave_sum(v[i]);
-    const int waves = blockDim.x / 64;
-    if (waves == 1) return;
+      for (int i = 0; i < kN; ++i) v[i] += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v[i]), 0x401f));   // lane ^ 16
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = (lane_of(v[i], 0) + lane_of(v[i], 16)) + (lane_of(v[i], 32) + lane_of(v[i], 48));
+    if (team.waves == 1) return;
+    const int wave = threadIdx.x / 64, first = wave / team.waves * team.waves;
     float (*const at)[kN] = lds[turn];
     turn ^= 1;
     if (threadIdx.x % 64 == 0) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) at[threadIdx.x / 64][i] = v[i];
+      for (int i = 0; i < kN; ++i) at[wave][i] = v[i];
     }
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < kN; ++i) v[i] = 0.f;
-    for (int w = 0; w < waves; ++w) {
+    for (int w = first; w < first + team.waves; ++w) {
 #pragma unroll
       for (int i = 0; i < kN; ++i) v[i] += at[w][i];
     }
@@ -235,6 +263,7 @@ struct NormFwd {
   float offset, eps, scale, inv_d;
   int S, d, normalize, gate_rows;
   int row0;                        // first row of the launch
+  Team team;
 };
 
 // The weights of eight columns.
@@ -253,12 +282,13 @@ __device__ __forceinline__ void store_packed(const Packed& p, int8_t* codes, uin
   if (threadIdx.x % 4 == 0) exps[row * ((d + 31) / 32) + col / 32] = (uint8_t)p.exp;
 }
 
-// kRb rows per workgroup, kNc chunks of 8 columns per lane.
+// kRb rows per team, kNc chunks of 8 columns per lane.
 template <class T, bool kRes, bool kPre, bool kRebuild, int kNc, int kRb>
 __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   __shared__ float lds[2][kNormMaxWaves][kRb];
-  RowSums<kRb> row_sums(lds);
-  const int r0 = a.row0 + blockIdx.x * kRb, d = a.d;
+  RowSums<kRb> row_sums(lds, a.team);
+  const int threads = a.team.threads(), lane = threadIdx.x % threads, d = a.d;
+  const int r0 = a.row0 + (blockIdx.x * (blockDim.x / threads) + threadIdx.x / threads) * kRb;
   const T* const X = static_cast<const T*>(a.X);
   float x[kRb][kNc][8];
   Eight<T> raw[kRb][kNc];
@@ -268,7 +298,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   for (int r = 0; r < kRb; ++r)
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * 8;
+      const int col = (k * threads + lane) * 8;
       const size_t at = (size_t)(r0 + r) * d + col;
       if (r0 + r < a.S && col < d) {
         if (kRebuild) c[r][k].load(a.codes_x + at, a.exps_x + (size_t)(r0 + r) * ((d + 31) / 32) + col / 32);
@@ -296,7 +326,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * 8;
+      const int col = (k * threads + lane) * 8;
       const bool on = col < d;
       float w[8];
       if (a.normalize) weights(a.w_post, a.offset, col, on, w);
@@ -335,7 +365,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
         if (kRebuild) c[r][k].get(x[r][k]);
         else raw[r][k].get(x[r][k]);
         if (!kRebuild && a.codes_y) {
-          const int col = (k * blockDim.x + threadIdx.x) * 8;
+          const int col = (k * threads + lane) * 8;
           const Packed p = pack_eight(x[r][k]);
           if (r0 + r < a.S && col < d) store_packed(p, a.codes_y, a.exps_y, r0 + r, d, col);
         }
@@ -356,7 +386,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   for (int r = 0; r < kRb; ++r) rstd[r] = rsqrtf(fmaf(rstd[r], a.inv_d, a.eps));
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    const int col = (k * blockDim.x + threadIdx.x) * 8;
+    const int col = (k * threads + lane) * 8;
     float w[8];
     weights(a.w_pre, a.offset, col, col < d, w);
 #pragma unroll
@@ -384,282 +414,290 @@ struct NormBwd {
   __bf16* dO;
   float *dw_pre, *dw_post, *dgate; // NULL: not wanted
   float *part_pre, *part_post;     // [workgroups][d] each
-  float* part_gate;                // [2][workgroups][d]: of the gate's row that began before the workgroup's rows; of the one that goes on behind them
+  float* part_gate;                // [2][teams][d]: of the gate's row that began before the team's rows; of the one that goes on behind them
   float offset, eps, scale, inv_d;
   int S, d, normalize, gate_rows;
-  int rows;                        // of a workgroup
+  int rows, teams;                 // of a team; in all
+  Team team;
 };
 
-// dw_post and dgate of eight columns from t = sum of dY * N / w_post over the rows of a call without a gate, or whose
-// rows share one gate.
-__device__ __forceinline__ void finish_post(const NormBwd& a, int col, const float (&t)[8]) {
-  float w[8], g[8], v[8];
-  weights(a.gate, 0.f, col, true, g);
-  if (a.dw_post) {
+// A row's eight entries as loaded: the tensor's, or codes and exponent of its checkpoint.
+template <class T> struct Source {
+  unsigned u[sizeof(T) * 2];
+  __device__ void load(const void* X, const int8_t* codes, const uint8_t* exps, size_t at, size_t block) {
+    if (codes) {
+      const norm_u32x2 c = *reinterpret_cast<const norm_u32x2*>(codes + at);
+      u[0] = c[0]; u[1] = c[1];
+      u[2] = exps[block];
+    } else {
+      const norm_u32x4* const p = reinterpret_cast<const norm_u32x4*>(static_cast<const T*>(X) + at);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = a.scale * g[i] * t[i];
-    Eight<float> e;
-    e.set(v);
-    e.store(a.dw_post + col);
+      for (unsigned i = 0; i < sizeof(T) / 2; ++i) {
+        const norm_u32x4 w = p[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[4 * i + k] = w[k];
+      }
+    }
   }
-  if (a.dgate) {
-    weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, true, w);
+  __device__ void get(bool checkpoint, float (&v)[8]) const {
+    if (checkpoint) {
+      EightCodes c;
+      c.c = {u[0], u[1]};
+      c.e = u[2];
+      c.get(v);
+    } else if (sizeof(T) == 2) {
+      Eight<__bf16> e;
+      e.u = {u[0], u[1], u[2], u[3]};
+      e.get(v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = a.scale * w[i] * t[i];
-    Eight<float> e;
-    e.set(v);
-    e.store(a.dgate + col);
+      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i % (sizeof(T) * 2)]);
+    }
+  }
+};
+
+// dw_post and dgate of four or eight columns from t = sum of dY * N / w_post over the rows of a call without a gate, or
+// whose rows share one gate.
+template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, int col, const float* t) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    if (a.dw_post) a.dw_post[col + i] = a.scale * (a.gate ? (float)a.gate[col + i] : 1.f) * t[i];
+    if (a.dgate) a.dgate[col + i] = a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col + i] : 1.f) : 1.f) * t[i];
   }
 }
 
-// kMany: more than one row of gates.
-template <class T, bool kPre, bool kRes, bool kMany, int kNc, int kRb>
+// A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
+// for their columns.  kMany: more than one row of gates.
+// With x the row of X, q its rstd, a = dH * ~w: the gradient is dres + q a - x q^3 sum(a x) / d; likewise for O with
+// b = dY * f, f = scale * gate * ~w_post.  One sum over the row waits for another where both norms are there.
+template <class T, bool kPre, bool kRes, bool kMany, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
-  __shared__ float lds1[2][kNormMaxWaves][kFirst * kRb], lds2[2][kNormMaxWaves][kRb];
-  RowSums<kFirst * kRb> first_sums(lds1);
-  RowSums<kRb> second_sums(lds2);
-  const int d = a.d, blocks = (d + 31) / 32;
-  const int begin = blockIdx.x * a.rows, end = min(begin + a.rows, a.S);
+  __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
+  extern __shared__ float lds_columns[];
+  RowSums<kFirst> first_sums(lds1, a.team);
+  RowSums<1> second_sum(lds2, a.team);
+  const int d = a.d, blocks = (d + 31) / 32, threads = a.team.threads(), lane = threadIdx.x % threads;
+  const int teams = blockDim.x / threads, in_block = threadIdx.x / threads, team = blockIdx.x * teams + in_block;
+  const int64_t first_row = (int64_t)team * a.rows;
+  const int begin = (int)min(first_row, (int64_t)a.S), end = (int)min(first_row + a.rows, (int64_t)a.S);
   const bool need_o = kRes && (a.O || a.codes_o);
-  float acc_pre[kNc][8] = {}, acc_post[kNc][8] = {}, acc_gate[kNc][8] = {};
-  int group = kMany ? begin / a.gate_rows : 0;      // the gate's row that acc_gate belongs to
-  for (int r0 = begin; r0 < end; r0 += kRb) {
-    Eight<__bf16> dh[kRb][kNc], o[kRb][kNc];
-    Eight<T> x[kRb][kNc], dy[kRb][kNc];
-    EightCodes cx[kRb][kNc], co[kRb][kNc];
+  float acc_pre[kNc][8] = {}, acc_group[kNc][8] = {}, acc_post[kNc][8] = {};
+  float w[kNc][8], f[kNc][8];
+  int group = 0, group_end = 0;                  // the gate's row that f and acc_group belong to, and the row behind its last
+  if (kMany) group = begin / a.gate_rows - 1, group_end = begin;
+  auto column = [&](int k) { return (k * threads + lane) * 8; };
+  auto load_f = [&](int k) {
+    const int col = column(k);
+    weights(a.gate ? a.gate + (kMany ? (size_t)group * d : 0) : nullptr, 0.f, col, col < d, f[k]);
+    float wo[8];
+    weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, col < d, wo);
 #pragma unroll
-    for (int r = 0; r < kRb; ++r)
-#pragma unroll
-      for (int k = 0; k < kNc; ++k) {
-        const int col = (k * blockDim.x + threadIdx.x) * 8;
-        if (r0 + r >= end || col >= d) continue;
-        const size_t at = (size_t)(r0 + r) * d + col, block = (size_t)(r0 + r) * blocks + col / 32;
-        if (kPre) {
-          dh[r][k].load(a.dH + at);
-          if (a.codes_x) cx[r][k].load(a.codes_x + at, a.exps_x + block);
-          else x[r][k].load(static_cast<const T*>(a.X) + at);
-          if (a.dres) dy[r][k].load(static_cast<const T*>(a.dres) + at);
-        } else {
-          dy[r][k].load(static_cast<const T*>(a.dY) + at);
-        }
-        if (need_o) {
-          if (a.codes_o) co[r][k].load(a.codes_o + at, a.exps_o + block);
-          else o[r][k].load(a.O + at);
-        }
-      }
-    auto get_x = [&](int r, int k, float (&v)[8]) { a.codes_x ? cx[r][k].get(v) : x[r][k].get(v); };
-    auto get_o = [&](int r, int k, float (&v)[8]) { a.codes_o ? co[r][k].get(v) : o[r][k].get(v); };
-    auto get_gate = [&](int r, int col, float (&g)[8]) {      // times the scale
-      const bool on = col < d && r0 + r < end;
-      weights(a.gate ? a.gate + (kMany ? (size_t)((unsigned)(r0 + r) / (unsigned)a.gate_rows) * d : 0) : nullptr, 0.f, col, on, g);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] *= a.scale;
-    };
-    float sums[kFirst * kRb];
-#pragma unroll
-    for (int i = 0; i < kFirst * kRb; ++i) sums[i] = 0.f;
+    for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
+  };
+  Eight<__bf16> dh_next[kNc];
+  Source<T> x_next[kNc];
+  Eight<T> dy_next[kNc];
+  Source<__bf16> o_next[kNc];
+  auto load = [&](int row) {
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * 8;
-      float w[8], wo[8];
-      if (kPre) weights(a.w_pre, a.offset, col, col < d, w);
-      if (kRes && a.normalize) weights(a.w_post, a.offset, col, col < d, wo);
-#pragma unroll
-      for (int r = 0; r < kRb; ++r) {
-        float* const s = sums + r * kFirst;
-        if (kPre) {
-          float xv[8], hv[8];
-          get_x(r, k, xv);
-          dh[r][k].get(hv);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            s[0] = fmaf(xv[i], xv[i], s[0]);
-            s[1] = fmaf(hv[i] * w[i], xv[i], s[1]);
-          }
-        }
-        if (kRes && a.normalize) {
-          float ov[8];
-          get_o(r, k, ov);
-          float* const so = s + (kPre ? 2 : 0);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) so[0] = fmaf(ov[i], ov[i], so[0]);
-          if (!kPre) {
-            float g[8], yv[8];
-            get_gate(r, col, g);
-            dy[r][k].get(yv);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) so[1] = fmaf(g[i] * yv[i] * wo[i], ov[i], so[1]);
-          }
-        }
+      const int col = column(k);
+      if (row >= end || col >= d) continue;
+      const size_t at = (size_t)row * d + col, block = (size_t)row * blocks + col / 32;
+      if (kPre) {
+        dh_next[k].load(a.dH + at);
+        x_next[k].load(a.X, a.codes_x, a.exps_x, at, block);
+        if (a.dres) dy_next[k].load(static_cast<const T*>(a.dres) + at);
+      } else {
+        dy_next[k].load(static_cast<const T*>(a.dY) + at);
       }
+      if (need_o) o_next[k].load(a.O, a.codes_o, a.exps_o, at, block);
     }
-    if (kPre || a.normalize) first_sums(sums);
-    float dyv[kRb][kNc][8];
-    float post[kRb];               // sum of b * O
-    float rstd_o[kRb];
+  };
 #pragma unroll
-    for (int r = 0; r < kRb; ++r) {
-      post[r] = 0.f;
-      rstd_o[r] = kRes && a.normalize ? rsqrtf(fmaf(sums[r * kFirst + (kPre ? 2 : 0)], a.inv_d, a.eps)) : 1.f;
-      if (!kPre) post[r] = sums[r * kFirst + (kFirst - 1)];
+  for (int k = 0; k < kNc; ++k) {
+    if (kPre) weights(a.w_pre, a.offset, column(k), column(k) < d, w[k]);
+    if (kRes && !kMany) load_f(k);
+#pragma unroll
+    for (int i = 0; i < 4 * (int)sizeof(T) / 2; ++i) x_next[k].u[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o_next[k].u[i] = 0;
+  }
+  load(begin);
+  for (int i_row = 0; i_row < a.rows; ++i_row) {         // as often in every team, for the barriers
+    const int row = begin + i_row;
+    const bool on = row < end;
+    const float live = on ? 1.f : 0.f;                   // what is left in the registers behind the last row is not summed up
+    float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
+    float sums[kFirst];
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) sums[i] = 0.f;
+    if (kMany && on && row == group_end) {
+      ++group;
+      group_end = (int)min((int64_t)(group + 1) * a.gate_rows, (int64_t)a.S);
+#pragma unroll
+      for (int k = 0; k < kNc; ++k) load_f(k);
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * 8;
-      float w[8], wo[8];
-      if (kPre) weights(a.w_pre, a.offset, col, col < d, w);
-      if (kPre && kRes && a.normalize) weights(a.w_post, a.offset, col, col < d, wo);
-#pragma unroll
-      for (int r = 0; r < kRb; ++r) {
-        dy[r][k].get(dyv[r][k]);
-        if (!kPre) continue;
-        const float rstd = rsqrtf(fmaf(sums[r * kFirst], a.inv_d, a.eps));
-        const float c = sums[r * kFirst + 1] * rstd * a.inv_d;
-        float xv[8], hv[8];
-        get_x(r, k, xv);
-        dh[r][k].get(hv);
+      dy_next[k].get(dy[k]);
+      if (kPre) {
+        x_next[k].get(a.codes_x != nullptr, x[k]);
+        dh_next[k].get(dh[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float xh = xv[i] * rstd;
-          acc_pre[k][i] = fmaf(hv[i], xh, acc_pre[k][i]);
-          dyv[r][k][i] += rstd * (hv[i] * w[i] - xh * c);
+          sums[0] = fmaf(x[k][i], x[k][i], sums[0]);
+          sums[1] = fmaf(dh[k][i] * w[k][i], x[k][i], sums[1]);
         }
-        if (r0 + r < end && col < d) {
-          Eight<T> e;
-          e.set(dyv[r][k]);
-          e.store(static_cast<T*>(a.dX) + (size_t)(r0 + r) * d + col);
-        }
-        if (kRes && a.normalize) {
-          float ov[8], g[8];
-          get_o(r, k, ov);
-          get_gate(r, col, g);
+      }
+      if (kRes) {
+        o_next[k].get(a.codes_o != nullptr, o[k]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) post[r] = fmaf(g[i] * dyv[r][k][i] * wo[i], ov[i], post[r]);
+        for (int i = 0; i < 8; ++i) {
+          sums[kPre ? 2 : 0] = fmaf(o[k][i], o[k][i], sums[kPre ? 2 : 0]);
+          if (!kPre) sums[1] = fmaf(dy[k][i] * f[k][i], o[k][i], sums[1]);
+        }
+      }
+    }
+    load(row + 1);
+    if (kPre || a.normalize) first_sums(sums);
+    float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
+    if (kPre) {
+      const float q = rsqrtf(fmaf(sums[0], a.inv_d, a.eps)), c = -q * q * q * sums[1] * a.inv_d;
+#pragma unroll
+      for (int k = 0; k < kNc; ++k) {
+        const int col = column(k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float u = dh[k][i] * (q * live);
+          acc_pre[k][i] = fmaf(u, x[k][i], acc_pre[k][i]);
+          dy[k][i] = fmaf(u, w[k][i], dy[k][i]);
+          dy[k][i] = fmaf(x[k][i], c, dy[k][i]);
+          if (kRes) post[0] = fmaf(dy[k][i] * f[k][i], o[k][i], post[0]);
+        }
+        if (on && col < d) {
+          Eight<T> e;
+          e.set(dy[k]);
+          e.store(static_cast<T*>(a.dX) + (size_t)row * d + col);
         }
       }
     }
     if (!kRes) continue;
-    if (kPre && a.normalize) second_sums(post);
+    if (kPre && a.normalize) second_sum(post);
+    const float q = a.normalize ? rsqrtf(fmaf(sums[kPre ? 2 : 0], a.inv_d, a.eps)) : 1.f;
+    const float c = a.normalize ? -q * q * q * post[0] * a.inv_d : 0.f;
 #pragma unroll
-    for (int r = 0; r < kRb; ++r) {
-      const bool last = kMany && r0 + r < end && (r0 + r + 1 == end || (r0 + r + 1) % a.gate_rows == 0);
+    for (int k = 0; k < kNc; ++k) {
+      const int col = column(k);
+      float out[8];
 #pragma unroll
-      for (int k = 0; k < kNc; ++k) {
-        const int col = (k * blockDim.x + threadIdx.x) * 8;
-        const bool on = col < d && r0 + r < end;
-        float g[8], ov[8] = {}, out[8], wo[8];
-        get_gate(r, col, g);
-        if (need_o) get_o(r, k, ov);
-        if (a.normalize) weights(a.w_post, a.offset, col, col < d, wo);
-        const float c = post[r] * rstd_o[r] * a.inv_d;
+      for (int i = 0; i < 8; ++i) {
+        const float u = dy[k][i] * (q * live);
+        out[i] = fmaf(o[k][i], c, u * f[k][i]);
+        acc_group[k][i] = fmaf(u, o[k][i], acc_group[k][i]);
+      }
+      if (!on || col >= d) continue;
+      Eight<__bf16> e;
+      e.set(out);
+      e.store(a.dO + (size_t)row * d + col);
+      if (kMany && (row + 1 == end || row + 1 == group_end)) {        // the team's last row of this row of the gate
+        const bool whole = (int64_t)group * a.gate_rows >= begin && group_end <= end;
+        const bool began_before = (int64_t)group * a.gate_rows < begin;
+        float g[8], wo[8];
+        weights(a.gate + (size_t)group * d, 0.f, col, true, g);
+        weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, true, wo);
+        Eight<float> sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float oh = ov[i] * rstd_o[r], e = g[i] * dyv[r][k][i];
-          out[i] = a.normalize ? rstd_o[r] * (e * wo[i] - oh * c) : e;
-          const float t = dyv[r][k][i] * oh;
-          if (kMany) {
-            acc_post[k][i] = fmaf(e, oh, acc_post[k][i]);
-            acc_gate[k][i] += t;
-          } else {
-            acc_post[k][i] += t;
-          }
+          acc_post[k][i] = fmaf(g[i] * a.scale, acc_group[k][i], acc_post[k][i]);
+          if (whole) acc_group[k][i] *= a.scale * wo[i];
         }
-        if (on) {
-          Eight<__bf16> e;
-          e.set(out);
-          e.store(a.dO + (size_t)(r0 + r) * d + col);
-        }
-        if (kMany && last) {
-          const int64_t from = (int64_t)group * a.gate_rows, to = min(from + a.gate_rows, (int64_t)a.S);
-          if (from >= begin && to <= end) {
-            float wv[8];
-            weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, col < d, wv);
+        sum.set(acc_group[k]);
+        sum.store((whole ? a.dgate + (size_t)group * d : a.part_gate + ((size_t)(began_before ? 0 : a.teams) + team) * d) + col);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) wv[i] *= a.scale * acc_gate[k][i];
-            Eight<float> e;
-            e.set(wv);
-            if (col < d) e.store(a.dgate + (size_t)group * d + col);
-          } else {
-            Eight<float> e;
-            e.set(acc_gate[k]);
-            if (col < d) e.store(a.part_gate + ((size_t)(from < begin ? 0 : gridDim.x) + blockIdx.x) * d + col);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc_gate[k][i] = 0.f;
-        }
+        for (int i = 0; i < 8; ++i) acc_group[k][i] = 0.f;
       }
-      if (last) ++group;
     }
   }
+  // the teams' sums, then to the workspace, or where they belong if this is the only workgroup
+  auto add_teams = [&](const float (&acc)[kNc][8], auto put) {
+    if (teams == 1) {
 #pragma unroll
-  for (int k = 0; k < kNc; ++k) {
-    const int col = (k * blockDim.x + threadIdx.x) * 8;
-    if (col >= d) continue;
-    Eight<float> e;
-    if (kPre && a.dw_pre) {
-      e.set(acc_pre[k]);
-      e.store((gridDim.x == 1 ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d) + col);
+      for (int k = 0; k < kNc; ++k)
+        if (column(k) < d) put(column(k), acc[k], std::integral_constant<int, 8>());
+      return;
     }
-    if (kRes && (a.dw_post || (a.dgate && !kMany))) {
-      if (gridDim.x == 1 && !kMany) {
-        finish_post(a, col, acc_post[k]);
-      } else {
-        e.set(acc_post[k]);
-        e.store((gridDim.x == 1 ? a.dw_post : a.part_post + (size_t)blockIdx.x * d) + col);
-      }
+    __syncthreads();
+    if (column(0) < d) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lds_columns[in_block * d + column(0) + i] = acc[0][i];
     }
+    __syncthreads();
+    for (int col = threadIdx.x; col < d; col += blockDim.x) {
+      float sum[1] = {0.f};
+      for (int t = 0; t < teams; ++t) sum[0] += lds_columns[t * d + col];
+      put(col, sum, std::integral_constant<int, 1>());
+    }
+  };
+  auto store = [&](float* to) {
+    return [=](int col, const float* v, auto n) {
+#pragma unroll
+      for (int i = 0; i < decltype(n)::value; ++i) to[col + i] = v[i];
+    };
+  };
+  if (kPre && a.dw_pre) add_teams(acc_pre, store(gridDim.x == 1 ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d));
+  if (kRes && kMany && a.dw_post) add_teams(acc_post, store(gridDim.x == 1 ? a.dw_post : a.part_post + (size_t)blockIdx.x * d));
+  if (kRes && !kMany && (a.dw_post || a.dgate)) {
+    if (gridDim.x == 1) add_teams(acc_group, [&](int col, const float* v, auto n) { finish_post<decltype(n)::value>(a, col, v); });
+    else add_teams(acc_group, store(a.part_post + (size_t)blockIdx.x * d));
   }
 }
 
-// Sums of the workgroups' sums: blockIdx.y = 0 dw_pre, 1 dw_post (and the gradient of a single row of gates), from 2 on the
-// rows of the gate that lie in more than one workgroup: each row of the gate in turn where it has at least as
-// many rows as a workgroup, else those across the border behind each workgroup.  A workgroup takes 64 columns: 16 lanes of
-// four, and 16 groups of lanes that share out the workgroups, summed up in order.
-constexpr int kReduceThreads = 256, kReduceCols = 64;
+// Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre, 1 dw_post (and the gradient of a single row of gates); from
+// 2 on the teams' sums for rows of the gate that lie in more than one team: each row of the gate in turn where it has at
+// least as many rows as a team, else those across the border behind each team.  A workgroup takes 64 columns: 16 lanes of four, and
+// groups of 16 lanes that share out the sums, added up in order.
+constexpr int kReduceThreads = 1024, kReduceCols = 64, kReduceSlices = kReduceThreads / 16;
 template <bool kMany>
 __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n) {
-  __shared__ norm_f32x4 lds[16][16];
+  __shared__ norm_f32x4 lds[kReduceSlices][16];
   const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, d = a.d;
   const int col = blockIdx.x * kReduceCols + lane * 4;
   const float* part = blockIdx.y == 0 ? a.part_pre : a.part_post;
   int first = 0, last = n - 1, group = 0;
-  if (blockIdx.y == 0 ? !a.dw_pre : blockIdx.y == 1 ? !(a.dw_post || (a.dgate && !kMany)) : !kMany) return;
+  if (blockIdx.y < 2 && (n == 1 || (blockIdx.y == 0 ? !a.dw_pre : !(a.dw_post || (a.dgate && !kMany))))) return;
   if (blockIdx.y >= 2) {
     const int i = blockIdx.y - 2;
     group = a.gate_rows >= a.rows ? i : (int)(((int64_t)(i + 1) * a.rows - 1) / a.gate_rows);
     const int64_t from = (int64_t)group * a.gate_rows, to = min(from + a.gate_rows, (int64_t)a.S);
     first = (int)(from / a.rows);
     last = (int)((to - 1) / a.rows);
-    if (first == last) return;               // written by the workgroup
+    if (first == last) return;               // written by the team
     part = a.part_gate;
   }
   norm_f32x4 sum = {0, 0, 0, 0};
   if (col < d) {
-    for (int p = first + slice; p <= last; p += 16) {
-      const size_t at = (blockIdx.y >= 2 && p == first ? (size_t)n : 0) + p;
+#pragma unroll 8
+    for (int p = first + slice; p <= last; p += kReduceSlices) {
+      const size_t at = (blockIdx.y >= 2 && p == first ? (size_t)a.teams : 0) + p;
       sum += *reinterpret_cast<const norm_f32x4*>(part + at * d + col);
     }
   }
   lds[slice][lane] = sum;
   __syncthreads();
+  const int used = min(kReduceSlices, last - first + 1);
   if (slice || col >= d) return;
-  for (int s = 1; s < 16; ++s) sum += lds[s][lane];
-  float f[4];
-  for (int i = 0; i < 4; ++i) f[i] = sum[i];
-  auto weight = [&](const __bf16* w, float offset, int i) { return offset + (w ? (float)w[col + i] : 1.f); };
-  auto put = [&](float* out, auto factor) {
-    norm_f32x4 v;
-    for (int i = 0; i < 4; ++i) v[i] = f[i] * factor(i);
-    *reinterpret_cast<norm_f32x4*>(out + col) = v;
-  };
-  auto n_weight = [&](int i) { return a.scale * weight(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, i); };
-  if (blockIdx.y == 0) put(a.dw_pre, [](int) { return 1.f; });
-  else if (blockIdx.y >= 2) put(a.dgate + (size_t)group * d, n_weight);
-  else {
-    if (a.dw_post) put(a.dw_post, [&](int i) { return kMany ? 1.f : a.scale * weight(a.gate, 0.f, i); });
-    if (!kMany && a.dgate) put(a.dgate, n_weight);
+  for (int s = 1; s < used; ++s) sum += lds[s][lane];
+  float t[4];
+  for (int i = 0; i < 4; ++i) t[i] = sum[i];
+  if (blockIdx.y == 1 && !kMany) {
+    finish_post<4>(a, col, t);
+    return;
   }
+  float* const to = blockIdx.y == 0 ? a.dw_pre : blockIdx.y == 1 ? a.dw_post : a.dgate + (size_t)group * d;
+  for (int i = 0; i < 4; ++i)
+    to[col + i] = blockIdx.y < 2 ? t[i] : a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col + i] : 1.f) : 1.f) * t[i];
 }
 
 }  // namespace mst

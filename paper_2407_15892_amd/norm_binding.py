@@ -139,10 +139,10 @@ def mst_norm_workspace_bytes(S: int, d: int, gate_rows: int = 0) -> int:
 
 
 def mst_norm_bwd_info(S: int, d: int) -> dict:
-    """Threads and rows of a workgroup of the backward calls, and their number."""
-    info = (ctypes.c_int64 * 3)()
+    """How a backward call goes over the rows: threads of a workgroup, teams in it, rows of a team, workgroups."""
+    info = (ctypes.c_int64 * 4)()
     _check(load_norm_library().mst_norm_bwd_info(S, d, info))
-    return dict(zip(("threads", "rows", "workgroups"), (int(x) for x in info)))
+    return dict(zip(("threads", "teams", "rows", "workgroups"), (int(x) for x in info)))
 
 
 def mst_ckpt_pack(X, codes, exps, stream=None) -> None:

@@ -104,7 +104,8 @@ def close(got, want, reach, ops, to="bf16"):
 
 
 def column_ops(S, d):
-    """Operations in a row of a sum over rows: the rows of a workgroup, then the workgroups (a sixteenth each, then 16)."""
+    """Operations in a row of a sum over rows: the rows of a team, the teams of a workgroup, then the workgroups (or, of a gate's
+    row, the teams): a 64th each, then 64."""
     import paper_2407_15892_amd as mst
     info = mst.mst_norm_bwd_info(S, d)
-    return info["rows"] + -(-info["workgroups"] // 16) + 16
+    return info["rows"] + info["teams"] + -(-info["workgroups"] * info["teams"] // 64) + 64

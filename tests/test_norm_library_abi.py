@@ -36,15 +36,16 @@ def test_workspace_and_rows_of_the_backward(mst):
     for d in (8, 64, 512, 520, 4096, 8192, 8200, 16384):
         for S in (1, 2, 3, 63, 64, 1000, 8192, 131072, (1 << 30) - 1):
             info = mst.mst_norm_bwd_info(S, d)
+            teams, all_teams = info["teams"], info["teams"] * info["workgroups"]
             assert info["threads"] % 64 == 0 and info["threads"] <= 1024
-            assert info["threads"] * 8 * (1 if d <= 8192 else 2) >= d
-            assert info["rows"] * (info["workgroups"] - 1) < S <= info["rows"] * info["workgroups"]
-            assert info["workgroups"] <= 256 * 16
+            assert info["threads"] // teams * 8 * (1 if d <= 8192 else 2) >= d
+            assert info["rows"] * (all_teams - teams) < S <= info["rows"] * all_teams
             one, many = mst.mst_norm_workspace_bytes(S, d), mst.mst_norm_workspace_bytes(S, d, 1)
-            part = info["workgroups"] * d * 4
-            assert one % 256 == 0 and many >= one and one <= 2 * part + 256 and many <= 4 * part + 256
-            if info["workgroups"] > 1:
-                assert one >= 2 * part and (S == 1 or many >= 4 * part)
+            sums = 2 * info["workgroups"] * d * 4 if info["workgroups"] > 1 else 0
+            assert one % 256 == 0 and sums <= one <= sums + 512
+            gates = 2 * all_teams * d * 4 if S > 1 else 0
+            assert sums + gates <= many <= sums + gates + 512
+            assert many <= 1 << 27                       # whatever the rows
             assert mst.mst_norm_workspace_bytes(S, d, S) == mst.mst_norm_workspace_bytes(S, d, S + 5) == one
             seen.add(info["workgroups"] == 1)
     assert seen == {True, False}
