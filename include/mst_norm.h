@@ -60,7 +60,8 @@
  *   - Where a backward call takes a tensor or its checkpoint, exactly one of the
  *     two is given (both of codes and exps, or neither).
  *   - Tensors are row-major without padding.  Requirements: 1 <= S < 2^30;
- *     8 <= d <= MST_NORM_MAX_D, d % 8 == 0; eps, scale and w_offset finite, eps >= 2^-126; gate_rows >= 1 with a gate (the gate then has
+ *     8 <= d <= MST_NORM_MAX_D, d % 8 == 0, S * d <= 2^36; eps, scale and w_offset finite,
+ *     eps >= 2^-126; gate_rows >= 1 with a gate (the gate then has
  *     ceil(S / gate_rows) rows), 0 without; all tensors 16-byte
  *     aligned but exps (any), workspace 256-byte aligned.
  *   - An output may be the very memory of an input of S * d entries of the same

@@ -16,7 +16,7 @@ constexpr int kNumCu = 256;
 mst_status check_launch() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
 
 mst_status check_shape(int64_t S, int64_t d) {
-  if (S < 1 || S >= (int64_t(1) << 30) || d < 8 || d % 8 != 0 || d > MST_NORM_MAX_D) return MST_ERR_BAD_SHAPE;
+  if (S < 1 || S >= (int64_t(1) << 30) || d < 8 || d % 8 != 0 || d > MST_NORM_MAX_D || S * d > (int64_t(1) << 36)) return MST_ERR_BAD_SHAPE;
   return MST_OK;
 }
 
@@ -110,7 +110,7 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p, st);
 }
 
-template <class T, bool kPre, bool kRes, bool kMany>
+template <class T, bool kPre, bool kRes, bool kMany, bool kCkptX, bool kCkptO>
 mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream_t st) {
   const BwdPlan p(a.S, a.d);
   a.rows = p.rows;
@@ -124,9 +124,9 @@ mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream
   const dim3 grid((unsigned)p.groups), block(p.row.threads());
   const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // at most 16 KB
   if (p.row.chunks == 1)
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 1>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, kCkptX, kCkptO, 1>), grid, block, lds, st, a);
   else
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, 2>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, kCkptX, kCkptO, 2>), grid, block, lds, st, a);
   const int64_t items = !kMany || a.rows % a.gate_rows == 0 ? 0 : a.gate_rows >= a.rows ? gate_groups : p.teams - 1;
   if ((p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) || items) {
     hipLaunchKernelGGL(k_norm_reduce<kMany>, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + items)), dim3(kReduceThreads), 0, st, a, (int)p.groups);
@@ -134,13 +134,22 @@ mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream
   return check_launch();
 }
 
+template <class T, bool kPre, bool kRes>
+mst_status dispatch_bwd(const NormBwd& a, int64_t gate_groups, void* workspace, hipStream_t st) {
+  constexpr bool kX = kPre, kO = kRes;             // where there can be a checkpoint
+  auto many = [&](auto m) {
+    constexpr bool kMany = kRes && decltype(m)::value;
+    if (a.codes_x && a.codes_o) return launch_bwd<T, kPre, kRes, kMany, kX, kO>(a, gate_groups, workspace, st);
+    if (a.codes_x) return launch_bwd<T, kPre, kRes, kMany, kX, false>(a, gate_groups, workspace, st);
+    if (a.codes_o) return launch_bwd<T, kPre, kRes, kMany, false, kO>(a, gate_groups, workspace, st);
+    return launch_bwd<T, kPre, kRes, kMany, false, false>(a, gate_groups, workspace, st);
+  };
+  return gate_groups > 1 ? many(std::true_type()) : many(std::false_type());
+}
 template <bool kPre, bool kRes>
 mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_groups, void* workspace, hipStream_t st) {
-  if (kRes && gate_groups > 1)
-    return type == MST_TYPE_FP32 ? launch_bwd<float, kPre, kRes, kRes>(a, gate_groups, workspace, st)
-                                 : launch_bwd<__bf16, kPre, kRes, kRes>(a, gate_groups, workspace, st);
-  return type == MST_TYPE_FP32 ? launch_bwd<float, kPre, kRes, false>(a, gate_groups, workspace, st)
-                               : launch_bwd<__bf16, kPre, kRes, false>(a, gate_groups, workspace, st);
+  return type == MST_TYPE_FP32 ? dispatch_bwd<float, kPre, kRes>(a, gate_groups, workspace, st)
+                               : dispatch_bwd<__bf16, kPre, kRes>(a, gate_groups, workspace, st);
 }
 
 // slots of a checkpoint kernel's launch stay below 2^30: rows of one launch

@@ -239,12 +239,16 @@ template <int kN> struct RowSums {
       for (int i = 0; i < kN; ++i) at[wave][i] = v[i];
     }
     lds_barrier();
+    const int from = threadIdx.x % (team.waves > 8 ? 16 : 8);      // each 8 or 16 lanes read the waves' sums and add them up
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = 0.f;
-    for (int w = first; w < first + team.waves; ++w) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] += at[w][i];
+    for (int i = 0; i < kN; ++i) {
+      const float x = at[(first + from) % kNormMaxWaves][i];
+      v[i] = from < team.waves ? x : 0.f;
     }
+    add_dpp<kQuadSwap1>(v);
+    add_dpp<kQuadSwap2>(v);
+    add_dpp<kHalfMirror>(v);
+    if (team.waves > 8) add_dpp<kMirror>(v);
   }
 };
 
@@ -421,39 +425,47 @@ struct NormBwd {
   Team team;
 };
 
-// A row's eight entries as loaded: the tensor's, or codes and exponent of its checkpoint.
-template <class T> struct Source {
-  unsigned u[sizeof(T) * 2];
-  __device__ void load(const void* X, const int8_t* codes, const uint8_t* exps, size_t at, size_t block) {
-    if (codes) {
-      const norm_u32x2 c = *reinterpret_cast<const norm_u32x2*>(codes + at);
-      u[0] = c[0]; u[1] = c[1];
-      u[2] = exps[block];
-    } else {
-      const norm_u32x4* const p = reinterpret_cast<const norm_u32x4*>(static_cast<const T*>(X) + at);
-#pragma unroll
-      for (unsigned i = 0; i < sizeof(T) / 2; ++i) {
-        const norm_u32x4 w = p[i];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) u[4 * i + k] = w[k];
-      }
-    }
+// A workgroup's rows of a tensor, as a buffer: what lies behind them, and a tensor that is not there, reads as zeros and
+// takes no stores.  Without branches around loads and stores the compiler knows how many are under way, and waits for the ones it needs.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, size_t from, int rows, uint32_t row_bytes) {
+  const char* const at = static_cast<const char*>(p) + from * row_bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, p ? (int)(rows * row_bytes) : 0, 0x00020000);
+}
+// Offset in entries of a lane that has no columns: behind a workgroup's rows (less than 2^29 entries) in bytes of 1, 2 or 4.
+constexpr uint32_t kNoColumn = 1u << 29;
+
+template <class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
+  const uint32_t byte = at * (uint32_t)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
+  } else {
+    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
+    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, 0));
   }
-  __device__ void get(bool checkpoint, float (&v)[8]) const {
-    if (checkpoint) {
-      EightCodes c;
-      c.c = {u[0], u[1]};
-      c.e = u[2];
-      c.get(v);
-    } else if (sizeof(T) == 2) {
-      Eight<__bf16> e;
-      e.u = {u[0], u[1], u[2], u[3]};
-      e.get(v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i % (sizeof(T) * 2)]);
-    }
+}
+template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
+  const uint32_t byte = at * (uint32_t)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, 0);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, 0);
   }
+}
+
+// A row's eight entries: the tensor's, or those of its checkpoint.
+template <class T, bool kCheckpoint> struct Source {
+  Eight<T> e;
+  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight(e, rows, at); }
+  __device__ void get(float (&v)[8]) const { e.get(v); }
+};
+template <class T> struct Source<T, true> {
+  EightCodes e;
+  __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
+    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0));
+    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, 0);
+  }
+  __device__ void get(float (&v)[8]) const { e.get(v); }
 };
 
 // dw_post and dgate of four or eight columns from t = sum of dY * N / w_post over the rows of a call without a gate, or
@@ -470,7 +482,7 @@ template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, 
 // for their columns.  kMany: more than one row of gates.
 // With x the row of X, q its rstd, a = dH * ~w: the gradient is dres + q a - x q^3 sum(a x) / d; likewise for O with
 // b = dY * f, f = scale * gate * ~w_post.  One sum over the row waits for another where both norms are there.
-template <class T, bool kPre, bool kRes, bool kMany, int kNc>
+template <class T, bool kPre, bool kRes, bool kMany, bool kCkptX, bool kCkptO, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
   __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
@@ -479,9 +491,9 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   RowSums<1> second_sum(lds2, a.team);
   const int d = a.d, blocks = (d + 31) / 32, threads = a.team.threads(), lane = threadIdx.x % threads;
   const int teams = blockDim.x / threads, in_block = threadIdx.x / threads, team = blockIdx.x * teams + in_block;
-  const int64_t first_row = (int64_t)team * a.rows;
-  const int begin = (int)min(first_row, (int64_t)a.S), end = (int)min(first_row + a.rows, (int64_t)a.S);
-  const bool need_o = kRes && (a.O || a.codes_o);
+  const int64_t first_row = (int64_t)blockIdx.x * teams * a.rows;
+  const int rows = (int)min((int64_t)teams * a.rows, a.S - first_row);      // of the workgroup
+  const int begin = (int)min((int64_t)team * a.rows, (int64_t)a.S), end = (int)min((int64_t)begin + a.rows, (int64_t)a.S);   // of the team
   float acc_pre[kNc][8] = {}, acc_group[kNc][8] = {}, acc_post[kNc][8] = {};
   float w[kNc][8], f[kNc][8];
   int group = 0, group_end = 0;                  // the gate's row that f and acc_group belong to, and the row behind its last
@@ -495,45 +507,46 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
   };
+  const __amdgpu_buffer_rsrc_t dh_rows = rows_of(a.dH, first_row, rows, 2 * d), dx_rows = rows_of(a.dX, first_row, rows, (int)sizeof(T) * d);
+  const __amdgpu_buffer_rsrc_t dy_rows = rows_of(kPre ? a.dres : a.dY, first_row, rows, (int)sizeof(T) * d);
+  const __amdgpu_buffer_rsrc_t x_rows = kCkptX ? rows_of(a.codes_x, first_row, rows, d) : rows_of(a.X, first_row, rows, (int)sizeof(T) * d);
+  const __amdgpu_buffer_rsrc_t o_rows = kCkptO ? rows_of(a.codes_o, first_row, rows, d) : rows_of(a.O, first_row, rows, 2 * d);
+  const __amdgpu_buffer_rsrc_t x_exps = rows_of(a.exps_x, first_row, rows, blocks), o_exps = rows_of(a.exps_o, first_row, rows, blocks);
+  const __amdgpu_buffer_rsrc_t do_rows = rows_of(a.dO, first_row, rows, 2 * d);
+  uint32_t at[kNc], block[kNc];                  // of the row that is loaded next
   Eight<__bf16> dh_next[kNc];
-  Source<T> x_next[kNc];
+  Source<T, kCkptX> x_next[kNc];
   Eight<T> dy_next[kNc];
-  Source<__bf16> o_next[kNc];
-  auto load = [&](int row) {
+  Source<__bf16, kCkptO> o_next[kNc];
+  auto load = [&]() {
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = column(k);
-      if (row >= end || col >= d) continue;
-      const size_t at = (size_t)row * d + col, block = (size_t)row * blocks + col / 32;
       if (kPre) {
-        dh_next[k].load(a.dH + at);
-        x_next[k].load(a.X, a.codes_x, a.exps_x, at, block);
-        if (a.dres) dy_next[k].load(static_cast<const T*>(a.dres) + at);
-      } else {
-        dy_next[k].load(static_cast<const T*>(a.dY) + at);
+        load_eight(dh_next[k], dh_rows, at[k]);
+        x_next[k].load(x_rows, x_exps, at[k], block[k]);
       }
-      if (need_o) o_next[k].load(a.O, a.codes_o, a.exps_o, at, block);
+      load_eight(dy_next[k], dy_rows, at[k]);
+      if (kRes) o_next[k].load(o_rows, o_exps, at[k], block[k]);
+      at[k] += d;
+      block[k] += blocks;
     }
   };
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    if (kPre) weights(a.w_pre, a.offset, column(k), column(k) < d, w[k]);
+    const bool on = column(k) < d;
+    at[k] = on ? in_block * a.rows * d + column(k) : kNoColumn;
+    block[k] = on ? in_block * a.rows * blocks + column(k) / 32 : kNoColumn;
+    if (kPre) weights(a.w_pre, a.offset, column(k), on, w[k]);
     if (kRes && !kMany) load_f(k);
-#pragma unroll
-    for (int i = 0; i < 4 * (int)sizeof(T) / 2; ++i) x_next[k].u[i] = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o_next[k].u[i] = 0;
   }
-  load(begin);
-  for (int i_row = 0; i_row < a.rows; ++i_row) {         // as often in every team, for the barriers
+  load();
+  for (int i_row = 0; i_row < a.rows; ++i_row) {         // as often in every team, for the barriers; zeros behind the last row
     const int row = begin + i_row;
-    const bool on = row < end;
-    const float live = on ? 1.f : 0.f;                   // what is left in the registers behind the last row is not summed up
     float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
     float sums[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; ++i) sums[i] = 0.f;
-    if (kMany && on && row == group_end) {
+    if (kMany && row < end && row == group_end) {
       ++group;
       group_end = (int)min((int64_t)(group + 1) * a.gate_rows, (int64_t)a.S);
 #pragma unroll
@@ -543,7 +556,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     for (int k = 0; k < kNc; ++k) {
       dy_next[k].get(dy[k]);
       if (kPre) {
-        x_next[k].get(a.codes_x != nullptr, x[k]);
+        x_next[k].get(x[k]);
         dh_next[k].get(dh[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -552,7 +565,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
       }
       if (kRes) {
-        o_next[k].get(a.codes_o != nullptr, o[k]);
+        o_next[k].get(o[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPre ? 2 : 0] = fmaf(o[k][i], o[k][i], sums[kPre ? 2 : 0]);
@@ -560,27 +573,24 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
       }
     }
-    load(row + 1);
+    load();
     if (kPre || a.normalize) first_sums(sums);
     float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
     if (kPre) {
       const float q = rsqrtf(fmaf(sums[0], a.inv_d, a.eps)), c = -q * q * q * sums[1] * a.inv_d;
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
-        const int col = column(k);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float u = dh[k][i] * (q * live);
+          const float u = dh[k][i] * q;
           acc_pre[k][i] = fmaf(u, x[k][i], acc_pre[k][i]);
           dy[k][i] = fmaf(u, w[k][i], dy[k][i]);
           dy[k][i] = fmaf(x[k][i], c, dy[k][i]);
           if (kRes) post[0] = fmaf(dy[k][i] * f[k][i], o[k][i], post[0]);
         }
-        if (on && col < d) {
-          Eight<T> e;
-          e.set(dy[k]);
-          e.store(static_cast<T*>(a.dX) + (size_t)row * d + col);
-        }
+        Eight<T> e;
+        e.set(dy[k]);
+        store_eight(e, dx_rows, at[k] - 2 * d);
       }
     }
     if (!kRes) continue;
@@ -593,15 +603,14 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       float out[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float u = dy[k][i] * (q * live);
+        const float u = dy[k][i] * q;
         out[i] = fmaf(o[k][i], c, u * f[k][i]);
         acc_group[k][i] = fmaf(u, o[k][i], acc_group[k][i]);
       }
-      if (!on || col >= d) continue;
       Eight<__bf16> e;
       e.set(out);
-      e.store(a.dO + (size_t)row * d + col);
-      if (kMany && (row + 1 == end || row + 1 == group_end)) {        // the team's last row of this row of the gate
+      store_eight(e, do_rows, at[k] - 2 * d);
+      if (kMany && col < d && row < end && (row + 1 == end || row + 1 == group_end)) {        // the team's last row of this row of the gate
         const bool whole = (int64_t)group * a.gate_rows >= begin && group_end <= end;
         const bool began_before = (int64_t)group * a.gate_rows < begin;
         float g[8], wo[8];
@@ -656,13 +665,13 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 
 // Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre, 1 dw_post (and the gradient of a single row of gates); from
 // 2 on the teams' sums for rows of the gate that lie in more than one team: each row of the gate in turn where it has at
-// least as many rows as a team, else those across the border behind each team.  A workgroup takes 64 columns: 16 lanes of four, and
-// groups of 16 lanes that share out the sums, added up in order.
-constexpr int kReduceThreads = 1024, kReduceCols = 64, kReduceSlices = kReduceThreads / 16;
+// least as many rows as a team, else those across the border behind each team.  A workgroup takes 32 columns (a cache line of each
+// sum): 8 lanes of four, and 128 groups of 8 lanes that share out the sums.  Added up in one order.
+constexpr int kReduceThreads = 1024, kReduceCols = 32, kReduceSlices = kReduceThreads / 8;
 template <bool kMany>
 __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n) {
-  __shared__ norm_f32x4 lds[kReduceSlices][16];
-  const int lane = threadIdx.x % 16, slice = threadIdx.x / 16, d = a.d;
+  __shared__ norm_f32x4 lds[kReduceThreads / 64][8];
+  const int lane = threadIdx.x % 8, slice = threadIdx.x / 8, d = a.d;
   const int col = blockIdx.x * kReduceCols + lane * 4;
   const float* part = blockIdx.y == 0 ? a.part_pre : a.part_post;
   int first = 0, last = n - 1, group = 0;
@@ -678,17 +687,23 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a,
   }
   norm_f32x4 sum = {0, 0, 0, 0};
   if (col < d) {
-#pragma unroll 8
+#pragma unroll 4
     for (int p = first + slice; p <= last; p += kReduceSlices) {
       const size_t at = (blockIdx.y >= 2 && p == first ? (size_t)a.teams : 0) + p;
       sum += *reinterpret_cast<const norm_f32x4*>(part + at * d + col);
     }
   }
-  lds[slice][lane] = sum;
+#pragma unroll
+  for (int x = 8; x < 64; x *= 2) {
+    norm_f32x4 o;
+    for (int i = 0; i < 4; ++i) o[i] = __shfl_xor(sum[i], x);
+    sum += o;
+  }
+  if (threadIdx.x % 64 < 8) lds[threadIdx.x / 64][lane] = sum;
   __syncthreads();
-  const int used = min(kReduceSlices, last - first + 1);
   if (slice || col >= d) return;
-  for (int s = 1; s < used; ++s) sum += lds[s][lane];
+#pragma unroll
+  for (int s = 1; s < kReduceThreads / 64; ++s) sum += lds[s][lane];
   float t[4];
   for (int i = 0; i < 4; ++i) t[i] = sum[i];
   if (blockIdx.y == 1 && !kMany) {

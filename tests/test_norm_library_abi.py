@@ -35,6 +35,8 @@ def test_workspace_and_rows_of_the_backward(mst):
     seen = set()
     for d in (8, 64, 512, 520, 4096, 8192, 8200, 16384):
         for S in (1, 2, 3, 63, 64, 1000, 8192, 131072, (1 << 30) - 1):
+            if S * d > 1 << 36:
+                continue
             info = mst.mst_norm_bwd_info(S, d)
             teams, all_teams = info["teams"], info["teams"] * info["workgroups"]
             assert info["threads"] % 64 == 0 and info["threads"] <= 1024
@@ -45,11 +47,12 @@ def test_workspace_and_rows_of_the_backward(mst):
             assert one % 256 == 0 and sums <= one <= sums + 512
             gates = 2 * all_teams * d * 4 if S > 1 else 0
             assert sums + gates <= many <= sums + gates + 512
+            assert teams * info["rows"] * d < 1 << 29           # offsets of a workgroup's rows
             assert many <= 1 << 27                       # whatever the rows
             assert mst.mst_norm_workspace_bytes(S, d, S) == mst.mst_norm_workspace_bytes(S, d, S + 5) == one
             seen.add(info["workgroups"] == 1)
     assert seen == {True, False}
-    for S, d in ((0, 8), (-1, 8), (1, 0), (1, 12), (1, 16392), (1 << 30, 8)):
+    for S, d in ((0, 8), (-1, 8), (1, 0), (1, 12), (1, 16392), (1 << 30, 8), ((1 << 23) + 1, 8192)):
         with pytest.raises(mst.MstError) as e:
             mst.mst_norm_workspace_bytes(S, d)
         assert e.value.status == SHAPE
