@@ -74,22 +74,32 @@ struct RowPlan {
 
 constexpr int kFwdRows[2] = {2, 1};      // rows of a team with one and with two chunks
 
-// Rows of a team of the backward calls.
+// How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate.
 struct BwdPlan {
   RowPlan row;
-  int rows, teams;                       // of a team; in all
-  int64_t groups;                        // workgroups
-  BwdPlan(int64_t S, int64_t d) : row(d) {
-    const int64_t most = kNumCu * std::max(1, 1024 / row.threads()) * row.teams;
-    rows = (int)((S + most - 1) / most);
-    const int64_t needed = (S + rows - 1) / rows;
-    groups = (needed + row.teams - 1) / row.teams;
-    teams = (int)(groups * row.teams);
+  bool whole;                            // teams take whole rows of the gate
+  int64_t gates, share, groups;          // rows of the gate (1 without); workgroups of each; workgroups
+  int rows;                              // that a team takes in turn
+  BwdPlan(int64_t S, int64_t d, int64_t gate_rows) : row(d) {
+    const int64_t L = gate_rows ? std::min(gate_rows, S) : S;
+    const int64_t most = kNumCu * std::max(1, 1024 / row.threads());      // workgroups that are resident together
+    gates = (S + L - 1) / L;
+    whole = gates > 1 && (2 * gates >= most * row.teams || L < row.teams) && L * row.teams * d < (int64_t(1) << 29);
+    if (whole) {
+      groups = std::min(most, (gates + row.teams - 1) / row.teams);
+      share = 0;
+      rows = (int)((gates + groups * row.teams - 1) / (groups * row.teams) * L);
+      return;
+    }
+    const int64_t wanted = (most + gates - 1) / gates;
+    rows = (int)((L + wanted * row.teams - 1) / (wanted * row.teams));
+    share = (L + (int64_t)rows * row.teams - 1) / ((int64_t)rows * row.teams);
+    groups = gates * share;
   }
 };
 
-size_t workspace_bytes(const BwdPlan& p, int64_t d, int64_t gate_groups) {      // dw_pre, dw_post by workgroup, two of the gate's rows by team
-  return mst_host::align_up((size_t)d * 4 * ((p.groups > 1 ? 2 * p.groups : 0) + (gate_groups > 1 ? 2 * p.teams : 0)) + 256, 256);
+size_t workspace_bytes(const BwdPlan& p, int64_t d) {      // dw_pre and dw_post by workgroup
+  return mst_host::align_up(p.groups > 1 ? 2 * (size_t)p.groups * d * 4 : 1, 256);
 }
 
 template <class T, bool kRes, bool kPre, bool kRebuild, int kNc>
@@ -110,46 +120,47 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p, st);
 }
 
-template <class T, bool kPre, bool kRes, bool kMany, bool kCkptX, bool kCkptO>
-mst_status launch_bwd(NormBwd a, int64_t gate_groups, void* workspace, hipStream_t st) {
-  const BwdPlan p(a.S, a.d);
+template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO>
+mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t st) {
   a.rows = p.rows;
-  a.teams = p.teams;
+  a.share = (int)p.share;
   a.team = p.row.team;
-  float* const ws = static_cast<float*>(workspace);
-  const size_t part = p.groups > 1 ? (size_t)p.groups * a.d : 0;
-  a.part_pre = ws;
-  a.part_post = ws + part;
-  a.part_gate = ws + 2 * part;
+  a.part_pre = static_cast<float*>(workspace);
+  a.part_post = a.part_pre + (size_t)p.groups * a.d;
   const dim3 grid((unsigned)p.groups), block(p.row.threads());
   const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // at most 16 KB
   if (p.row.chunks == 1)
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, kCkptX, kCkptO, 1>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, 1>), grid, block, lds, st, a);
   else
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kMany, kCkptX, kCkptO, 2>), grid, block, lds, st, a);
-  const int64_t items = !kMany || a.rows % a.gate_rows == 0 ? 0 : a.gate_rows >= a.rows ? gate_groups : p.teams - 1;
-  if ((p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) || items) {
-    hipLaunchKernelGGL(k_norm_reduce<kMany>, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + items)), dim3(kReduceThreads), 0, st, a, (int)p.groups);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, 2>), grid, block, lds, st, a);
+  if (p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) {
+    int slices = 1;                                       // of the sums of a row of the gate
+    while (slices < kReduceSlices && slices < p.share) slices *= 2;
+    const int64_t per_block = kReduceSlices / slices, gates = a.dgate && !kWhole && p.gates > 1 ? (p.gates + per_block - 1) / per_block : 0;
+    hipLaunchKernelGGL(k_norm_reduce, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + gates)), dim3(kReduceThreads), 0, st, a,
+                       (int)p.groups, (int)kWhole, slices);
   }
   return check_launch();
 }
 
 template <class T, bool kPre, bool kRes>
-mst_status dispatch_bwd(const NormBwd& a, int64_t gate_groups, void* workspace, hipStream_t st) {
+mst_status dispatch_bwd(NormBwd a, int64_t gate_rows, void* workspace, hipStream_t st) {
   constexpr bool kX = kPre, kO = kRes;             // where there can be a checkpoint
-  auto many = [&](auto m) {
-    constexpr bool kMany = kRes && decltype(m)::value;
-    if (a.codes_x && a.codes_o) return launch_bwd<T, kPre, kRes, kMany, kX, kO>(a, gate_groups, workspace, st);
-    if (a.codes_x) return launch_bwd<T, kPre, kRes, kMany, kX, false>(a, gate_groups, workspace, st);
-    if (a.codes_o) return launch_bwd<T, kPre, kRes, kMany, false, kO>(a, gate_groups, workspace, st);
-    return launch_bwd<T, kPre, kRes, kMany, false, false>(a, gate_groups, workspace, st);
+  const BwdPlan p(a.S, a.d, gate_rows);
+  a.gate_rows = (int)(gate_rows ? std::min<int64_t>(gate_rows, a.S) : a.S);
+  auto go = [&](auto w) {
+    constexpr bool kWhole = kRes && decltype(w)::value;
+    if (a.codes_x && a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, kX, kO>(a, p, workspace, st);
+    if (a.codes_x) return launch_bwd<T, kPre, kRes, kWhole, kX, false>(a, p, workspace, st);
+    if (a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, false, kO>(a, p, workspace, st);
+    return launch_bwd<T, kPre, kRes, kWhole, false, false>(a, p, workspace, st);
   };
-  return gate_groups > 1 ? many(std::true_type()) : many(std::false_type());
+  return p.whole ? go(std::true_type()) : go(std::false_type());
 }
 template <bool kPre, bool kRes>
-mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_groups, void* workspace, hipStream_t st) {
-  return type == MST_TYPE_FP32 ? dispatch_bwd<float, kPre, kRes>(a, gate_groups, workspace, st)
-                               : dispatch_bwd<__bf16, kPre, kRes>(a, gate_groups, workspace, st);
+mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_rows, void* workspace, hipStream_t st) {
+  return type == MST_TYPE_FP32 ? dispatch_bwd<float, kPre, kRes>(a, gate_rows, workspace, st)
+                               : dispatch_bwd<__bf16, kPre, kRes>(a, gate_rows, workspace, st);
 }
 
 // slots of a checkpoint kernel's launch stay below 2^30: rows of one launch
@@ -196,19 +207,21 @@ mst_status mst_norm_workspace_bytes(int64_t S, int64_t d, int64_t gate_rows, siz
   if (s != MST_OK) return s;
   if (gate_rows < 0) return MST_ERR_BAD_ARGUMENT;
   if (!bytes) return MST_ERR_NULL_POINTER;
-  *bytes = workspace_bytes(BwdPlan(S, d), d, gate_rows ? (S + std::min(gate_rows, S) - 1) / std::min(gate_rows, S) : 0);
+  *bytes = workspace_bytes(BwdPlan(S, d, gate_rows), d);
   return MST_OK;
 }
 
-mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t* info) {
+mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t gate_rows, int64_t* info) {
   mst_status s = check_shape(S, d);
   if (s != MST_OK) return s;
+  if (gate_rows < 0) return MST_ERR_BAD_ARGUMENT;
   if (!info) return MST_ERR_NULL_POINTER;
-  const BwdPlan p(S, d);
+  const BwdPlan p(S, d, gate_rows);
   info[0] = p.row.threads();
   info[1] = p.row.teams;
   info[2] = p.rows;
   info[3] = p.groups;
+  info[4] = p.whole;
   return MST_OK;
 }
 
@@ -292,7 +305,7 @@ mst_status mst_prenorm_bwd(const void* dH, const void* X, const int8_t* codes, c
   if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps) || (X && codes) || (dw_pre && !w_pre))
     return MST_ERR_BAD_ARGUMENT;
   if (w_pre && !dw_pre) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d), d, 0);
+  const size_t need = workspace_bytes(BwdPlan(S, d, 0), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   Operands ops;
   ops.add(dH, S * d, 2, false, true);
@@ -354,7 +367,7 @@ mst_status mst_residual_bwd(const void* dY, int32_t stream_type, const void* O, 
       (dw_post && !w_post) || (dgate && !gate))
     return MST_ERR_BAD_ARGUMENT;
   if ((w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes)) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d), d, gate_groups);
+  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   if (!normalize && !gate) O = nullptr, codes = nullptr, exps = nullptr;
   Operands ops;
@@ -374,8 +387,7 @@ mst_status mst_residual_bwd(const void* dY, int32_t stream_type, const void* O, 
   a.dO = static_cast<__bf16*>(dO); a.dw_post = dw_post; a.dgate = dgate;
   a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
   a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
-  a.gate_rows = (int)std::min(gate_rows, S);
-  return dispatch_bwd<false, true>(a, stream_type, gate_groups, workspace, as_stream(stream));
+  return dispatch_bwd<false, true>(a, stream_type, gate_rows, workspace, as_stream(stream));
 }
 
 mst_status mst_residual_prenorm_fwd(const void* O, const void* X, int32_t stream_type, int32_t normalize, const void* w_post,
@@ -430,7 +442,7 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
       (O && codes_o) || (Y && codes_y) || (w_post && !normalize) || (dw_post && !w_post) || (dgate && !gate) || (dw_pre && !w_pre))
     return MST_ERR_BAD_ARGUMENT;
   if ((w_pre && !dw_pre) || (w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes_o)) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d), d, gate_groups);
+  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   if (!normalize && !gate) O = nullptr, codes_o = nullptr, exps_o = nullptr;
   Operands ops;
@@ -459,8 +471,7 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
   a.dX = dY; a.dO = static_cast<__bf16*>(dO); a.dw_pre = dw_pre; a.dw_post = dw_post; a.dgate = dgate;
   a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
   a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
-  a.gate_rows = (int)std::min(gate_rows, S);
-  return dispatch_bwd<true, true>(a, stream_type, gate_groups, workspace, as_stream(stream));
+  return dispatch_bwd<true, true>(a, stream_type, gate_rows, workspace, as_stream(stream));
 }
 
 }  // extern "C"

@@ -418,20 +418,21 @@ struct NormBwd {
   __bf16* dO;
   float *dw_pre, *dw_post, *dgate; // NULL: not wanted
   float *part_pre, *part_post;     // [workgroups][d] each
-  float* part_gate;                // [2][teams][d]: of the gate's row that began before the team's rows; of the one that goes on behind them
   float offset, eps, scale, inv_d;
-  int S, d, normalize, gate_rows;
-  int rows, teams;                 // of a team; in all
+  int S, d, normalize;
+  int gate_rows;                   // without a gate S
+  int share;                       // workgroups that share a row of the gate (not kWhole)
+  int rows;                        // that a team takes in turn
   Team team;
 };
 
-// A workgroup's rows of a tensor, as a buffer: what lies behind them, and a tensor that is not there, reads as zeros and
-// takes no stores.  Without branches around loads and stores the compiler knows how many are under way, and waits for the ones it needs.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, size_t from, int rows, uint32_t row_bytes) {
+// Some rows of a tensor as a buffer: what lies behind them, and a tensor that is not there, reads as zeros and takes no
+// stores.  Without branches around loads and stores the compiler knows how many are under way, and waits for the ones it needs.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t from, int rows, int row_bytes) {
   const char* const at = static_cast<const char*>(p) + from * row_bytes;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, p ? (int)(rows * row_bytes) : 0, 0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, p ? rows * row_bytes : 0, 0x00020000);
 }
-// Offset in entries of a lane that has no columns: behind a workgroup's rows (less than 2^29 entries) in bytes of 1, 2 or 4.
+// Offset in entries of a lane that has no columns: behind those rows (less than 2^29 entries) in bytes of 1, 2 or 4.
 constexpr uint32_t kNoColumn = 1u << 29;
 
 template <class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
@@ -468,21 +469,31 @@ template <class T> struct Source<T, true> {
   __device__ void get(float (&v)[8]) const { e.get(v); }
 };
 
-// dw_post and dgate of four or eight columns from t = sum of dY * N / w_post over the rows of a call without a gate, or
-// whose rows share one gate.
+// dw_post and dgate of kN columns from t = sum of dY * N / w_post over the rows of a row of the gate (dw_post: if it is the
+// only one, or there is no gate).
+__device__ __forceinline__ float post_weight(const NormBwd& a, int col) {
+  return a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col] : 1.f) : 1.f);
+}
+__device__ __forceinline__ float gate_factor(const NormBwd& a, int group, int col) {
+  return a.scale * (a.gate ? (float)a.gate[(size_t)group * a.d + col] : 1.f);
+}
 template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, int col, const float* t) {
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    if (a.dw_post) a.dw_post[col + i] = a.scale * (a.gate ? (float)a.gate[col + i] : 1.f) * t[i];
-    if (a.dgate) a.dgate[col + i] = a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col + i] : 1.f) : 1.f) * t[i];
+    if (a.dw_post) a.dw_post[col + i] = gate_factor(a, 0, col + i) * t[i];
+    if (a.dgate) a.dgate[col + i] = post_weight(a, col + i) * t[i];
   }
 }
 
 // A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
-// for their columns.  kMany: more than one row of gates.
+// for their columns.
+//   kWhole = false  `share` workgroups have the rows of one row of the gate (all rows without a gate), adjacent rows in
+//                   adjacent teams: memory is passed through in a few streams.  Sums of dY * N, without the gate, to the workspace.
+//   kWhole = true   for many short rows of gates: a team has all rows of one, then those of another; it writes their gradient
+//                   and sums up dw_post.
 // With x the row of X, q its rstd, a = dH * ~w: the gradient is dres + q a - x q^3 sum(a x) / d; likewise for O with
 // b = dY * f, f = scale * gate * ~w_post.  One sum over the row waits for another where both norms are there.
-template <class T, bool kPre, bool kRes, bool kMany, bool kCkptX, bool kCkptO, int kNc>
+template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
   __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
@@ -490,67 +501,75 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   RowSums<kFirst> first_sums(lds1, a.team);
   RowSums<1> second_sum(lds2, a.team);
   const int d = a.d, blocks = (d + 31) / 32, threads = a.team.threads(), lane = threadIdx.x % threads;
-  const int teams = blockDim.x / threads, in_block = threadIdx.x / threads, team = blockIdx.x * teams + in_block;
-  const int64_t first_row = (int64_t)blockIdx.x * teams * a.rows;
-  const int rows = (int)min((int64_t)teams * a.rows, a.S - first_row);      // of the workgroup
-  const int begin = (int)min((int64_t)team * a.rows, (int64_t)a.S), end = (int)min((int64_t)begin + a.rows, (int64_t)a.S);   // of the team
+  const int teams = blockDim.x / threads, in_block = threadIdx.x / threads;
+  // The workgroup's rows at a time: those of its teams, `apart` rows from each other, the first at `row`.
+  const int apart = kWhole ? a.gate_rows : 1;
+  int group = kWhole ? (int)blockIdx.x * teams : (int)blockIdx.x / a.share;      // the gate's row (of the first team)
+  const int end = kWhole ? a.S : (int)min((int64_t)(group + 1) * a.gate_rows, (int64_t)a.S);
+  int64_t row = (int64_t)group * a.gate_rows + (kWhole ? 0 : (int64_t)(blockIdx.x % a.share) * teams), next = row;
+  int in_group = 0, next_in_group = 0;             // kWhole: rows of the gate's row that are done
+  auto advance = [&](int64_t& r, int& done) {
+    if (kWhole) {
+      ++r;
+      if (++done == a.gate_rows) {
+        done = 0;
+        r += ((int64_t)gridDim.x * teams - 1) * a.gate_rows;
+      }
+    } else {
+      r += (int64_t)a.share * teams;
+    }
+  };
   float acc_pre[kNc][8] = {}, acc_group[kNc][8] = {}, acc_post[kNc][8] = {};
   float w[kNc][8], f[kNc][8];
-  int group = 0, group_end = 0;                  // the gate's row that f and acc_group belong to, and the row behind its last
-  if (kMany) group = begin / a.gate_rows - 1, group_end = begin;
   auto column = [&](int k) { return (k * threads + lane) * 8; };
-  auto load_f = [&](int k) {
+  auto load_f = [&](int k, int g, bool on) {
     const int col = column(k);
-    weights(a.gate ? a.gate + (kMany ? (size_t)group * d : 0) : nullptr, 0.f, col, col < d, f[k]);
+    weights(a.gate ? a.gate + (size_t)g * d : nullptr, 0.f, col, on && col < d, f[k]);
     float wo[8];
     weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, col < d, wo);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
   };
-  const __amdgpu_buffer_rsrc_t dh_rows = rows_of(a.dH, first_row, rows, 2 * d), dx_rows = rows_of(a.dX, first_row, rows, (int)sizeof(T) * d);
-  const __amdgpu_buffer_rsrc_t dy_rows = rows_of(kPre ? a.dres : a.dY, first_row, rows, (int)sizeof(T) * d);
-  const __amdgpu_buffer_rsrc_t x_rows = kCkptX ? rows_of(a.codes_x, first_row, rows, d) : rows_of(a.X, first_row, rows, (int)sizeof(T) * d);
-  const __amdgpu_buffer_rsrc_t o_rows = kCkptO ? rows_of(a.codes_o, first_row, rows, d) : rows_of(a.O, first_row, rows, 2 * d);
-  const __amdgpu_buffer_rsrc_t x_exps = rows_of(a.exps_x, first_row, rows, blocks), o_exps = rows_of(a.exps_o, first_row, rows, blocks);
-  const __amdgpu_buffer_rsrc_t do_rows = rows_of(a.dO, first_row, rows, 2 * d);
-  uint32_t at[kNc], block[kNc];                  // of the row that is loaded next
+  uint32_t at[kNc], block[kNc];
   Eight<__bf16> dh_next[kNc];
   Source<T, kCkptX> x_next[kNc];
   Eight<T> dy_next[kNc];
   Source<__bf16, kCkptO> o_next[kNc];
+  auto rows_at = [&](int64_t r) { return (int)max((int64_t)0, min((int64_t)(teams - 1) * apart + 1, end - r)); };
   auto load = [&]() {
+    const int rows = rows_at(next);
+    const __amdgpu_buffer_rsrc_t dy_rows = rows_of(kPre ? a.dres : a.dY, next, rows, (int)sizeof(T) * d);
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
       if (kPre) {
-        load_eight(dh_next[k], dh_rows, at[k]);
-        x_next[k].load(x_rows, x_exps, at[k], block[k]);
+        load_eight(dh_next[k], rows_of(a.dH, next, rows, 2 * d), at[k]);
+        x_next[k].load(kCkptX ? rows_of(a.codes_x, next, rows, d) : rows_of(a.X, next, rows, (int)sizeof(T) * d),
+                       rows_of(a.exps_x, next, rows, blocks), at[k], block[k]);
       }
       load_eight(dy_next[k], dy_rows, at[k]);
-      if (kRes) o_next[k].load(o_rows, o_exps, at[k], block[k]);
-      at[k] += d;
-      block[k] += blocks;
+      if (kRes)
+        o_next[k].load(kCkptO ? rows_of(a.codes_o, next, rows, d) : rows_of(a.O, next, rows, 2 * d), rows_of(a.exps_o, next, rows, blocks),
+                       at[k], block[k]);
     }
+    advance(next, next_in_group);
   };
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
     const bool on = column(k) < d;
-    at[k] = on ? in_block * a.rows * d + column(k) : kNoColumn;
-    block[k] = on ? in_block * a.rows * blocks + column(k) / 32 : kNoColumn;
+    at[k] = on ? in_block * apart * d + column(k) : kNoColumn;
+    block[k] = on ? in_block * apart * blocks + column(k) / 32 : kNoColumn;
     if (kPre) weights(a.w_pre, a.offset, column(k), on, w[k]);
-    if (kRes && !kMany) load_f(k);
+    if (kRes && !kWhole) load_f(k, group, true);
   }
   load();
   for (int i_row = 0; i_row < a.rows; ++i_row) {         // as often in every team, for the barriers; zeros behind the last row
-    const int row = begin + i_row;
     float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
     float sums[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; ++i) sums[i] = 0.f;
-    if (kMany && row < end && row == group_end) {
-      ++group;
-      group_end = (int)min((int64_t)(group + 1) * a.gate_rows, (int64_t)a.S);
+    if (kWhole && in_group == 0) {
 #pragma unroll
-      for (int k = 0; k < kNc; ++k) load_f(k);
+      for (int k = 0; k < kNc; ++k) load_f(k, group + in_block, row + (int64_t)in_block * apart < end);
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
@@ -574,6 +593,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       }
     }
     load();
+    const int rows = rows_at(row);
     if (kPre || a.normalize) first_sums(sums);
     float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
     if (kPre) {
@@ -590,44 +610,47 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
         Eight<T> e;
         e.set(dy[k]);
-        store_eight(e, dx_rows, at[k] - 2 * d);
+        store_eight(e, rows_of(a.dX, row, rows, (int)sizeof(T) * d), at[k]);
       }
     }
-    if (!kRes) continue;
-    if (kPre && a.normalize) second_sum(post);
-    const float q = a.normalize ? rsqrtf(fmaf(sums[kPre ? 2 : 0], a.inv_d, a.eps)) : 1.f;
-    const float c = a.normalize ? -q * q * q * post[0] * a.inv_d : 0.f;
+    if (kRes) {
+      if (kPre && a.normalize) second_sum(post);
+      const float q = a.normalize ? rsqrtf(fmaf(sums[kPre ? 2 : 0], a.inv_d, a.eps)) : 1.f;
+      const float c = a.normalize ? -q * q * q * post[0] * a.inv_d : 0.f;
 #pragma unroll
-    for (int k = 0; k < kNc; ++k) {
-      const int col = column(k);
-      float out[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float u = dy[k][i] * q;
-        out[i] = fmaf(o[k][i], c, u * f[k][i]);
-        acc_group[k][i] = fmaf(u, o[k][i], acc_group[k][i]);
-      }
-      Eight<__bf16> e;
-      e.set(out);
-      store_eight(e, do_rows, at[k] - 2 * d);
-      if (kMany && col < d && row < end && (row + 1 == end || row + 1 == group_end)) {        // the team's last row of this row of the gate
-        const bool whole = (int64_t)group * a.gate_rows >= begin && group_end <= end;
-        const bool began_before = (int64_t)group * a.gate_rows < begin;
-        float g[8], wo[8];
-        weights(a.gate + (size_t)group * d, 0.f, col, true, g);
-        weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, true, wo);
-        Eight<float> sum;
+      for (int k = 0; k < kNc; ++k) {
+        float out[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          acc_post[k][i] = fmaf(g[i] * a.scale, acc_group[k][i], acc_post[k][i]);
-          if (whole) acc_group[k][i] *= a.scale * wo[i];
+          const float u = dy[k][i] * q;
+          out[i] = fmaf(o[k][i], c, u * f[k][i]);
+          acc_group[k][i] = fmaf(u, o[k][i], acc_group[k][i]);
         }
-        sum.set(acc_group[k]);
-        sum.store((whole ? a.dgate + (size_t)group * d : a.part_gate + ((size_t)(began_before ? 0 : a.teams) + team) * d) + col);
+        Eight<__bf16> e;
+        e.set(out);
+        store_eight(e, rows_of(a.dO, row, rows, 2 * d), at[k]);
+      }
+      const int64_t mine = row + (int64_t)in_block * apart;
+      if (kWhole && (in_group == a.gate_rows - 1 || mine == end - 1) && mine < end) {      // the last row of its row of the gate
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc_group[k][i] = 0.f;
+        for (int k = 0; k < kNc; ++k) {
+          const int col = column(k);
+          if (col >= d) continue;
+          Eight<float> e;
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            acc_post[k][i] = fmaf(gate_factor(a, group + in_block, col + i), acc_group[k][i], acc_post[k][i]);
+            v[i] = post_weight(a, col + i) * acc_group[k][i];
+            acc_group[k][i] = 0.f;
+          }
+          e.set(v);
+          e.store(a.dgate + (size_t)(group + in_block) * d + col);
+        }
       }
     }
+    advance(row, in_group);
+    if (kWhole && in_group == 0) group += gridDim.x * teams;
   }
   // the teams' sums, then to the workspace, or where they belong if this is the only workgroup
   auto add_teams = [&](const float (&acc)[kNc][8], auto put) {
@@ -655,64 +678,61 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       for (int i = 0; i < decltype(n)::value; ++i) to[col + i] = v[i];
     };
   };
-  if (kPre && a.dw_pre) add_teams(acc_pre, store(gridDim.x == 1 ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d));
-  if (kRes && kMany && a.dw_post) add_teams(acc_post, store(gridDim.x == 1 ? a.dw_post : a.part_post + (size_t)blockIdx.x * d));
-  if (kRes && !kMany && (a.dw_post || a.dgate)) {
-    if (gridDim.x == 1) add_teams(acc_group, [&](int col, const float* v, auto n) { finish_post<decltype(n)::value>(a, col, v); });
+  const bool alone = gridDim.x == 1;
+  if (kPre && a.dw_pre) add_teams(acc_pre, store(alone ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d));
+  if (kRes && kWhole && a.dw_post) add_teams(acc_post, store(alone ? a.dw_post : a.part_post + (size_t)blockIdx.x * d));
+  if (kRes && !kWhole && (a.dw_post || a.dgate)) {
+    if (alone) add_teams(acc_group, [&](int col, const float* v, auto n) { finish_post<decltype(n)::value>(a, col, v); });
     else add_teams(acc_group, store(a.part_post + (size_t)blockIdx.x * d));
   }
 }
 
-// Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre, 1 dw_post (and the gradient of a single row of gates); from
-// 2 on the teams' sums for rows of the gate that lie in more than one team: each row of the gate in turn where it has at
-// least as many rows as a team, else those across the border behind each team.  A workgroup takes 32 columns (a cache line of each
-// sum): 8 lanes of four, and 128 groups of 8 lanes that share out the sums.  Added up in one order.
+// Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre; 1 dw_post, each times its row of the gate if the
+// workgroups have not done that (and the gradient of a single row of gates); from 2 on the gradients of several rows of gates, `share` sums
+// each.  A workgroup takes 32 columns (a cache line of each sum): 8 lanes of four, and 128 groups of 8 lanes; of these `slices`
+// (a power of two) share out the sums of a result, and are added up pair by pair.
 constexpr int kReduceThreads = 1024, kReduceCols = 32, kReduceSlices = kReduceThreads / 8;
-template <bool kMany>
-__global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n) {
-  __shared__ norm_f32x4 lds[kReduceThreads / 64][8];
+__global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n, int whole, int gate_slices) {
+  __shared__ norm_f32x4 lds[kReduceSlices][8];
   const int lane = threadIdx.x % 8, slice = threadIdx.x / 8, d = a.d;
   const int col = blockIdx.x * kReduceCols + lane * 4;
+  const int gates = a.dgate && !whole ? n / a.share : 0;
+  const bool one_gate = gates == 1;
+  int slices = kReduceSlices, first = 0, count = n, group = 0;
   const float* part = blockIdx.y == 0 ? a.part_pre : a.part_post;
-  int first = 0, last = n - 1, group = 0;
-  if (blockIdx.y < 2 && (n == 1 || (blockIdx.y == 0 ? !a.dw_pre : !(a.dw_post || (a.dgate && !kMany))))) return;
+  if (blockIdx.y == 0 ? !a.dw_pre : blockIdx.y == 1 && !a.dw_post && !one_gate) return;
   if (blockIdx.y >= 2) {
-    const int i = blockIdx.y - 2;
-    group = a.gate_rows >= a.rows ? i : (int)(((int64_t)(i + 1) * a.rows - 1) / a.gate_rows);
-    const int64_t from = (int64_t)group * a.gate_rows, to = min(from + a.gate_rows, (int64_t)a.S);
-    first = (int)(from / a.rows);
-    last = (int)((to - 1) / a.rows);
-    if (first == last) return;               // written by the team
-    part = a.part_gate;
+    slices = gate_slices;
+    group = (blockIdx.y - 2) * (kReduceSlices / slices) + slice / slices;
+    first = group * a.share;
+    count = group < gates ? a.share : 0;
   }
+  const bool weighted = blockIdx.y == 1 && gates > 1;
   norm_f32x4 sum = {0, 0, 0, 0};
   if (col < d) {
 #pragma unroll 4
-    for (int p = first + slice; p <= last; p += kReduceSlices) {
-      const size_t at = (blockIdx.y >= 2 && p == first ? (size_t)a.teams : 0) + p;
-      sum += *reinterpret_cast<const norm_f32x4*>(part + at * d + col);
+    for (int p = slice % slices; p < count; p += slices) {
+      norm_f32x4 v = *reinterpret_cast<const norm_f32x4*>(part + (size_t)(first + p) * d + col);
+      if (weighted) {
+        for (int i = 0; i < 4; ++i) v[i] *= gate_factor(a, p / a.share, col + i);
+      }
+      sum += v;
     }
   }
-#pragma unroll
-  for (int x = 8; x < 64; x *= 2) {
-    norm_f32x4 o;
-    for (int i = 0; i < 4; ++i) o[i] = __shfl_xor(sum[i], x);
-    sum += o;
+  lds[slice][lane] = sum;
+  for (int s = slices / 2; s > 0; s /= 2) {
+    __syncthreads();
+    if (slice % slices < s) lds[slice][lane] = sum += lds[slice + s][lane];
   }
-  if (threadIdx.x % 64 < 8) lds[threadIdx.x / 64][lane] = sum;
-  __syncthreads();
-  if (slice || col >= d) return;
-#pragma unroll
-  for (int s = 1; s < kReduceThreads / 64; ++s) sum += lds[s][lane];
+  if (slice % slices || col >= d || count == 0) return;
   float t[4];
   for (int i = 0; i < 4; ++i) t[i] = sum[i];
-  if (blockIdx.y == 1 && !kMany) {
+  if (blockIdx.y == 1 && !whole && !weighted) {
     finish_post<4>(a, col, t);
     return;
   }
   float* const to = blockIdx.y == 0 ? a.dw_pre : blockIdx.y == 1 ? a.dw_post : a.dgate + (size_t)group * d;
-  for (int i = 0; i < 4; ++i)
-    to[col + i] = blockIdx.y < 2 ? t[i] : a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col + i] : 1.f) : 1.f) * t[i];
+  for (int i = 0; i < 4; ++i) to[col + i] = blockIdx.y < 2 ? t[i] : post_weight(a, col + i) * t[i];
 }
 
 }  // namespace mst

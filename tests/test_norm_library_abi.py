@@ -37,21 +37,29 @@ def test_workspace_and_rows_of_the_backward(mst):
         for S in (1, 2, 3, 63, 64, 1000, 8192, 131072, (1 << 30) - 1):
             if S * d > 1 << 36:
                 continue
-            info = mst.mst_norm_bwd_info(S, d)
-            teams, all_teams = info["teams"], info["teams"] * info["workgroups"]
-            assert info["threads"] % 64 == 0 and info["threads"] <= 1024
-            assert info["threads"] // teams * 8 * (1 if d <= 8192 else 2) >= d
-            assert info["rows"] * (all_teams - teams) < S <= info["rows"] * all_teams
-            one, many = mst.mst_norm_workspace_bytes(S, d), mst.mst_norm_workspace_bytes(S, d, 1)
-            sums = 2 * info["workgroups"] * d * 4 if info["workgroups"] > 1 else 0
-            assert one % 256 == 0 and sums <= one <= sums + 512
-            gates = 2 * all_teams * d * 4 if S > 1 else 0
-            assert sums + gates <= many <= sums + gates + 512
-            assert teams * info["rows"] * d < 1 << 29           # offsets of a workgroup's rows
-            assert many <= 1 << 27                       # whatever the rows
+            one = mst.mst_norm_workspace_bytes(S, d)
             assert mst.mst_norm_workspace_bytes(S, d, S) == mst.mst_norm_workspace_bytes(S, d, S + 5) == one
-            seen.add(info["workgroups"] == 1)
-    assert seen == {True, False}
+            for L in sorted({0, 1, 2, 7, 100, S // 3 + 1, S - 1 or 1, S, S + 3}):
+                info = mst.mst_norm_bwd_info(S, d, L)
+                teams, rows, groups, whole = (info[k] for k in ("teams", "rows", "workgroups", "whole"))
+                length = min(L, S) if L else S
+                gates = -(-S // length)
+                assert info["threads"] % 64 == 0 and info["threads"] <= 1024
+                assert info["threads"] // teams * 8 * (1 if d <= 8192 else 2) >= d
+                if whole:                                # every row of the gate has a team
+                    assert gates > 1 and rows % length == 0
+                    assert teams * groups * (rows // length - 1) < gates <= teams * groups * (rows // length)
+                    assert teams * length * d < 1 << 29  # offsets of a workgroup's rows at a time
+                else:
+                    assert groups % gates == 0           # as many workgroups each
+                    share = groups // gates
+                    assert teams * rows * (share - 1) < length <= teams * rows * share
+                bytes_ = mst.mst_norm_workspace_bytes(S, d, L)
+                sums = 2 * groups * d * 4 if groups > 1 else 0
+                assert bytes_ % 256 == 0 and sums <= bytes_ <= sums + 256
+                assert bytes_ <= 1 << 28
+                seen.add((groups == 1, bool(whole)))
+    assert seen == {(True, False), (False, False), (True, True), (False, True)}
     for S, d in ((0, 8), (-1, 8), (1, 0), (1, 12), (1, 16392), (1 << 30, 8), ((1 << 23) + 1, 8192)):
         with pytest.raises(mst.MstError) as e:
             mst.mst_norm_workspace_bytes(S, d)
