@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -43,9 +44,9 @@ def _compile(src_name: str, lib_path: str, verbose: bool) -> str:
 def build(verbose: bool = False) -> str:
     """Compile csrc/mst_api.hip into libmst_lmhead.so, csrc/mst_mlp_api.hip into libmst_mlp.so and csrc/mst_norm_api.hip
     into libmst_norm.so; returns the path of the LM-head library."""
-    _compile("mst_norm_api.hip", NORM_LIB_PATH, verbose)
-    _compile("mst_mlp_api.hip", MLP_LIB_PATH, verbose)
-    return _compile("mst_api.hip", LIB_PATH, verbose)
+    jobs = [("mst_api.hip", LIB_PATH), ("mst_mlp_api.hip", MLP_LIB_PATH), ("mst_norm_api.hip", NORM_LIB_PATH)]
+    with ThreadPoolExecutor(len(jobs)) as pool:
+        return list(pool.map(lambda job: _compile(*job, verbose), jobs))[0]
 
 
 if __name__ == "__main__":

@@ -12,6 +12,7 @@ using namespace mst;
 using mst_host::misaligned;
 
 constexpr int kNumCu = 256;
+constexpr int64_t kCacheBytes = 128 << 20;
 
 mst_status check_launch() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
 
@@ -80,9 +81,9 @@ struct BwdPlan {
   bool whole;                            // teams take whole rows of the gate
   int64_t gates, share, groups;          // rows of the gate (1 without); workgroups of each; workgroups
   int rows;                              // that a team takes in turn
-  BwdPlan(int64_t S, int64_t d, int64_t gate_rows) : row(d) {
+  BwdPlan(int64_t S, int64_t d, int64_t gate_rows, bool pre) : row(d) {
     const int64_t L = gate_rows ? std::min(gate_rows, S) : S;
-    const int64_t most = kNumCu * std::max(1, 1024 / row.threads());      // workgroups that are resident together
+    const int64_t most = kNumCu * std::max(1, (pre ? 512 : 1024) / row.threads());
     gates = (S + L - 1) / L;
     whole = gates > 1 && (2 * gates >= most * row.teams || L < row.teams) && L * row.teams * d < (int64_t(1) << 29);
     if (whole) {
@@ -120,7 +121,7 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p, st);
 }
 
-template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO>
+template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy>
 mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t st) {
   a.rows = p.rows;
   a.share = (int)p.share;
@@ -130,9 +131,9 @@ mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t 
   const dim3 grid((unsigned)p.groups), block(p.row.threads());
   const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // at most 16 KB
   if (p.row.chunks == 1)
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, 1>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, kPolicy, 1>), grid, block, lds, st, a);
   else
-    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, 2>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, kPolicy, 2>), grid, block, lds, st, a);
   if (p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) {
     int slices = 1;                                       // of the sums of a row of the gate
     while (slices < kReduceSlices && slices < p.share) slices *= 2;
@@ -146,16 +147,20 @@ mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t 
 template <class T, bool kPre, bool kRes>
 mst_status dispatch_bwd(NormBwd a, int64_t gate_rows, void* workspace, hipStream_t st) {
   constexpr bool kX = kPre, kO = kRes;             // where there can be a checkpoint
-  const BwdPlan p(a.S, a.d, gate_rows);
+  const BwdPlan p(a.S, a.d, gate_rows, kPre);
   a.gate_rows = (int)(gate_rows ? std::min<int64_t>(gate_rows, a.S) : a.S);
-  auto go = [&](auto w) {
+  auto go = [&](auto w, auto stream) {
     constexpr bool kWhole = kRes && decltype(w)::value;
-    if (a.codes_x && a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, kX, kO>(a, p, workspace, st);
-    if (a.codes_x) return launch_bwd<T, kPre, kRes, kWhole, kX, false>(a, p, workspace, st);
-    if (a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, false, kO>(a, p, workspace, st);
-    return launch_bwd<T, kPre, kRes, kWhole, false, false>(a, p, workspace, st);
+    constexpr int kPolicy = decltype(stream)::value ? kNonTemporalAccess : 0;
+    if (a.codes_x && a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, kX, kO, kPolicy>(a, p, workspace, st);
+    if (a.codes_x) return launch_bwd<T, kPre, kRes, kWhole, kX, false, kPolicy>(a, p, workspace, st);
+    if (a.codes_o) return launch_bwd<T, kPre, kRes, kWhole, false, kO, kPolicy>(a, p, workspace, st);
+    return launch_bwd<T, kPre, kRes, kWhole, false, false, kPolicy>(a, p, workspace, st);
   };
-  return p.whole ? go(std::true_type()) : go(std::false_type());
+  const int64_t n = (int64_t)a.S * a.d, t = sizeof(T);
+  const bool stream = n * ((kPre ? 2 + 2 * t + (a.codes_x ? 1 : t) : t) + (kRes ? 3 : 0)) > kCacheBytes;
+  if (p.whole) return stream ? go(std::true_type(), std::true_type()) : go(std::true_type(), std::false_type());
+  return stream ? go(std::false_type(), std::true_type()) : go(std::false_type(), std::false_type());
 }
 template <bool kPre, bool kRes>
 mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_rows, void* workspace, hipStream_t st) {
@@ -207,16 +212,16 @@ mst_status mst_norm_workspace_bytes(int64_t S, int64_t d, int64_t gate_rows, siz
   if (s != MST_OK) return s;
   if (gate_rows < 0) return MST_ERR_BAD_ARGUMENT;
   if (!bytes) return MST_ERR_NULL_POINTER;
-  *bytes = workspace_bytes(BwdPlan(S, d, gate_rows), d);
+  *bytes = std::max(workspace_bytes(BwdPlan(S, d, gate_rows, false), d), workspace_bytes(BwdPlan(S, d, gate_rows, true), d));
   return MST_OK;
 }
 
-mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t gate_rows, int64_t* info) {
+mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t gate_rows, int32_t prenorm, int64_t* info) {
   mst_status s = check_shape(S, d);
   if (s != MST_OK) return s;
   if (gate_rows < 0) return MST_ERR_BAD_ARGUMENT;
   if (!info) return MST_ERR_NULL_POINTER;
-  const BwdPlan p(S, d, gate_rows);
+  const BwdPlan p(S, d, gate_rows, prenorm != 0);
   info[0] = p.row.threads();
   info[1] = p.row.teams;
   info[2] = p.rows;
@@ -305,7 +310,7 @@ mst_status mst_prenorm_bwd(const void* dH, const void* X, const int8_t* codes, c
   if (!good_type(stream_type) || !good_norm(eps, w_offset) || !both_or_neither(codes, exps) || (X && codes) || (dw_pre && !w_pre))
     return MST_ERR_BAD_ARGUMENT;
   if (w_pre && !dw_pre) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d, 0), d);
+  const size_t need = workspace_bytes(BwdPlan(S, d, 0, true), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   Operands ops;
   ops.add(dH, S * d, 2, false, true);
@@ -367,7 +372,7 @@ mst_status mst_residual_bwd(const void* dY, int32_t stream_type, const void* O, 
       (dw_post && !w_post) || (dgate && !gate))
     return MST_ERR_BAD_ARGUMENT;
   if ((w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes)) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows), d);
+  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows, false), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   if (!normalize && !gate) O = nullptr, codes = nullptr, exps = nullptr;
   Operands ops;
@@ -442,7 +447,7 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
       (O && codes_o) || (Y && codes_y) || (w_post && !normalize) || (dw_post && !w_post) || (dgate && !gate) || (dw_pre && !w_pre))
     return MST_ERR_BAD_ARGUMENT;
   if ((w_pre && !dw_pre) || (w_post && !dw_post) || (gate && !dgate) || ((normalize || gate) && !O && !codes_o)) return MST_ERR_NULL_POINTER;
-  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows), d);
+  const size_t need = workspace_bytes(BwdPlan(S, d, gate_rows, true), d);
   if (!workspace || workspace_size < need) return MST_ERR_WORKSPACE;
   if (!normalize && !gate) O = nullptr, codes_o = nullptr, exps_o = nullptr;
   Operands ops;

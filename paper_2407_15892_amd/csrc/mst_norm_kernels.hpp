@@ -434,37 +434,41 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t
 }
 // Offset in entries of a lane that has no columns: behind those rows (less than 2^29 entries) in bytes of 1, 2 or 4.
 constexpr uint32_t kNoColumn = 1u << 29;
+// Rows whose loads are under way while one is summed up.
+template <class T> constexpr int rows_ahead(bool pre, bool res, int chunks) { return pre && !res && chunks == 1 && sizeof(T) == 2 ? 2 : 1; }
 
-template <class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
+constexpr int kNonTemporalAccess = 2;         // cache policy of buffer loads and stores
+
+template <int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
   const uint32_t byte = at * (uint32_t)sizeof(T);
   if constexpr (sizeof(T) == 2) {
-    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
+    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
   } else {
-    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
-    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, 0));
+    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
+    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, kPolicy));
   }
 }
 template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
   const uint32_t byte = at * (uint32_t)sizeof(T);
   if constexpr (sizeof(T) == 2) {
-    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, kNonTemporalAccess);
   } else {
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, kNonTemporalAccess);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, kNonTemporalAccess);
   }
 }
 
 // A row's eight entries: the tensor's, or those of its checkpoint.
-template <class T, bool kCheckpoint> struct Source {
+template <class T, bool kCheckpoint, int kPolicy> struct Source {
   Eight<T> e;
-  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight(e, rows, at); }
+  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight<kPolicy>(e, rows, at); }
   __device__ void get(float (&v)[8]) const { e.get(v); }
 };
-template <class T> struct Source<T, true> {
+template <class T, int kPolicy> struct Source<T, true, kPolicy> {
   EightCodes e;
   __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
-    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0));
-    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, 0);
+    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, kPolicy));
+    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, kPolicy);
   }
   __device__ void get(float (&v)[8]) const { e.get(v); }
 };
@@ -493,7 +497,7 @@ template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, 
 //                   and sums up dw_post.
 // With x the row of X, q its rstd, a = dH * ~w: the gradient is dres + q a - x q^3 sum(a x) / d; likewise for O with
 // b = dY * f, f = scale * gate * ~w_post.  One sum over the row waits for another where both norms are there.
-template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kNc>
+template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
   __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
@@ -531,24 +535,25 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
   };
   uint32_t at[kNc], block[kNc];
-  Eight<__bf16> dh_next[kNc];
-  Source<T, kCkptX> x_next[kNc];
-  Eight<T> dy_next[kNc];
-  Source<__bf16, kCkptO> o_next[kNc];
+  constexpr int kAhead = rows_ahead<T>(kPre, kRes, kNc);
+  Eight<__bf16> dh_next[kAhead][kNc];
+  Source<T, kCkptX, kPolicy> x_next[kAhead][kNc];
+  Eight<T> dy_next[kAhead][kNc];
+  Source<__bf16, kCkptO, kPolicy> o_next[kAhead][kNc];
   auto rows_at = [&](int64_t r) { return (int)max((int64_t)0, min((int64_t)(teams - 1) * apart + 1, end - r)); };
-  auto load = [&]() {
+  auto load = [&](int slot) {
     const int rows = rows_at(next);
     const __amdgpu_buffer_rsrc_t dy_rows = rows_of(kPre ? a.dres : a.dY, next, rows, (int)sizeof(T) * d);
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
       if (kPre) {
-        load_eight(dh_next[k], rows_of(a.dH, next, rows, 2 * d), at[k]);
-        x_next[k].load(kCkptX ? rows_of(a.codes_x, next, rows, d) : rows_of(a.X, next, rows, (int)sizeof(T) * d),
+        load_eight<kPolicy>(dh_next[slot][k], rows_of(a.dH, next, rows, 2 * d), at[k]);
+        x_next[slot][k].load(kCkptX ? rows_of(a.codes_x, next, rows, d) : rows_of(a.X, next, rows, (int)sizeof(T) * d),
                        rows_of(a.exps_x, next, rows, blocks), at[k], block[k]);
       }
-      load_eight(dy_next[k], dy_rows, at[k]);
+      load_eight<kPolicy>(dy_next[slot][k], dy_rows, at[k]);
       if (kRes)
-        o_next[k].load(kCkptO ? rows_of(a.codes_o, next, rows, d) : rows_of(a.O, next, rows, 2 * d), rows_of(a.exps_o, next, rows, blocks),
+        o_next[slot][k].load(kCkptO ? rows_of(a.codes_o, next, rows, d) : rows_of(a.O, next, rows, 2 * d), rows_of(a.exps_o, next, rows, blocks),
                        at[k], block[k]);
     }
     advance(next, next_in_group);
@@ -561,8 +566,9 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     if (kPre) weights(a.w_pre, a.offset, column(k), on, w[k]);
     if (kRes && !kWhole) load_f(k, group, true);
   }
-  load();
-  for (int i_row = 0; i_row < a.rows; ++i_row) {         // as often in every team, for the barriers; zeros behind the last row
+#pragma unroll
+  for (int slot = 0; slot < kAhead; ++slot) load(slot);
+  auto one_row = [&](int slot) {
     float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
     float sums[kFirst];
 #pragma unroll
@@ -573,10 +579,10 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      dy_next[k].get(dy[k]);
+      dy_next[slot][k].get(dy[k]);
       if (kPre) {
-        x_next[k].get(x[k]);
-        dh_next[k].get(dh[k]);
+        x_next[slot][k].get(x[k]);
+        dh_next[slot][k].get(dh[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[0] = fmaf(x[k][i], x[k][i], sums[0]);
@@ -584,7 +590,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
       }
       if (kRes) {
-        o_next[k].get(o[k]);
+        o_next[slot][k].get(o[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPre ? 2 : 0] = fmaf(o[k][i], o[k][i], sums[kPre ? 2 : 0]);
@@ -592,7 +598,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
       }
     }
-    load();
+    load(slot);
     const int rows = rows_at(row);
     if (kPre || a.normalize) first_sums(sums);
     float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
@@ -651,6 +657,10 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     }
     advance(row, in_group);
     if (kWhole && in_group == 0) group += gridDim.x * teams;
+  };
+  for (int i_row = 0; i_row < a.rows; i_row += kAhead) {         // as often in every team, for the barriers; zeros behind the last row
+#pragma unroll
+    for (int slot = 0; slot < kAhead; ++slot) one_row(slot);
   }
   // the teams' sums, then to the workspace, or where they belong if this is the only workgroup
   auto add_teams = [&](const float (&acc)[kNc][8], auto put) {
@@ -690,10 +700,10 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 // Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre; 1 dw_post, each times its row of the gate if the
 // workgroups have not done that (and the gradient of a single row of gates); from 2 on the gradients of several rows of gates, `share` sums
 // each.  A workgroup takes 32 columns (a cache line of each sum): 8 lanes of four, and 128 groups of 8 lanes; of these `slices`
-// (a power of two) share out the sums of a result, and are added up pair by pair.
+// (a power of two) share out the sums of a result, and are added up in one order.
 constexpr int kReduceThreads = 1024, kReduceCols = 32, kReduceSlices = kReduceThreads / 8;
 __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n, int whole, int gate_slices) {
-  __shared__ norm_f32x4 lds[kReduceSlices][8];
+  __shared__ norm_f32x4 lds[kReduceSlices / 8][8];
   const int lane = threadIdx.x % 8, slice = threadIdx.x / 8, d = a.d;
   const int col = blockIdx.x * kReduceCols + lane * 4;
   const int gates = a.dgate && !whole ? n / a.share : 0;
@@ -719,10 +729,19 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a,
       sum += v;
     }
   }
-  lds[slice][lane] = sum;
-  for (int s = slices / 2; s > 0; s /= 2) {
+#pragma unroll
+  for (int x = 8; x < 64; x *= 2) {            // the eight slices of a wave
+    if (x >= slices * 8) break;
+    norm_f32x4 o;
+    for (int i = 0; i < 4; ++i) o[i] = __shfl_xor(sum[i], x);
+    sum += o;
+  }
+  if (slices > 8) {
+    if (slice % 8 == 0) lds[slice / 8][lane] = sum;
     __syncthreads();
-    if (slice % slices < s) lds[slice][lane] = sum += lds[slice + s][lane];
+    if (slice % slices == 0) {
+      for (int s = 1; s < slices / 8; ++s) sum += lds[slice / 8 + s][lane];
+    }
   }
   if (slice % slices || col >= d || count == 0) return;
   float t[4];

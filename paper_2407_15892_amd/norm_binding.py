@@ -42,7 +42,7 @@ def load_norm_library() -> ctypes.CDLL:
     lib.mst_norm_version.restype = c.c_char_p
     lib.mst_norm_version.argtypes = []
     lib.mst_norm_workspace_bytes.argtypes = [i64, i64, i64, c.POINTER(size)]
-    lib.mst_norm_bwd_info.argtypes = [i64, i64, i64, c.POINTER(i64)]
+    lib.mst_norm_bwd_info.argtypes = [i64, i64, i64, i32, c.POINTER(i64)]
     lib.mst_ckpt_pack.argtypes = [p, i32, i64, i64, p, p, p]
     lib.mst_ckpt_unpack.argtypes = [p, p, i64, i64, p, i32, p]
     lib.mst_prenorm_fwd.argtypes = [p, i32, p, f32, f32, i64, i64, p, p, p, p]
@@ -138,11 +138,11 @@ def mst_norm_workspace_bytes(S: int, d: int, gate_rows: int = 0) -> int:
     return int(n.value)
 
 
-def mst_norm_bwd_info(S: int, d: int, gate_rows: int = 0) -> dict:
+def mst_norm_bwd_info(S: int, d: int, gate_rows: int = 0, prenorm: bool = True) -> dict:
     """How a backward call goes over the rows: threads of a workgroup, teams in it, rows of a team, workgroups, whether a team
-    takes whole rows of the gate."""
+    takes whole rows of the gate.  prenorm: False for mst_residual_bwd."""
     info = (ctypes.c_int64 * 5)()
-    _check(load_norm_library().mst_norm_bwd_info(S, d, gate_rows, info))
+    _check(load_norm_library().mst_norm_bwd_info(S, d, gate_rows, int(prenorm), info))
     return dict(zip(("threads", "teams", "rows", "workgroups", "whole"), (int(x) for x in info)))
 
 

@@ -103,9 +103,9 @@ def close(got, want, reach, ops, to="bf16"):
                              f"tolerance {tol[tuple(at)]}; worst {np.nanmax(np.abs(got - want) / tol)} tolerances")
 
 
-def column_ops(S, d, gate_rows=0):
+def column_ops(S, d, gate_rows=0, prenorm=True):
     """Operations in a row of a sum over rows: the rows of a team, the teams of a workgroup, then the workgroups: a 128th each, then
     7 steps; and the products with gate, weight and scale."""
     import paper_2407_15892_amd as mst
-    info = mst.mst_norm_bwd_info(S, d, gate_rows)
+    info = mst.mst_norm_bwd_info(S, d, gate_rows, prenorm)
     return 2 * info["rows"] + info["teams"] + -(-info["workgroups"] // 128) + 7 + 4

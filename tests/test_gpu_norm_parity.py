@@ -93,7 +93,7 @@ def check_forward(c, parts, got, checkpoints=True):
 def check_backward(c, parts, got, from_checkpoint, dres=True):
     y = orc.restore(*orc.checkpoint(c.y)) if from_checkpoint else c.y
     o = orc.restore(*orc.checkpoint(c.o)) if from_checkpoint else c.o
-    cols = column_ops(c.S, c.d, c.gate_rows if parts != "pre" else 0)
+    cols = column_ops(c.S, c.d, c.gate_rows if parts != "pre" else 0, parts != "res")
     dy, reach, ops = c.dres, np.abs(c.dres), 0
     if parts != "res":
         dy, dw, reach, dw_reach = orc.norm_bwd(c.dh, y, c.w_pre, c.offset, EPS)

@@ -39,8 +39,8 @@ def test_workspace_and_rows_of_the_backward(mst):
                 continue
             one = mst.mst_norm_workspace_bytes(S, d)
             assert mst.mst_norm_workspace_bytes(S, d, S) == mst.mst_norm_workspace_bytes(S, d, S + 5) == one
-            for L in sorted({0, 1, 2, 7, 100, S // 3 + 1, S - 1 or 1, S, S + 3}):
-                info = mst.mst_norm_bwd_info(S, d, L)
+            for L, prenorm in [(L, p) for L in sorted({0, 1, 2, 7, 100, S // 3 + 1, S - 1 or 1, S, S + 3}) for p in (False, True)]:
+                info = mst.mst_norm_bwd_info(S, d, L, prenorm)
                 teams, rows, groups, whole = (info[k] for k in ("teams", "rows", "workgroups", "whole"))
                 length = min(L, S) if L else S
                 gates = -(-S // length)
@@ -54,9 +54,10 @@ def test_workspace_and_rows_of_the_backward(mst):
                     assert groups % gates == 0           # as many workgroups each
                     share = groups // gates
                     assert teams * rows * (share - 1) < length <= teams * rows * share
-                bytes_ = mst.mst_norm_workspace_bytes(S, d, L)
-                sums = 2 * groups * d * 4 if groups > 1 else 0
-                assert bytes_ % 256 == 0 and sums <= bytes_ <= sums + 256
+                sums = -(-2 * groups * d * 4 // 256) * 256 if groups > 1 else 256
+                other = mst.mst_norm_bwd_info(S, d, L, not prenorm)["workgroups"]
+                bytes_ = mst.mst_norm_workspace_bytes(S, d, L)           # that of the call which needs most
+                assert bytes_ == max(sums, -(-2 * other * d * 4 // 256) * 256 if other > 1 else 256)
                 assert bytes_ <= 1 << 28
                 seen.add((groups == 1, bool(whole)))
     assert seen == {(True, False), (False, False), (True, True), (False, True)}
