@@ -12,7 +12,7 @@ using namespace mst;
 using mst_host::misaligned;
 
 constexpr int kNumCu = 256;
-constexpr int64_t kCacheBytes = 128 << 20;
+constexpr int64_t kCacheBytes = 192 << 20;
 
 mst_status check_launch() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
 
@@ -73,7 +73,7 @@ struct RowPlan {
   int threads() const { return team.lanes * team.waves * teams; }
 };
 
-constexpr int kFwdRows[2] = {2, 1};      // rows of a team with one and with two chunks
+constexpr int fwd_rows(bool res, int chunks) { return chunks == 1 && !res ? 2 : 1; }      // of a team
 
 // How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate.
 struct BwdPlan {
@@ -103,14 +103,15 @@ size_t workspace_bytes(const BwdPlan& p, int64_t d) {      // dw_pre and dw_post
   return mst_host::align_up(p.groups > 1 ? 2 * (size_t)p.groups * d * 4 : 1, 256);
 }
 
-template <class T, bool kRes, bool kPre, bool kRebuild, int kNc>
+template <class T, bool kRes, bool kPre, bool kRebuild, int kPolicy, int kNc>
 mst_status launch_fwd_chunks(NormFwd a, const RowPlan& p, hipStream_t st) {
-  const int64_t kRows = kFwdRows[kNc - 1] * p.teams;              // of a workgroup
+  constexpr int kRb = fwd_rows(kRes, kNc);
+  const int64_t kRows = kRb * p.teams;              // of a workgroup
   const int64_t most = (int64_t(1) << 31) / p.threads() * kRows;  // a launch has fewer than 2^32 lanes
   a.team = p.team;
   for (int64_t r = 0; r < a.S; r += most) {
     a.row0 = (int)r;
-    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kNc, kFwdRows[kNc - 1]>),
+    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kPolicy, kNc, kRb>),
                        dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)), dim3(p.threads()), 0, st, a);
   }
   return check_launch();
@@ -118,7 +119,10 @@ mst_status launch_fwd_chunks(NormFwd a, const RowPlan& p, hipStream_t st) {
 template <class T, bool kRes, bool kPre, bool kRebuild>
 mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   const RowPlan p(a.d);
-  return p.chunks == 1 ? launch_fwd_chunks<T, kRes, kPre, kRebuild, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 2>(a, p, st);
+  const int64_t t = kRebuild ? 1 : sizeof(T), n = (int64_t)a.S * a.d;
+  const bool stream = n * (t + (kPre ? 2 : 0) + (kRes ? 2 + t : 0)) > kCacheBytes;
+  if (p.chunks == 2) return launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 2>(a, p, st);
+  return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
 }
 
 template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy>
@@ -149,6 +153,7 @@ mst_status dispatch_bwd(NormBwd a, int64_t gate_rows, void* workspace, hipStream
   constexpr bool kX = kPre, kO = kRes;             // where there can be a checkpoint
   const BwdPlan p(a.S, a.d, gate_rows, kPre);
   a.gate_rows = (int)(gate_rows ? std::min<int64_t>(gate_rows, a.S) : a.S);
+  a.gates = (int)p.gates;
   auto go = [&](auto w, auto stream) {
     constexpr bool kWhole = kRes && decltype(w)::value;
     constexpr int kPolicy = decltype(stream)::value ? kNonTemporalAccess : 0;
@@ -173,21 +178,25 @@ int64_t ckpt_rows(int64_t d) { return (int64_t(1) << 30) / (4 * tail_blocks(d));
 
 template <class T>
 void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
+  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
   const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
+  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
   for (int64_t r = 0, n; r < S; r += n) {
     n = std::min(S - r, ckpt_rows(d));
     const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL(k_ckpt_pack<T>, dim3((slots + kCkptThreads - 1) / kCkptThreads), dim3(kCkptThreads), 0, st,
+    hipLaunchKernelGGL((stream ? k_ckpt_pack<T, true> : k_ckpt_pack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
                        X + r * d, per_row, slots, (int)d, codes + r * d, exps + r * tail_blocks(d));
   }
 }
 template <class T>
 void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
+  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
   const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
+  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
   for (int64_t r = 0, n; r < S; r += n) {
     n = std::min(S - r, ckpt_rows(d));
     const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL(k_ckpt_unpack<T>, dim3((slots + kCkptThreads - 1) / kCkptThreads), dim3(kCkptThreads), 0, st,
+    hipLaunchKernelGGL((stream ? k_ckpt_unpack<T, true> : k_ckpt_unpack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
                        codes + r * d, exps + r * tail_blocks(d), per_row, slots, (int)d, X + r * d);
   }
 }
@@ -277,7 +286,7 @@ mst_status mst_prenorm_fwd(const void* X, int32_t stream_type, const void* w_pre
   a.X = X; a.w_pre = bf(w_pre); a.H = static_cast<__bf16*>(H);
   a.codes_y = codes; a.exps_y = exps;
   a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
-  a.S = (int)S; a.d = (int)d;
+  a.S = (int)S; a.d = (int)d; a.gate_rows = (int)S; a.gates = 1;
   return stream_type == MST_TYPE_FP32 ? launch_fwd<float, false, true, false>(a, as_stream(stream))
                                       : launch_fwd<__bf16, false, true, false>(a, as_stream(stream));
 }
@@ -297,7 +306,7 @@ mst_status mst_prenorm_rebuild(const int8_t* codes, const uint8_t* exps, const v
   NormFwd a = {};
   a.codes_x = codes; a.exps_x = exps; a.w_pre = bf(w_pre); a.H = static_cast<__bf16*>(H);
   a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
-  a.S = (int)S; a.d = (int)d;
+  a.S = (int)S; a.d = (int)d; a.gate_rows = (int)S; a.gates = 1;
   return launch_fwd<__bf16, false, true, true>(a, as_stream(stream));
 }
 
@@ -354,7 +363,8 @@ mst_status mst_residual_fwd(const void* O, const void* X, int32_t stream_type, i
   a.codes_o = codes; a.exps_o = exps;
   a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
   a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
-  a.gate_rows = (int)std::min(gate_rows, S);
+  a.gate_rows = (int)(gate ? std::min(gate_rows, S) : S);
+  a.gates = (int)std::max<int64_t>(gate_groups, 1);
   return stream_type == MST_TYPE_FP32 ? launch_fwd<float, true, false, false>(a, as_stream(stream))
                                       : launch_fwd<__bf16, true, false, false>(a, as_stream(stream));
 }
@@ -426,7 +436,8 @@ mst_status mst_residual_prenorm_fwd(const void* O, const void* X, int32_t stream
   a.codes_o = codes_o; a.exps_o = exps_o; a.codes_y = codes_y; a.exps_y = exps_y;
   a.offset = w_offset; a.eps = eps; a.scale = scale; a.inv_d = 1.f / (float)d;
   a.S = (int)S; a.d = (int)d; a.normalize = normalize != 0;
-  a.gate_rows = (int)std::min(gate_rows, S);
+  a.gate_rows = (int)(gate ? std::min(gate_rows, S) : S);
+  a.gates = (int)std::max<int64_t>(gate_groups, 1);
   return stream_type == MST_TYPE_FP32 ? launch_fwd<float, true, true, false>(a, as_stream(stream))
                                       : launch_fwd<__bf16, true, true, false>(a, as_stream(stream));
 }

@@ -30,6 +30,8 @@ template <> struct Eight<__bf16> {
   norm_u32x4 u = {0, 0, 0, 0};
   __device__ void load(const __bf16* p) { u = *reinterpret_cast<const norm_u32x4*>(p); }
   __device__ void store(__bf16* p) const { *reinterpret_cast<norm_u32x4*>(p) = u; }
+  __device__ void load_streamed(const __bf16* p) { u = __builtin_nontemporal_load(reinterpret_cast<const norm_u32x4*>(p)); }
+  __device__ void store_streamed(__bf16* p) const { __builtin_nontemporal_store(u, reinterpret_cast<norm_u32x4*>(p)); }
   __device__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -55,6 +57,8 @@ template <> struct Eight<float> {
     *reinterpret_cast<norm_f32x4*>(p) = a;
     *reinterpret_cast<norm_f32x4*>(p + 4) = b;
   }
+  __device__ void load_streamed(const float* p) { load(p); }            // halves of a line: not past the caches
+  __device__ void store_streamed(float* p) const { store(p); }
   __device__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
@@ -79,8 +83,9 @@ template <int kByte> __device__ __forceinline__ float signed_byte(unsigned u) {
 struct EightCodes {
   norm_u32x2 c = {0, 0};
   unsigned e = 0;
-  __device__ void load(const int8_t* codes, const uint8_t* exp) {
-    c = *reinterpret_cast<const norm_u32x2*>(codes);
+  template <bool kStream> __device__ void load(const int8_t* codes, const uint8_t* exp) {
+    const norm_u32x2* const p = reinterpret_cast<const norm_u32x2*>(codes);
+    c = kStream ? __builtin_nontemporal_load(p) : *p;
     e = *exp;
   }
   __device__ void get(float (&v)[8]) const {
@@ -149,37 +154,58 @@ struct FastDiv {
 };
 
 constexpr int kCkptThreads = 256;
+template <class T> constexpr int kCkptEights = sizeof(T) == 2 ? 2 : 1;      // eights per lane, a workgroup's lanes apart
 
 // One lane per eight entries; a row takes a whole number of quads, so that a quad is a block.
-template <class T>
+template <class T, bool kStream>
 __global__ __launch_bounds__(kCkptThreads) void k_ckpt_pack(const T* X, FastDiv per_row, uint32_t slots, int d, int8_t* codes, uint8_t* exps) {
-  const uint32_t n = blockIdx.x * kCkptThreads + threadIdx.x;
-  const uint32_t row = per_row(n < slots ? n : 0), in_row = n - row * per_row.d;
-  const bool on = n < slots && (int)in_row * 8 < d;
-  Eight<T> x;
-  if (on) x.load(X + (size_t)row * d + in_row * 8);
-  float v[8];
-  x.get(v);
-  const Packed p = pack_eight(v);
-  if (!on) return;
-  *reinterpret_cast<norm_u32x2*>(codes + (size_t)row * d + in_row * 8) = p.codes;
-  if (threadIdx.x % 4 == 0) exps[(n >> 2)] = (uint8_t)p.exp;
+  constexpr int kEights = kCkptEights<T>;
+  Eight<T> x[kEights];
+  uint32_t n[kEights];
+  size_t at[kEights];
+  bool on[kEights];
+#pragma unroll
+  for (int i = 0; i < kEights; ++i) {
+    n[i] = (blockIdx.x * kEights + i) * kCkptThreads + threadIdx.x;
+    const uint32_t row = per_row(n[i] < slots ? n[i] : 0), in_row = n[i] - row * per_row.d;
+    on[i] = n[i] < slots && (int)in_row * 8 < d;
+    at[i] = (size_t)row * d + in_row * 8;
+    if (on[i]) kStream ? x[i].load_streamed(X + at[i]) : x[i].load(X + at[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kEights; ++i) {
+    float v[8];
+    x[i].get(v);
+    const Packed p = pack_eight(v);
+    if (!on[i]) continue;
+    __builtin_nontemporal_store(p.codes, reinterpret_cast<norm_u32x2*>(codes + at[i]));
+    if (threadIdx.x % 4 == 0) exps[n[i] >> 2] = (uint8_t)p.exp;
+  }
 }
 
-template <class T>
+template <class T, bool kStream>
 __global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* codes, const uint8_t* exps, FastDiv per_row, uint32_t slots, int d, T* X) {
-  const uint32_t n = blockIdx.x * kCkptThreads + threadIdx.x;
-  if (n >= slots) return;
-  const uint32_t row = per_row(n), in_row = n - row * per_row.d;
-  if ((int)in_row * 8 >= d) return;
-  const size_t at = (size_t)row * d + in_row * 8;
-  EightCodes c;
-  c.load(codes + at, exps + (n >> 2));
-  float v[8];
-  c.get(v);
-  Eight<T> x;
-  x.set(v);
-  x.store(X + at);
+  constexpr int kEights = kCkptEights<T>;
+  EightCodes c[kEights];
+  size_t at[kEights];
+  bool on[kEights];
+#pragma unroll
+  for (int i = 0; i < kEights; ++i) {
+    const uint32_t n = (blockIdx.x * kEights + i) * kCkptThreads + threadIdx.x;
+    const uint32_t row = per_row(n < slots ? n : 0), in_row = n - row * per_row.d;
+    on[i] = n < slots && (int)in_row * 8 < d;
+    at[i] = (size_t)row * d + in_row * 8;
+    if (on[i]) c[i].template load<kStream>(codes + at[i], exps + (n >> 2));
+  }
+#pragma unroll
+  for (int i = 0; i < kEights; ++i) {
+    if (!on[i]) continue;
+    float v[8];
+    c[i].get(v);
+    Eight<T> x;
+    x.set(v);
+    x.store_streamed(X + at[i]);
+  }
 }
 
 // ---- sums over a row -----------------------------------------------------------------------------------------------------
@@ -252,10 +278,72 @@ template <int kN> struct RowSums {
   }
 };
 
+// ---- rows and weights in memory ------------------------------------------------------------------------------------------
+
+// Some rows of a tensor as a buffer: what lies behind them, and a tensor that is not there, reads as zeros and takes no
+// stores.  Without branches around loads and stores the compiler knows how many are under way, and waits for the ones it needs.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t from, int rows, int row_bytes) {
+  const char* const at = static_cast<const char*>(p) + from * row_bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, p ? rows * row_bytes : 0, 0x00020000);
+}
+// Offset in entries of a lane that has no columns: behind those rows (less than 2^29 entries) in bytes of 1, 2 or 4.
+constexpr uint32_t kNoColumn = 1u << 29;
+// Rows whose loads are under way while one is summed up.
+template <class T> constexpr int rows_ahead(bool pre, bool res, int chunks) { return pre && !res && chunks == 1 && sizeof(T) == 2 ? 2 : 1; }
+
+constexpr int kNonTemporalAccess = 2;         // cache policy of buffer loads and stores
+constexpr int kStorePolicy = kNonTemporalAccess;
+
+template <int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
+  const uint32_t byte = at * (uint32_t)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
+  } else {
+    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
+    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, kPolicy));
+  }
+}
+template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
+  const uint32_t byte = at * (uint32_t)sizeof(T);
+  if constexpr (sizeof(T) == 2) {
+    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, kStorePolicy);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, 0);
+  }
+}
+
+// A row's eight entries: the tensor's, or those of its checkpoint.
+template <class T, bool kCheckpoint, int kPolicy> struct Source {
+  Eight<T> e;
+  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight<kPolicy>(e, rows, at); }
+  __device__ void get(float (&v)[8]) const { e.get(v); }
+};
+template <class T, int kPolicy> struct Source<T, true, kPolicy> {
+  EightCodes e;
+  __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
+    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, kPolicy));
+    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, kPolicy);
+  }
+  __device__ void get(float (&v)[8]) const { e.get(v); }
+};
+
+// Eight weights (or gates); the buffer of ones that are not there is empty.
+__device__ __forceinline__ Eight<__bf16> load_weights(const __bf16* w, int d, int col) {
+  Eight<__bf16> e;
+  load_eight<0>(e, rows_of(w, 0, 1, 2 * d), col < d ? col : kNoColumn);
+  return e;
+}
+__device__ __forceinline__ void weights(const Eight<__bf16>& e, bool there, float offset, float (&v)[8]) {
+  e.get(v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = offset + (there ? v[i] : 1.f);
+}
+
 // ---- forward -------------------------------------------------------------------------------------------------------------
 
 struct NormFwd {
-  const void* X;                   // stream type; without kRes NULL where codes_x stand for it
+  const void* X;                   // stream type; NULL with kRebuild, where codes_x stand for it
   const __bf16* O;
   const __bf16 *w_pre, *w_post;    // NULL: ones
   const __bf16* gate;              // NULL: ones
@@ -265,51 +353,57 @@ struct NormFwd {
   int8_t* codes_o; uint8_t* exps_o;
   int8_t* codes_y; uint8_t* exps_y;      // of Y, or without kRes of X
   float offset, eps, scale, inv_d;
-  int S, d, normalize, gate_rows;
+  int S, d, normalize;
+  int gate_rows, gates;            // without a gate S and 1
   int row0;                        // first row of the launch
   Team team;
 };
 
-// The weights of eight columns.
-__device__ __forceinline__ void weights(const __bf16* w, float offset, int col, bool on, float (&v)[8]) {
-  Eight<__bf16> e;
-  if (w) {
-    if (on) e.load(w + col);
-    e.get(v);
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = offset + (w ? v[i] : 1.f);
-}
-
-__device__ __forceinline__ void store_packed(const Packed& p, int8_t* codes, uint8_t* exps, size_t row, int d, int col) {
-  *reinterpret_cast<norm_u32x2*>(codes + row * d + col) = p.codes;
-  if (threadIdx.x % 4 == 0) exps[row * ((d + 31) / 32) + col / 32] = (uint8_t)p.exp;
+__device__ __forceinline__ void store_packed(const Packed& p, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
+  __builtin_amdgcn_raw_buffer_store_b64(p.codes, codes, at, 0, kStorePolicy);
+  __builtin_amdgcn_raw_buffer_store_b8((unsigned char)p.exp, exps, threadIdx.x % 4 ? kNoColumn : block, 0, 0);
 }
 
 // kRb rows per team, kNc chunks of 8 columns per lane.
-template <class T, bool kRes, bool kPre, bool kRebuild, int kNc, int kRb>
+template <class T, bool kRes, bool kPre, bool kRebuild, int kPolicy, int kNc, int kRb>
 __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   __shared__ float lds[2][kNormMaxWaves][kRb];
   RowSums<kRb> row_sums(lds, a.team);
-  const int threads = a.team.threads(), lane = threadIdx.x % threads, d = a.d;
-  const int r0 = a.row0 + (blockIdx.x * (blockDim.x / threads) + threadIdx.x / threads) * kRb;
-  const T* const X = static_cast<const T*>(a.X);
-  float x[kRb][kNc][8];
-  Eight<T> raw[kRb][kNc];
-  Eight<__bf16> o[kRb][kNc];
-  EightCodes c[kRb][kNc];
+  const int threads = a.team.threads(), lane = threadIdx.x % threads, teams = blockDim.x / threads, in_block = threadIdx.x / threads;
+  const int d = a.d, blocks = (d + 31) / 32;
+  const int first = a.row0 + (int)blockIdx.x * teams * kRb;
+  const int rows = min(teams * kRb, a.S - first);        // of the workgroup
+  const int first_gate = a.gates > 1 ? first / a.gate_rows : 0;
+  uint32_t at[kRb][kNc], block[kRb][kNc], gate_at[kRb][kNc];
+  Source<T, kRebuild, kPolicy> raw[kRb][kNc];
+  Eight<__bf16> o[kRb][kNc], g[kRb][kNc], w[kNc], wo[kNc];
 #pragma unroll
-  for (int r = 0; r < kRb; ++r)
+  for (int r = 0; r < kRb; ++r) {
+    const int row = r * teams + in_block;
+    const int gate = a.gates > 1 ? (first + row - first_gate * a.gate_rows) / a.gate_rows : 0;
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
       const int col = (k * threads + lane) * 8;
-      const size_t at = (size_t)(r0 + r) * d + col;
-      if (r0 + r < a.S && col < d) {
-        if (kRebuild) c[r][k].load(a.codes_x + at, a.exps_x + (size_t)(r0 + r) * ((d + 31) / 32) + col / 32);
-        else raw[r][k].load(X + at);
-        if (kRes) o[r][k].load(a.O + at);
-      }
+      at[r][k] = col < d ? row * d + col : kNoColumn;
+      block[r][k] = col < d ? row * blocks + col / 32 : kNoColumn;
+      gate_at[r][k] = col < d ? gate * d + col : kNoColumn;
+      raw[r][k].load(kRebuild ? rows_of(a.codes_x, first, rows, d) : rows_of(a.X, first, rows, (int)sizeof(T) * d), rows_of(a.exps_x, first, rows, blocks),
+                     at[r][k], block[r][k]);
+      if (kRes) load_eight<kPolicy>(o[r][k], rows_of(a.O, first, rows, 2 * d), at[r][k]);
     }
+  }
+#pragma unroll
+  for (int k = 0; k < kNc; ++k) {
+    const int col = (k * threads + lane) * 8;
+    if (kRes) {
+      wo[k] = load_weights(a.w_post, d, col);
+#pragma unroll
+      for (int r = 0; r < kRb; ++r) load_eight<0>(g[r][k], rows_of(a.gate, first_gate, min(teams * kRb, a.gates - first_gate), 2 * d), gate_at[r][k]);
+    }
+    if (kPre) w[k] = load_weights(a.w_pre, d, col);
+  }
+  const __amdgpu_buffer_rsrc_t codes_y = rows_of(a.codes_y, first, rows, d), exps_y = rows_of(a.exps_y, first, rows, blocks);
+  float x[kRb][kNc][8];
   if (kRes) {
     float rstd[kRb];
     if (a.normalize) {
@@ -330,34 +424,25 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * threads + lane) * 8;
-      const bool on = col < d;
-      float w[8];
-      if (a.normalize) weights(a.w_post, a.offset, col, on, w);
+      float wv[8];
+      weights(wo[k], a.normalize && a.w_post, a.normalize ? a.offset : 0.f, wv);
 #pragma unroll
       for (int r = 0; r < kRb; ++r) {
-        const size_t row = r0 + r;
-        const bool here = on && r0 + r < a.S;
-        float v[8], base[8];
+        float v[8], base[8], gv[8];
         o[r][k].get(v);
-        if (a.codes_o) {
-          const Packed p = pack_eight(v);
-          if (here) store_packed(p, a.codes_o, a.exps_o, row, d, col);
-        }
+        if (a.codes_o)
+          store_packed(pack_eight(v), rows_of(a.codes_o, first, rows, d), rows_of(a.exps_o, first, rows, blocks), at[r][k], block[r][k]);
         raw[r][k].get(base);
-        float g[8];
-        weights(a.gate ? a.gate + (size_t)((unsigned)(r0 + r) / (unsigned)a.gate_rows) * d : nullptr, 0.f, col, here, g);
+        weights(g[r][k], a.gate != nullptr, 0.f, gv);
+        const float q = a.normalize ? rstd[r] : 1.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float n = a.normalize ? v[i] * rstd[r] * w[i] : v[i];
-          x[r][k][i] = fmaf(a.scale * g[i], n, base[i]);
-        }
-        raw[r][k].set(x[r][k]);
-        if (here) raw[r][k].store(static_cast<T*>(a.Y) + row * d + col);
+        for (int i = 0; i < 8; ++i) x[r][k][i] = fmaf(a.scale * gv[i], v[i] * q * wv[i], base[i]);
+        Eight<T> y;
+        y.set(x[r][k]);
+        store_eight(y, rows_of(a.Y, first, rows, (int)sizeof(T) * d), at[r][k]);
         if (kPre && a.codes_y) {
-          raw[r][k].get(base);
-          const Packed p = pack_eight(base);
-          if (here) store_packed(p, a.codes_y, a.exps_y, row, d, col);
+          y.get(base);
+          store_packed(pack_eight(base), codes_y, exps_y, at[r][k], block[r][k]);
         }
       }
     }
@@ -366,13 +451,8 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
     for (int r = 0; r < kRb; ++r)
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
-        if (kRebuild) c[r][k].get(x[r][k]);
-        else raw[r][k].get(x[r][k]);
-        if (!kRebuild && a.codes_y) {
-          const int col = (k * threads + lane) * 8;
-          const Packed p = pack_eight(x[r][k]);
-          if (r0 + r < a.S && col < d) store_packed(p, a.codes_y, a.exps_y, r0 + r, d, col);
-        }
+        raw[r][k].get(x[r][k]);
+        if (!kRebuild && a.codes_y) store_packed(pack_eight(x[r][k]), codes_y, exps_y, at[r][k], block[r][k]);
       }
   }
   if (!kPre) return;
@@ -387,21 +467,18 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   }
   row_sums(rstd);
 #pragma unroll
-  for (int r = 0; r < kRb; ++r) rstd[r] = rsqrtf(fmaf(rstd[r], a.inv_d, a.eps));
-#pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    const int col = (k * threads + lane) * 8;
-    float w[8];
-    weights(a.w_pre, a.offset, col, col < d, w);
+    float wv[8];
+    weights(w[k], a.w_pre != nullptr, a.offset, wv);
 #pragma unroll
     for (int r = 0; r < kRb; ++r) {
-      if (r0 + r >= a.S || col >= d) continue;
+      const float q = rsqrtf(fmaf(rstd[r], a.inv_d, a.eps));
       float h[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = x[r][k][i] * rstd[r] * w[i];
+      for (int i = 0; i < 8; ++i) h[i] = x[r][k][i] * q * wv[i];
       Eight<__bf16> e;
       e.set(h);
-      e.store(a.H + (size_t)(r0 + r) * d + col);
+      store_eight(e, rows_of(a.H, first, rows, 2 * d), at[r][k]);
     }
   }
 }
@@ -420,57 +497,10 @@ struct NormBwd {
   float *part_pre, *part_post;     // [workgroups][d] each
   float offset, eps, scale, inv_d;
   int S, d, normalize;
-  int gate_rows;                   // without a gate S
+  int gate_rows, gates;            // without a gate S and 1
   int share;                       // workgroups that share a row of the gate (not kWhole)
   int rows;                        // that a team takes in turn
   Team team;
-};
-
-// Some rows of a tensor as a buffer: what lies behind them, and a tensor that is not there, reads as zeros and takes no
-// stores.  Without branches around loads and stores the compiler knows how many are under way, and waits for the ones it needs.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t from, int rows, int row_bytes) {
-  const char* const at = static_cast<const char*>(p) + from * row_bytes;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, p ? rows * row_bytes : 0, 0x00020000);
-}
-// Offset in entries of a lane that has no columns: behind those rows (less than 2^29 entries) in bytes of 1, 2 or 4.
-constexpr uint32_t kNoColumn = 1u << 29;
-// Rows whose loads are under way while one is summed up.
-template <class T> constexpr int rows_ahead(bool pre, bool res, int chunks) { return pre && !res && chunks == 1 && sizeof(T) == 2 ? 2 : 1; }
-
-constexpr int kNonTemporalAccess = 2;         // cache policy of buffer loads and stores
-
-template <int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
-  const uint32_t byte = at * (uint32_t)sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
-  } else {
-    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
-    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, kPolicy));
-  }
-}
-template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
-  const uint32_t byte = at * (uint32_t)sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, kNonTemporalAccess);
-  } else {
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, kNonTemporalAccess);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, kNonTemporalAccess);
-  }
-}
-
-// A row's eight entries: the tensor's, or those of its checkpoint.
-template <class T, bool kCheckpoint, int kPolicy> struct Source {
-  Eight<T> e;
-  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight<kPolicy>(e, rows, at); }
-  __device__ void get(float (&v)[8]) const { e.get(v); }
-};
-template <class T, int kPolicy> struct Source<T, true, kPolicy> {
-  EightCodes e;
-  __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
-    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, kPolicy));
-    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, kPolicy);
-  }
-  __device__ void get(float (&v)[8]) const { e.get(v); }
 };
 
 // dw_post and dgate of kN columns from t = sum of dY * N / w_post over the rows of a row of the gate (dw_post: if it is the
@@ -526,11 +556,16 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   float acc_pre[kNc][8] = {}, acc_group[kNc][8] = {}, acc_post[kNc][8] = {};
   float w[kNc][8], f[kNc][8];
   auto column = [&](int k) { return (k * threads + lane) * 8; };
-  auto load_f = [&](int k, int g, bool on) {
-    const int col = column(k);
-    weights(a.gate ? a.gate + (size_t)g * d : nullptr, 0.f, col, on && col < d, f[k]);
+  // The gate's rows of the workgroup's teams.
+  auto load_gate = [&](int k) {
+    Eight<__bf16> g;
+    load_eight<0>(g, rows_of(a.gate, group, max(0, min(kWhole ? teams : 1, a.gates - group)), 2 * d), column(k) < d ? (kWhole ? in_block * d : 0) + column(k) : kNoColumn);
+    return g;
+  };
+  auto set_f = [&](int k, const Eight<__bf16>& gate, const Eight<__bf16>& weight) {
     float wo[8];
-    weights(a.normalize ? a.w_post : nullptr, a.normalize ? a.offset : 0.f, col, col < d, wo);
+    weights(gate, a.gate != nullptr, 0.f, f[k]);
+    weights(weight, a.normalize && a.w_post, a.normalize ? a.offset : 0.f, wo);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
   };
@@ -563,11 +598,21 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     const bool on = column(k) < d;
     at[k] = on ? in_block * apart * d + column(k) : kNoColumn;
     block[k] = on ? in_block * apart * blocks + column(k) / 32 : kNoColumn;
-    if (kPre) weights(a.w_pre, a.offset, column(k), on, w[k]);
-    if (kRes && !kWhole) load_f(k, group, true);
   }
 #pragma unroll
   for (int slot = 0; slot < kAhead; ++slot) load(slot);
+  Eight<__bf16> w_raw[kNc], wo_raw[kNc], g_raw[kNc];
+#pragma unroll
+  for (int k = 0; k < kNc; ++k) {
+    if (kPre) w_raw[k] = load_weights(a.w_pre, d, column(k));
+    if (kRes) wo_raw[k] = load_weights(a.w_post, d, column(k));
+    if (kRes && !kWhole) g_raw[k] = load_gate(k);
+  }
+#pragma unroll
+  for (int k = 0; k < kNc; ++k) {
+    if (kPre) weights(w_raw[k], a.w_pre != nullptr, a.offset, w[k]);
+    if (kRes && !kWhole) set_f(k, g_raw[k], wo_raw[k]);
+  }
   auto one_row = [&](int slot) {
     float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
     float sums[kFirst];
@@ -575,7 +620,10 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     for (int i = 0; i < kFirst; ++i) sums[i] = 0.f;
     if (kWhole && in_group == 0) {
 #pragma unroll
-      for (int k = 0; k < kNc; ++k) load_f(k, group + in_block, row + (int64_t)in_block * apart < end);
+      for (int k = 0; k < kNc; ++k) {
+        g_raw[k] = load_gate(k);
+        set_f(k, g_raw[k], wo_raw[k]);
+      }
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
@@ -643,11 +691,13 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
           const int col = column(k);
           if (col >= d) continue;
           Eight<float> e;
-          float v[8];
+          float v[8], gv[8];
+          weights(wo_raw[k], a.normalize && a.w_post, a.normalize ? a.offset : 0.f, v);
+          weights(g_raw[k], true, 0.f, gv);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            acc_post[k][i] = fmaf(gate_factor(a, group + in_block, col + i), acc_group[k][i], acc_post[k][i]);
-            v[i] = post_weight(a, col + i) * acc_group[k][i];
+            acc_post[k][i] = fmaf(a.scale * gv[i], acc_group[k][i], acc_post[k][i]);
+            v[i] *= a.scale * acc_group[k][i];
             acc_group[k][i] = 0.f;
           }
           e.set(v);

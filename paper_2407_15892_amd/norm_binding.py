@@ -65,66 +65,86 @@ def _check(status: int) -> None:
         raise MstError(status, _load_lmhead_library().mst_strerror(status).decode())
 
 
+_BF16, _FP32, _INT8, _UINT8 = torch.bfloat16, torch.float32, torch.int8, torch.uint8
+
+# A short call on the GPU takes less time than its checks here would if they were written without care: one pass over
+# each tensor's attributes, texts only where something is refused.
+
+
+def _refuse(name, t, dtype, shape):
+    if t.dtype is not dtype:
+        raise MstError(BAD_ARGUMENT, f"{name}: {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise MstError(BAD_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise MstError(BAD_ARGUMENT, f"{name}: not contiguous (strides {t.stride()})")
+    raise MstError(NO_DEVICE, f"{name}: on {t.device}, not on the device of the other tensors")
+
+
 class _Tensors:
-    """The tensors of one call: each is checked for what the call expects, `ready` that they are all on the current GPU."""
+    """The tensors of one call: `at` checks each for what the call expects, `ready` that they are on the current GPU."""
+
+    __slots__ = ("S", "d", "shape", "stream_dtype", "stream_type", "device")
 
     def __init__(self, name: str, t):
-        """t: the [S, d] tensor that sets the sizes of the others."""
+        """t: the [S, d] tensor of the residual stream (or H) that sets the sizes, the type and the device of the others."""
         if t is None or t.dim() != 2:
             raise MstError(BAD_SHAPE, f"{name}: a tensor [S, d] is needed")
         self.shape = t.shape
         self.S, self.d = t.shape
-        self.devices = set()
+        self.stream_dtype = t.dtype
+        self.device = t.get_device()
+        self.stream_type = TYPE_BF16
+        if t.dtype is _FP32:
+            self.stream_type = TYPE_FP32
+        elif t.dtype is not _BF16:
+            raise MstError(BAD_ARGUMENT, f"{name}: {t.dtype}, expected {_BF16} or {_FP32}")
 
-    def take(self, name: str, t, dtypes, shape):
+    def at(self, name: str, t, dtype, shape):
         """Address of t (None: NULL)."""
         if t is None:
             return None
-        if t.dtype not in dtypes:
-            raise MstError(BAD_ARGUMENT, f"{name}: {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-        if t.shape != shape:
-            raise MstError(BAD_SHAPE, f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-        return self.address(name, t)
-
-    def address(self, name: str, t):
-        if not t.is_contiguous():
-            raise MstError(BAD_ARGUMENT, f"{name}: not contiguous (strides {t.stride()})")
-        self.devices.add(t.get_device())
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self.device:
+            _refuse(name, t, dtype, shape)
         return t.data_ptr()
 
-    def rows(self, name: str, t, *dtypes):
-        return self.take(name, t, dtypes, self.shape)
+    def stream_rows(self, name: str, t):
+        return self.at(name, t, self.stream_dtype, self.shape)
 
-    def weight(self, name: str, t, dtype=torch.bfloat16):
-        return self.take(name, t, (dtype,), (self.d,))
+    def rows(self, name: str, t):
+        return self.at(name, t, _BF16, self.shape)
 
-    def checkpoint(self, name: str, codes, exps):
-        return (self.take("codes" + name, codes, (torch.int8,), self.shape),
-                self.take("exps" + name, exps, (torch.uint8,), (self.S, -(-self.d // 32))))
+    def weight(self, name: str, t, dtype=_BF16):
+        return self.at(name, t, dtype, (self.d,))
 
-    def gate(self, name: str, t, gate_rows: int, dtype=torch.bfloat16):
-        if t is not None and gate_rows < 1:
+    def checkpoint(self, codes, exps, which: str = ""):
+        if codes is None and exps is None:
+            return None, None
+        return self.at("codes" + which, codes, _INT8, self.shape), self.at("exps" + which, exps, _UINT8, (self.S, (self.d + 31) // 32))
+
+    def gate(self, name: str, t, gate_rows: int, dtype=_BF16):
+        if t is None:
+            return None
+        if gate_rows < 1:
             raise MstError(BAD_ARGUMENT, f"{name}: gate_rows is {gate_rows}")
-        return self.take(name, t, (dtype,), (-(-self.S // max(gate_rows, 1)), self.d))
+        return self.at(name, t, dtype, (-(-self.S // gate_rows), self.d))
 
     def workspace(self, t):
         if t is None:
             return None, 0
-        return self.address("workspace", t), t.numel() * t.element_size()
+        if not t.is_contiguous() or t.get_device() != self.device:
+            _refuse("workspace", t, t.dtype, t.shape)
+        return t.data_ptr(), t.nbytes
 
     def ready(self, stream):
         """Handle of the stream to enqueue on."""
-        if self.devices != {torch.cuda.current_device() if torch.cuda.is_initialized() else -2}:
-            raise MstError(NO_DEVICE, f"tensors on devices {sorted(self.devices)} (-1: CPU), expected the current GPU alone")
-        return _stream_handle(stream)
+        if self.device < 0 or self.device != torch.cuda.current_device():
+            raise MstError(NO_DEVICE, f"tensors on {f'GPU {self.device}' if self.device >= 0 else 'the CPU'}, expected the current GPU")
+        return _raw_stream(self.device) if stream is None and _raw_stream else _stream_handle(stream)
 
 
-_BF16, _FP32 = torch.bfloat16, torch.float32
-_STREAM = (_BF16, _FP32)
-
-
-def _stream_type(t) -> int:
-    return TYPE_FP32 if t.dtype is _FP32 else TYPE_BF16
+# PyTorch's current stream as an integer (0: the default one), without a Stream object around it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def mst_norm_version() -> str:
@@ -149,30 +169,30 @@ def mst_norm_bwd_info(S: int, d: int, gate_rows: int = 0, prenorm: bool = True) 
 def mst_ckpt_pack(X, codes, exps, stream=None) -> None:
     """Enqueue the 8-bit checkpoint of X (bf16 or fp32 [S,d]): codes int8 [S,d], exps uint8 [S,ceil(d/32)]."""
     t = _Tensors("X", X)
-    x, (c, e) = t.rows("X", X, *_STREAM), t.checkpoint("", codes, exps)
-    _check(load_norm_library().mst_ckpt_pack(x, _stream_type(X), t.S, t.d, c, e, t.ready(stream)))
+    x, (c, e) = t.stream_rows("X", X), t.checkpoint(codes, exps)
+    _check(load_norm_library().mst_ckpt_pack(x, t.stream_type, t.S, t.d, c, e, t.ready(stream)))
 
 
 def mst_ckpt_unpack(codes, exps, X, stream=None) -> None:
     """Enqueue the tensor that a checkpoint stands for, into X (bf16 or fp32 [S,d]; the same values in either)."""
     t = _Tensors("X", X)
-    x, (c, e) = t.rows("X", X, *_STREAM), t.checkpoint("", codes, exps)
-    _check(load_norm_library().mst_ckpt_unpack(c, e, t.S, t.d, x, _stream_type(X), t.ready(stream)))
+    x, (c, e) = t.stream_rows("X", X), t.checkpoint(codes, exps)
+    _check(load_norm_library().mst_ckpt_unpack(c, e, t.S, t.d, x, t.stream_type, t.ready(stream)))
 
 
 def mst_prenorm_fwd(X, w_pre, H, eps: float, w_offset: float = 0.0, codes=None, exps=None, stream=None) -> None:
     """Enqueue the norm before a block.  X bf16 or fp32 [S,d], w_pre bf16 [d] or None (ones); H bf16 [S,d] is overwritten, and
     the checkpoint of X where codes and exps are given."""
     t = _Tensors("X", X)
-    x, w, h = t.rows("X", X, *_STREAM), t.weight("w_pre", w_pre, _BF16), t.rows("H", H, _BF16)
-    c, e = t.checkpoint("", codes, exps)
-    _check(load_norm_library().mst_prenorm_fwd(x, _stream_type(X), w, w_offset, eps, t.S, t.d, h, c, e, t.ready(stream)))
+    x, w, h = t.stream_rows("X", X), t.weight("w_pre", w_pre), t.rows("H", H)
+    c, e = t.checkpoint(codes, exps)
+    _check(load_norm_library().mst_prenorm_fwd(x, t.stream_type, w, w_offset, eps, t.S, t.d, h, c, e, t.ready(stream)))
 
 
 def mst_prenorm_rebuild(codes, exps, w_pre, H, eps: float, w_offset: float = 0.0, stream=None) -> None:
     """Enqueue H = norm of the tensor that a checkpoint stands for: a block's input again, for its backward pass."""
     t = _Tensors("H", H)
-    w, h, (c, e) = t.weight("w_pre", w_pre, _BF16), t.rows("H", H, _BF16), t.checkpoint("", codes, exps)
+    w, h, (c, e) = t.weight("w_pre", w_pre), t.rows("H", H), t.checkpoint(codes, exps)
     _check(load_norm_library().mst_prenorm_rebuild(c, e, w, w_offset, eps, t.S, t.d, h, t.ready(stream)))
 
 
@@ -181,11 +201,11 @@ def mst_prenorm_bwd(dH, w_pre, dX, dw_pre, workspace, eps: float, w_offset: floa
     """Enqueue the gradients of the norm before a block.  dH bf16 [S,d]; X (the type of dX) or its checkpoint; dres (the type of
     dX) or None: what reaches X around the block.  dX bf16 or fp32 [S,d] and dw_pre fp32 [d] (None with w_pre None) are overwritten."""
     t = _Tensors("dX", dX)
-    dx, kind = t.rows("dX", dX, *_STREAM), dX.dtype
-    dh, x, r = t.rows("dH", dH, _BF16), t.rows("X", X, kind), t.rows("dres", dres, kind)
-    w, dw, (c, e) = t.weight("w_pre", w_pre, _BF16), t.weight("dw_pre", dw_pre, _FP32), t.checkpoint("", codes, exps)
+    dx = t.stream_rows("dX", dX)
+    dh, x, r = t.rows("dH", dH), t.stream_rows("X", X), t.stream_rows("dres", dres)
+    w, dw, (c, e) = t.weight("w_pre", w_pre), t.weight("dw_pre", dw_pre, _FP32), t.checkpoint(codes, exps)
     ws, size = t.workspace(workspace)
-    _check(load_norm_library().mst_prenorm_bwd(dh, x, c, e, r, _stream_type(dX), w, w_offset, eps, t.S, t.d, ws, size, dx, dw,
+    _check(load_norm_library().mst_prenorm_bwd(dh, x, c, e, r, t.stream_type, w, w_offset, eps, t.S, t.d, ws, size, dx, dw,
                                                t.ready(stream)))
 
 
@@ -195,10 +215,10 @@ def mst_residual_fwd(O, X, Y, w=None, gate=None, gate_rows: int = 0, scale: floa
     (ones), gate bf16 [ceil(S/gate_rows),d] or None; Y (the type of X) is overwritten, and the checkpoint of O where codes and exps
     are given."""
     t = _Tensors("X", X)
-    x, kind = t.rows("X", X, *_STREAM), X.dtype
-    o, y, (c, e) = t.rows("O", O, _BF16), t.rows("Y", Y, kind), t.checkpoint("", codes, exps)
-    w_, g = t.weight("w", w, _BF16), t.gate("gate", gate, gate_rows, _BF16)
-    _check(load_norm_library().mst_residual_fwd(o, x, _stream_type(X), int(normalize), w_, w_offset, eps, g, gate_rows, scale, t.S, t.d, y, c, e,
+    x = t.stream_rows("X", X)
+    o, y, (c, e) = t.rows("O", O), t.stream_rows("Y", Y), t.checkpoint(codes, exps)
+    w_, g = t.weight("w", w), t.gate("gate", gate, gate_rows)
+    _check(load_norm_library().mst_residual_fwd(o, x, t.stream_type, int(normalize), w_, w_offset, eps, g, gate_rows, scale, t.S, t.d, y, c, e,
                                                 t.ready(stream)))
 
 
@@ -207,12 +227,12 @@ def mst_residual_bwd(dY, dO, workspace, w=None, dw=None, gate=None, gate_rows: i
     """Enqueue the gradients of the residual.  dY bf16 or fp32 [S,d]; O bf16 or its checkpoint (neither is needed without norm and
     gate).  dO bf16 [S,d], dw fp32 [d] (with w) and dgate fp32 (the shape of gate, with it) are overwritten."""
     t = _Tensors("dY", dY)
-    dy, do, o = t.rows("dY", dY, *_STREAM), t.rows("dO", dO, _BF16), t.rows("O", O, _BF16)
-    c, e = t.checkpoint("", codes, exps)
-    w_, dw_ = t.weight("w", w, _BF16), t.weight("dw", dw, _FP32)
-    g, dg = t.gate("gate", gate, gate_rows, _BF16), t.gate("dgate", dgate, gate_rows, _FP32)
+    dy, do, o = t.stream_rows("dY", dY), t.rows("dO", dO), t.rows("O", O)
+    c, e = t.checkpoint(codes, exps)
+    w_, dw_ = t.weight("w", w), t.weight("dw", dw, _FP32)
+    g, dg = t.gate("gate", gate, gate_rows), t.gate("dgate", dgate, gate_rows, _FP32)
     ws, size = t.workspace(workspace)
-    _check(load_norm_library().mst_residual_bwd(dy, _stream_type(dY), o, c, e, int(normalize), w_, w_offset, eps, g, gate_rows, scale, t.S, t.d,
+    _check(load_norm_library().mst_residual_bwd(dy, t.stream_type, o, c, e, int(normalize), w_, w_offset, eps, g, gate_rows, scale, t.S, t.d,
                                                 ws, size, do, dw_, dg, t.ready(stream)))
 
 
@@ -221,12 +241,12 @@ def mst_residual_prenorm_fwd(O, X, Y, H, w_pre, w_post=None, gate=None, gate_row
                              stream=None) -> None:
     """Enqueue mst_residual_fwd and, from its Y, mst_prenorm_fwd, in one pass."""
     t = _Tensors("X", X)
-    x, kind = t.rows("X", X, *_STREAM), X.dtype
-    o, y, h = t.rows("O", O, _BF16), t.rows("Y", Y, kind), t.rows("H", H, _BF16)
-    (co, eo), (cy, ey) = t.checkpoint("_o", codes_o, exps_o), t.checkpoint("_y", codes_y, exps_y)
-    wo, wp = t.weight("w_post", w_post, _BF16), t.weight("w_pre", w_pre, _BF16)
-    g = t.gate("gate", gate, gate_rows, _BF16)
-    _check(load_norm_library().mst_residual_prenorm_fwd(o, x, _stream_type(X), int(normalize), wo, g, gate_rows, scale, wp, w_offset, eps, t.S, t.d,
+    x = t.stream_rows("X", X)
+    o, y, h = t.rows("O", O), t.stream_rows("Y", Y), t.rows("H", H)
+    (co, eo), (cy, ey) = t.checkpoint(codes_o, exps_o, "_o"), t.checkpoint(codes_y, exps_y, "_y")
+    wo, wp = t.weight("w_post", w_post), t.weight("w_pre", w_pre)
+    g = t.gate("gate", gate, gate_rows)
+    _check(load_norm_library().mst_residual_prenorm_fwd(o, x, t.stream_type, int(normalize), wo, g, gate_rows, scale, wp, w_offset, eps, t.S, t.d,
                                                         y, h, co, eo, cy, ey, t.ready(stream)))
 
 
@@ -236,12 +256,12 @@ def mst_residual_prenorm_bwd(dH, dres, dY, dO, workspace, w_pre, dw_pre, w_post=
     """Enqueue mst_prenorm_bwd, whose dX is dY, and mst_residual_bwd of that dY, in one pass.  Y (the type of dY) and O (bf16):
     each itself or its checkpoint."""
     t = _Tensors("dY", dY)
-    dy, kind = t.rows("dY", dY, *_STREAM), dY.dtype
-    dh, r, y, o = t.rows("dH", dH, _BF16), t.rows("dres", dres, kind), t.rows("Y", Y, kind), t.rows("O", O, _BF16)
-    do, (co, eo), (cy, ey) = t.rows("dO", dO, _BF16), t.checkpoint("_o", codes_o, exps_o), t.checkpoint("_y", codes_y, exps_y)
-    wo, wp = t.weight("w_post", w_post, _BF16), t.weight("w_pre", w_pre, _BF16)
+    dy = t.stream_rows("dY", dY)
+    dh, r, y, o = t.rows("dH", dH), t.stream_rows("dres", dres), t.stream_rows("Y", Y), t.rows("O", O)
+    do, (co, eo), (cy, ey) = t.rows("dO", dO), t.checkpoint(codes_o, exps_o, "_o"), t.checkpoint(codes_y, exps_y, "_y")
+    wo, wp = t.weight("w_post", w_post), t.weight("w_pre", w_pre)
     dwo, dwp = t.weight("dw_post", dw_post, _FP32), t.weight("dw_pre", dw_pre, _FP32)
-    g, dg = t.gate("gate", gate, gate_rows, _BF16), t.gate("dgate", dgate, gate_rows, _FP32)
+    g, dg = t.gate("gate", gate, gate_rows), t.gate("dgate", dgate, gate_rows, _FP32)
     ws, size = t.workspace(workspace)
-    _check(load_norm_library().mst_residual_prenorm_bwd(dh, r, _stream_type(dY), y, cy, ey, o, co, eo, int(normalize), wo, g, gate_rows, scale,
+    _check(load_norm_library().mst_residual_prenorm_bwd(dh, r, t.stream_type, y, cy, ey, o, co, eo, int(normalize), wo, g, gate_rows, scale,
                                                         wp, w_offset, eps, t.S, t.d, ws, size, dy, do, dwp, dwo, dg, t.ready(stream)))
