@@ -299,8 +299,8 @@ template <int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight
   if constexpr (sizeof(T) == 2) {
     e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
   } else {
-    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
-    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, kPolicy));
+    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
+    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, 0));
   }
 }
 template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
@@ -708,10 +708,13 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     advance(row, in_group);
     if (kWhole && in_group == 0) group += gridDim.x * teams;
   };
-  for (int i_row = 0; i_row < a.rows; i_row += kAhead) {         // as often in every team, for the barriers; zeros behind the last row
+  // As many rows in every team, for the barriers; zeros behind the last one.
+  int i_row = 0;
+  for (; i_row + kAhead <= a.rows; i_row += kAhead) {
 #pragma unroll
     for (int slot = 0; slot < kAhead; ++slot) one_row(slot);
   }
+  if (kAhead > 1 && i_row < a.rows) one_row(0);
   // the teams' sums, then to the workspace, or where they belong if this is the only workgroup
   auto add_teams = [&](const float (&acc)[kNc][8], auto put) {
     if (teams == 1) {
@@ -728,6 +731,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     __syncthreads();
     for (int col = threadIdx.x; col < d; col += blockDim.x) {
       float sum[1] = {0.f};
+#pragma unroll 4
       for (int t = 0; t < teams; ++t) sum[0] += lds_columns[t * d + col];
       put(col, sum, std::integral_constant<int, 1>());
     }
@@ -746,6 +750,17 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     else add_teams(acc_group, store(a.part_post + (size_t)blockIdx.x * d));
   }
 }
+
+// Four weights as floats, ones where there are none.
+struct Four {
+  norm_f32x4 v;
+  __device__ void load(const __bf16* w, size_t at, float offset) {
+    norm_u32x2 u = {0x3f803f80u, 0x3f803f80u};
+    if (w) u = *reinterpret_cast<const norm_u32x2*>(w + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = offset + __uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+  }
+};
 
 // Sums of the workgroups' sums (n of them): blockIdx.y = 0 dw_pre; 1 dw_post, each times its row of the gate if the
 // workgroups have not done that (and the gradient of a single row of gates); from 2 on the gradients of several rows of gates, `share` sums
@@ -768,13 +783,20 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a,
     count = group < gates ? a.share : 0;
   }
   const bool weighted = blockIdx.y == 1 && gates > 1;
+  // what the sums are multiplied with, loaded beside them
+  const bool on = col < d;
+  Four w, g;
+  w.load(a.normalize ? a.w_post : nullptr, on ? col : 0, a.normalize ? a.offset : 0.f);
+  g.load(a.gate, (size_t)(blockIdx.y >= 2 ? min(group, gates - 1) : 0) * d + (on ? col : 0), 0.f);
   norm_f32x4 sum = {0, 0, 0, 0};
-  if (col < d) {
+  if (on) {
 #pragma unroll 4
     for (int p = slice % slices; p < count; p += slices) {
       norm_f32x4 v = *reinterpret_cast<const norm_f32x4*>(part + (size_t)(first + p) * d + col);
       if (weighted) {
-        for (int i = 0; i < 4; ++i) v[i] *= gate_factor(a, p / a.share, col + i);
+        Four of;
+        of.load(a.gate, (size_t)((unsigned)p / (unsigned)a.share) * d + col, 0.f);
+        v *= of.v * a.scale;
       }
       sum += v;
     }
@@ -793,15 +815,15 @@ __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a,
       for (int s = 1; s < slices / 8; ++s) sum += lds[slice / 8 + s][lane];
     }
   }
-  if (slice % slices || col >= d || count == 0) return;
-  float t[4];
-  for (int i = 0; i < 4; ++i) t[i] = sum[i];
-  if (blockIdx.y == 1 && !whole && !weighted) {
-    finish_post<4>(a, col, t);
-    return;
+  if (slice % slices || !on || count == 0) return;
+  auto put = [&](float* to, norm_f32x4 v) { *reinterpret_cast<norm_f32x4*>(to + col) = v; };
+  if (blockIdx.y == 0) put(a.dw_pre, sum);
+  else if (blockIdx.y >= 2) put(a.dgate + (size_t)group * d, sum * w.v * a.scale);
+  else if (whole || weighted) put(a.dw_post, sum);
+  else {
+    if (a.dw_post) put(a.dw_post, sum * g.v * a.scale);
+    if (one_gate) put(a.dgate, sum * w.v * a.scale);
   }
-  float* const to = blockIdx.y == 0 ? a.dw_pre : blockIdx.y == 1 ? a.dw_post : a.dgate + (size_t)group * d;
-  for (int i = 0; i < 4; ++i) to[col + i] = blockIdx.y < 2 ? t[i] : post_weight(a, col + i) * t[i];
 }
 
 }  // namespace mst
