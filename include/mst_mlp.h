@@ -116,6 +116,23 @@ mst_status mst_mlp_bwd(const void* X, const void* Wg, const void* Wu, const void
                        void* dX, float* dWg, float* dWu, float* dWd, void* stream);
 
 /*
+ * Backward from an 8-bit checkpoint (mst_norm.h) in place of X: a training program keeps 33 bytes for 32 entries of the residual
+ * stream instead of the block's input.  The rows of X are rebuilt in the workspace, group of rows by group of rows:
+ *   normalize != 0   X = the norm before the block of the checkpoint (mst_prenorm_rebuild; w_pre [d] bf16 or NULL, w_offset, eps)
+ *   normalize == 0   X = what the checkpoint stands for (w_pre NULL; eps is checked all the same)
+ * with the bits of mst_prenorm_rebuild or mst_ckpt_unpack and mst_mlp_bwd on their output.
+ *   codes [S, d] int8, 16-byte aligned;  exps [S, ceil(d / 32)] uint8;  d <= MST_NORM_MAX_D;  no output and no part of the workspace
+ *   may overlap codes, exps or w_pre
+ * mst_mlp_ckpt_workspace_bytes (host, pure): that of mst_mlp_bwd and the X of the largest group of rows.
+ */
+mst_status mst_mlp_ckpt_workspace_bytes(int64_t S, int64_t d, int64_t I, int32_t M, size_t* bytes);
+mst_status mst_mlp_bwd_ckpt(const int8_t* codes, const uint8_t* exps, int32_t normalize, const void* w_pre, float w_offset, float eps,
+                            const void* Wg, const void* Wu, const void* Wd, const void* dO,
+                            int64_t S, int64_t d, int64_t I, int32_t M,
+                            void* workspace, size_t workspace_bytes,
+                            void* dX, float* dWg, float* dWu, float* dWd, void* stream);
+
+/*
  * Which block tiles the launches of a group of `rows` rows take (host, pure; a test aid).  All give the same O and dX
  * bit for bit.  info[0..2] = gate/up (forward and backward), info[3..5] = down, info[6..8] = dA and info[9..11] = dX
  * where they have launches of their own (mst_mlp_da_in_gateup, mst_mlp_dx_tile), each as

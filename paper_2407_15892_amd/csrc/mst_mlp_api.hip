@@ -6,6 +6,7 @@
 #include "host_util.hpp"
 #include "launch_model.hpp"
 #include "mst_mlp_kernels.hpp"
+#include "norm_launch.hpp"
 
 #include <cmath>
 #include <mutex>
@@ -534,6 +535,91 @@ DwProblem dw_problem(const __bf16* G, int ldg, const __bf16* H, int ldh, int d, 
   return q;
 }
 
+// Room for the input of the largest group of rows, where the backward rebuilds it (dX can overlap no input's rows then).
+size_t x_slot(const Plan& p) {
+  const BackwardGroups groups(p, true);
+  return mst_host::align_up((size_t)std::min(std::max<int64_t>(groups.cap, p.C), p.S) * p.d * 2, 256);
+}
+
+// Algorithm 3 on checked arguments.  rows_of_x(first row, rows): where the block's input of these rows is, or has been put by
+// launches on the stream; x_range: the memory of it that the caller owns (nullptr: none that dX could overlap).
+template <class RowsOfX>
+mst_status mlp_backward(const Plan& p, RowsOfX rows_of_x, const void* x_range, const void* Wg, const void* Wu, const void* Wd, const void* dO,
+                        void* workspace, void* dX, float* dWg, float* dWu, float* dWd, hipStream_t st) {
+  const __bf16* Wgb = static_cast<const __bf16*>(Wg);
+  const __bf16* Wub = static_cast<const __bf16*>(Wu);
+  const __bf16* Wdb = static_cast<const __bf16*>(Wd);
+  const __bf16* dOb = static_cast<const __bf16*>(dO);
+  __bf16* dXb = static_cast<__bf16*>(dX);
+  char* ws = static_cast<char*>(workspace);
+  const int dI = (int)p.I, dd = (int)p.d;
+  const size_t x_bytes = (size_t)p.S * p.d * 2, w_bytes = (size_t)p.I * p.d * 2;
+  const bool dx_is_free = !(x_range && overlap(dX, x_bytes, x_range, x_bytes)) && !overlap(dX, x_bytes, dO, x_bytes) && !overlap(dX, x_bytes, Wg, w_bytes) &&
+                          !overlap(dX, x_bytes, Wu, w_bytes) && !overlap(dX, x_bytes, Wd, w_bytes);
+  const BackwardGroups groups(p, dx_is_free);
+  const DwChoice dw = dw_choice(std::min(groups.cap, p.S), p.d, p.I);
+
+  // Algorithm 3: loop over groups of rows, likewise; their dX lands in its row range, the weight gradients accumulate
+  for (int64_t r0 = 0; r0 < p.S;) {
+    int in_dx = 0;
+    const int rows = (int)groups.next(p.S - r0, &in_dx);
+    __bf16* buf[3];                                             // dA, then dG in place; dU; A
+    for (int k = 0; k < 3; ++k)
+      buf[k] = k < in_dx ? dXb + p.S * p.d - (k + 1) * (int64_t)rows * p.I
+                         : reinterpret_cast<__bf16*>(ws + (k - in_dx) * groups.slot(in_dx));
+    __bf16 *const bufG = buf[0], *const bufU = buf[1], *const bufA = buf[2];
+    const bool more = r0 + rows < p.S;
+    const __bf16* Xc = rows_of_x(r0, rows);
+    const __bf16* dOc = dOb + r0 * p.d;
+    const int acc = r0 > 0 ? 1 : 0;
+    const bool da_in_gateup = fuse_da(rows, p.d, p.I);
+    if (!da_in_gateup) {
+      Scope sc(st, MST_MLP_K_DA);
+      launch_nn(st, dOc, Wdb, nullptr, nullptr, rows, dI, dd, bufG);
+    }
+    {
+      Scope sc(st, MST_MLP_K_GATEUP_BWD);
+      if (da_in_gateup)
+        launch_gateup_small<Tile64Lone, true, true>(st, Xc, Wgb, Wub, rows, dd, dI, dI, bufA, bufG, bufU, DaProblem{dOc, Wdb});
+      else
+        launch_gateup<true>(st, Xc, Wgb, Wub, rows, dd, dI, bufA, bufG, bufU);
+    }
+    const DxKind dx = choose_dx(rows, p.d, p.I, acc != 0, dw);
+    if (dx == kDxOwn) {
+      Scope sc(st, MST_MLP_K_DX);
+      launch_nn(st, bufG, Wgb, bufU, Wub, rows, dd, dI, dXb + r0 * p.d);
+    }
+    {
+      Scope sc(st, MST_MLP_K_DW);
+      const int tile = dw.small ? Tile64::EA : kTile;
+      DwProblems ps;
+      ps.p[0] = dw_problem(bufG, dI, Xc, dd, dd, dI, dWg, tile, dw.even);     // dWg [I][d] (+)= dG^T X
+      ps.p[1] = dw_problem(bufU, dI, Xc, dd, dd, dI, dWu, tile, dw.even);     // dWu [I][d] (+)= dU^T X
+      ps.p[2] = dw_problem(dOc, dd, bufA, dI, dI, dd, dWd, tile, dw.even);    // dWd [d][I] (+)= dO^T A
+      const dim3 grid(ps.p[0].grid + ps.p[1].grid + ps.p[2].grid);
+      DxProblem x = {};
+      x.dG = bufG; x.Wg = Wgb; x.dU = bufU; x.Wu = Wub;
+      x.d = dd; x.I = dI; x.dX = dXb + r0 * p.d;
+      if (dx == kDx64 || dx == kDx32) {
+        (dx == kDx32 ? launch_dx_dw3_small<Tile32> : launch_dx_dw3_small<Tile64Lone>)(st, x, ps, rows, acc);
+      } else if (dx != kDxOwn) {
+        (dx == kDxHalf ? launch_dx_dw3<Tile16Half> : dx == kDxQuarter ? launch_dx_dw3<Tile16Quarter> : launch_dx_dw3<Tile16>)(st, x, ps, rows, dw.even, acc != 0, more ? 1 : 0);
+      } else if (dw.small) {
+        if (dw.lone)
+          hipLaunchKernelGGL(k_mlp_dw3_small<Tile64Lone>, grid, dim3(Tile64Lone::kThreads), Tile64Lone::kLds, st, ps, rows, acc);
+        else
+          hipLaunchKernelGGL(k_mlp_dw3_small<Tile64>, grid, dim3(Tile64::kThreads), Tile64::kLds, st, ps, rows, acc);
+      } else {
+        const auto kernel = dw.even ? (acc ? k_mlp_dw3<false, true> : k_mlp_dw3<true, true>)
+                                 : (acc ? k_mlp_dw3<false, false> : k_mlp_dw3<true, false>);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLdsBytes, st, ps, rows, more ? 1 : 0);
+      }
+    }
+    r0 += rows;
+  }
+  return check_launch();
+}
+
 }  // namespace
 
 extern "C" {
@@ -611,80 +697,61 @@ mst_status mst_mlp_bwd(const void* X, const void* Wg, const void* Wu, const void
       misaligned(dX, 16) || misaligned(dWg, 16) || misaligned(dWu, 16) || misaligned(dWd, 16) || misaligned(workspace, 256))
     return MST_ERR_ALIGNMENT;
   if ((s = prepare_device()) != MST_OK) return s;
-  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const __bf16* Xb = static_cast<const __bf16*>(X);
-  const __bf16* Wgb = static_cast<const __bf16*>(Wg);
-  const __bf16* Wub = static_cast<const __bf16*>(Wu);
-  const __bf16* Wdb = static_cast<const __bf16*>(Wd);
-  const __bf16* dOb = static_cast<const __bf16*>(dO);
-  __bf16* dXb = static_cast<__bf16*>(dX);
-  char* ws = static_cast<char*>(workspace);
-  const int dI = (int)p.I, dd = (int)p.d;
-  const size_t x_bytes = (size_t)S * d * 2, w_bytes = (size_t)I * d * 2;
-  const bool dx_is_free = !overlap(dX, x_bytes, X, x_bytes) && !overlap(dX, x_bytes, dO, x_bytes) && !overlap(dX, x_bytes, Wg, w_bytes) &&
-                          !overlap(dX, x_bytes, Wu, w_bytes) && !overlap(dX, x_bytes, Wd, w_bytes);
-  const BackwardGroups groups(p, dx_is_free);
-  const DwChoice dw = dw_choice(std::min(groups.cap, p.S), p.d, p.I);
+  const __bf16* const Xb = static_cast<const __bf16*>(X);
+  return mlp_backward(p, [&](int64_t r0, int) { return Xb + r0 * p.d; }, X, Wg, Wu, Wd, dO, workspace, dX, dWg, dWu, dWd,
+                      reinterpret_cast<hipStream_t>(stream));
+}
 
-  // Algorithm 3: loop over groups of rows, likewise; their dX lands in its row range, the weight gradients accumulate
-  for (int64_t r0 = 0; r0 < p.S;) {
-    int in_dx = 0;
-    const int rows = (int)groups.next(p.S - r0, &in_dx);
-    __bf16* buf[3];                                             // dA, then dG in place; dU; A
-    for (int k = 0; k < 3; ++k)
-      buf[k] = k < in_dx ? dXb + p.S * p.d - (k + 1) * (int64_t)rows * p.I
-                         : reinterpret_cast<__bf16*>(ws + (k - in_dx) * groups.slot(in_dx));
-    __bf16 *const bufG = buf[0], *const bufU = buf[1], *const bufA = buf[2];
-    const bool more = r0 + rows < p.S;
-    const __bf16* Xc = Xb + r0 * p.d;
-    const __bf16* dOc = dOb + r0 * p.d;
-    const int acc = r0 > 0 ? 1 : 0;
-    const bool da_in_gateup = fuse_da(rows, p.d, p.I);
-    if (!da_in_gateup) {
-      Scope sc(st, MST_MLP_K_DA);
-      launch_nn(st, dOc, Wdb, nullptr, nullptr, rows, dI, dd, bufG);
+mst_status mst_mlp_ckpt_workspace_bytes(int64_t S, int64_t d, int64_t I, int32_t M, size_t* bytes) {
+  Plan p;
+  mst_status s = make_plan(S, d, I, M, &p);
+  if (s != MST_OK) return s;
+  if (d > MST_NORM_MAX_D) return MST_ERR_BAD_SHAPE;
+  if (!bytes) return MST_ERR_NULL_POINTER;
+  *bytes = 3 * p.slot + x_slot(p);
+  return MST_OK;
+}
+
+mst_status mst_mlp_bwd_ckpt(const int8_t* codes, const uint8_t* exps, int32_t normalize, const void* w_pre, float w_offset, float eps,
+                            const void* Wg, const void* Wu, const void* Wd, const void* dO,
+                            int64_t S, int64_t d, int64_t I, int32_t M,
+                            void* workspace, size_t workspace_bytes,
+                            void* dX, float* dWg, float* dWu, float* dWd, void* stream) {
+  Plan p;
+  mst_status s = make_plan(S, d, I, M, &p);
+  if (s != MST_OK) return s;
+  if (d > MST_NORM_MAX_D) return MST_ERR_BAD_SHAPE;
+  if (!codes || !exps || !Wg || !Wu || !Wd || !dO || !dX || !dWg || !dWu || !dWd) return MST_ERR_NULL_POINTER;
+  if ((w_pre && !normalize) || !mst_norm::good_norm(eps, w_offset)) return MST_ERR_BAD_ARGUMENT;
+  if (!workspace || workspace_bytes < 3 * p.slot + x_slot(p)) return MST_ERR_WORKSPACE;
+  if (misaligned(codes, 16) || misaligned(w_pre, 16) || misaligned(Wg, 16) || misaligned(Wu, 16) || misaligned(Wd, 16) || misaligned(dO, 16) ||
+      misaligned(dX, 16) || misaligned(dWg, 16) || misaligned(dWu, 16) || misaligned(dWd, 16) || misaligned(workspace, 256))
+    return MST_ERR_ALIGNMENT;
+  const int64_t blocks = mst_norm::blocks_of_row(d);
+  const size_t w_bytes = (size_t)I * d * 4;
+  const struct { const void* at; size_t bytes; } outs[] = {{workspace, 3 * p.slot + x_slot(p)}, {dX, (size_t)S * d * 2}, {dWg, w_bytes}, {dWu, w_bytes}, {dWd, w_bytes}};
+  for (const auto& out : outs)                  // the checkpoint is read group of rows by group of rows, w_pre each time
+    if (overlap(out.at, out.bytes, codes, (size_t)S * d) || overlap(out.at, out.bytes, exps, (size_t)(S * blocks)) ||
+        (w_pre && overlap(out.at, out.bytes, w_pre, (size_t)d * 2)))
+      return MST_ERR_BAD_ARGUMENT;
+  if ((s = prepare_device()) != MST_OK) return s;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  __bf16* const X = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + 3 * p.slot);
+  auto rebuild = [&](int64_t r0, int rows) -> const __bf16* {
+    const int8_t* const c = codes + r0 * d;
+    const uint8_t* const e = exps + r0 * blocks;
+    if (!normalize) {
+      mst_norm::launch_unpack(c, e, rows, d, X, st);
+      return X;
     }
-    {
-      Scope sc(st, MST_MLP_K_GATEUP_BWD);
-      if (da_in_gateup)
-        launch_gateup_small<Tile64Lone, true, true>(st, Xc, Wgb, Wub, rows, dd, dI, dI, bufA, bufG, bufU, DaProblem{dOc, Wdb});
-      else
-        launch_gateup<true>(st, Xc, Wgb, Wub, rows, dd, dI, bufA, bufG, bufU);
-    }
-    const DxKind dx = choose_dx(rows, p.d, p.I, acc != 0, dw);
-    if (dx == kDxOwn) {
-      Scope sc(st, MST_MLP_K_DX);
-      launch_nn(st, bufG, Wgb, bufU, Wub, rows, dd, dI, dXb + r0 * p.d);
-    }
-    {
-      Scope sc(st, MST_MLP_K_DW);
-      const int tile = dw.small ? Tile64::EA : kTile;
-      DwProblems ps;
-      ps.p[0] = dw_problem(bufG, dI, Xc, dd, dd, dI, dWg, tile, dw.even);     // dWg [I][d] (+)= dG^T X
-      ps.p[1] = dw_problem(bufU, dI, Xc, dd, dd, dI, dWu, tile, dw.even);     // dWu [I][d] (+)= dU^T X
-      ps.p[2] = dw_problem(dOc, dd, bufA, dI, dI, dd, dWd, tile, dw.even);    // dWd [d][I] (+)= dO^T A
-      const dim3 grid(ps.p[0].grid + ps.p[1].grid + ps.p[2].grid);
-      DxProblem x = {};
-      x.dG = bufG; x.Wg = Wgb; x.dU = bufU; x.Wu = Wub;
-      x.d = dd; x.I = dI; x.dX = dXb + r0 * p.d;
-      if (dx == kDx64 || dx == kDx32) {
-        (dx == kDx32 ? launch_dx_dw3_small<Tile32> : launch_dx_dw3_small<Tile64Lone>)(st, x, ps, rows, acc);
-      } else if (dx != kDxOwn) {
-        (dx == kDxHalf ? launch_dx_dw3<Tile16Half> : dx == kDxQuarter ? launch_dx_dw3<Tile16Quarter> : launch_dx_dw3<Tile16>)(st, x, ps, rows, dw.even, acc != 0, more ? 1 : 0);
-      } else if (dw.small) {
-        if (dw.lone)
-          hipLaunchKernelGGL(k_mlp_dw3_small<Tile64Lone>, grid, dim3(Tile64Lone::kThreads), Tile64Lone::kLds, st, ps, rows, acc);
-        else
-          hipLaunchKernelGGL(k_mlp_dw3_small<Tile64>, grid, dim3(Tile64::kThreads), Tile64::kLds, st, ps, rows, acc);
-      } else {
-        const auto kernel = dw.even ? (acc ? k_mlp_dw3<false, true> : k_mlp_dw3<true, true>)
-                                 : (acc ? k_mlp_dw3<false, false> : k_mlp_dw3<true, false>);
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), kLdsBytes, st, ps, rows, more ? 1 : 0);
-      }
-    }
-    r0 += rows;
-  }
-  return check_launch();
+    mst::NormFwd a = {};
+    a.codes_x = c; a.exps_x = e; a.w_pre = static_cast<const __bf16*>(w_pre); a.H = X;
+    a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
+    a.S = rows; a.d = (int)d; a.gate_rows = rows; a.gates = 1;
+    (void)mst_norm::launch_fwd<__bf16, false, true, true>(a, st);      // reported by the check behind all launches
+    return X;
+  };
+  return mlp_backward(p, rebuild, nullptr, Wg, Wu, Wd, dO, workspace, dX, dWg, dWu, dWd, st);
 }
 
 mst_status mst_mlp_tile_info(int64_t rows, int64_t d, int64_t I, int64_t* info) {

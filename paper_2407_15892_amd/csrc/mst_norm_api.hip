@@ -1,7 +1,7 @@
 // Host side of the norm, residual and checkpoint calls: argument validation, workspace carving, launches.
 #include "../../include/mst_norm.h"
 #include "host_util.hpp"
-#include "mst_norm_kernels.hpp"
+#include "norm_launch.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -9,19 +9,15 @@
 namespace {
 
 using namespace mst;
+using namespace mst_norm;
 using mst_host::misaligned;
 
 constexpr int kNumCu = 256;
-constexpr int64_t kCacheBytes = 192 << 20;
-
-mst_status check_launch() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
 
 mst_status check_shape(int64_t S, int64_t d) {
   if (S < 1 || S >= (int64_t(1) << 30) || d < 8 || d % 8 != 0 || d > MST_NORM_MAX_D || S * d > (int64_t(1) << 36)) return MST_ERR_BAD_SHAPE;
   return MST_OK;
 }
-
-int64_t tail_blocks(int64_t d) { return (d + 31) / 32; }
 
 // The tensors of a call, to be checked in one go.
 struct Operands {
@@ -50,7 +46,6 @@ struct Operands {
 
 int type_bytes(int32_t type) { return type == MST_TYPE_FP32 ? 4 : 2; }
 bool good_type(int32_t type) { return type == MST_TYPE_BF16 || type == MST_TYPE_FP32; }
-bool good_norm(float eps, float offset) { return std::isfinite(eps) && eps >= 0x1p-126f && std::isfinite(offset); }
 
 // Gate and scale; rows of the gate in *rows (0 without one).
 mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t S, int64_t* rows) {
@@ -58,22 +53,6 @@ mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t 
   *rows = gate ? (S + std::min(gate_rows, S) - 1) / std::min(gate_rows, S) : 0;
   return MST_OK;
 }
-
-// How rows are held: chunks of eight columns per lane, and teams of lanes.  A workgroup has as many teams as fit 512 lanes.
-struct RowPlan {
-  int chunks, teams;
-  Team team;
-  explicit RowPlan(int64_t d) {
-    chunks = d <= 8 * 64 * kNormMaxWaves ? 1 : 2;
-    team.lanes = 8;
-    while (team.lanes < 64 && team.lanes * 8 < d) team.lanes *= 2;
-    team.waves = (int)((d + 8 * 64 * chunks - 1) / (8 * 64 * chunks));
-    teams = std::max(1, 512 / (team.lanes * team.waves));
-  }
-  int threads() const { return team.lanes * team.waves * teams; }
-};
-
-constexpr int fwd_rows(bool res, int chunks) { return chunks == 1 && !res ? 2 : 1; }      // of a team
 
 // How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate.
 struct BwdPlan {
@@ -103,28 +82,6 @@ size_t workspace_bytes(const BwdPlan& p, int64_t d) {      // dw_pre and dw_post
   return mst_host::align_up(p.groups > 1 ? 2 * (size_t)p.groups * d * 4 : 1, 256);
 }
 
-template <class T, bool kRes, bool kPre, bool kRebuild, int kPolicy, int kNc>
-mst_status launch_fwd_chunks(NormFwd a, const RowPlan& p, hipStream_t st) {
-  constexpr int kRb = fwd_rows(kRes, kNc);
-  const int64_t kRows = kRb * p.teams;              // of a workgroup
-  const int64_t most = (int64_t(1) << 31) / p.threads() * kRows;  // a launch has fewer than 2^32 lanes
-  a.team = p.team;
-  for (int64_t r = 0; r < a.S; r += most) {
-    a.row0 = (int)r;
-    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kPolicy, kNc, kRb>),
-                       dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)), dim3(p.threads()), 0, st, a);
-  }
-  return check_launch();
-}
-template <class T, bool kRes, bool kPre, bool kRebuild>
-mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
-  const RowPlan p(a.d);
-  const int64_t t = kRebuild ? 1 : sizeof(T), n = (int64_t)a.S * a.d;
-  const bool stream = n * (t + (kPre ? 2 : 0) + (kRes ? 2 + t : 0)) > kCacheBytes;
-  if (p.chunks == 2) return launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 2>(a, p, st);
-  return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
-}
-
 template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy>
 mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t st) {
   a.rows = p.rows;
@@ -145,7 +102,7 @@ mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t 
     hipLaunchKernelGGL(k_norm_reduce, dim3((a.d + kReduceCols - 1) / kReduceCols, (unsigned)(2 + gates)), dim3(kReduceThreads), 0, st, a,
                        (int)p.groups, (int)kWhole, slices);
   }
-  return check_launch();
+  return launched();
 }
 
 template <class T, bool kPre, bool kRes>
@@ -171,34 +128,6 @@ template <bool kPre, bool kRes>
 mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_rows, void* workspace, hipStream_t st) {
   return type == MST_TYPE_FP32 ? dispatch_bwd<float, kPre, kRes>(a, gate_rows, workspace, st)
                                : dispatch_bwd<__bf16, kPre, kRes>(a, gate_rows, workspace, st);
-}
-
-// slots of a checkpoint kernel's launch stay below 2^30: rows of one launch
-int64_t ckpt_rows(int64_t d) { return (int64_t(1) << 30) / (4 * tail_blocks(d)); }
-
-template <class T>
-void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
-  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
-  const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
-  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
-  for (int64_t r = 0, n; r < S; r += n) {
-    n = std::min(S - r, ckpt_rows(d));
-    const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL((stream ? k_ckpt_pack<T, true> : k_ckpt_pack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
-                       X + r * d, per_row, slots, (int)d, codes + r * d, exps + r * tail_blocks(d));
-  }
-}
-template <class T>
-void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
-  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
-  const FastDiv per_row((uint32_t)(4 * tail_blocks(d)));
-  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
-  for (int64_t r = 0, n; r < S; r += n) {
-    n = std::min(S - r, ckpt_rows(d));
-    const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL((stream ? k_ckpt_unpack<T, true> : k_ckpt_unpack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
-                       codes + r * d, exps + r * tail_blocks(d), per_row, slots, (int)d, X + r * d);
-  }
 }
 
 mst_status check_device() {
@@ -247,11 +176,11 @@ mst_status mst_ckpt_pack(const void* X, int32_t type, int64_t S, int64_t d, int8
   Operands ops;
   ops.add(X, S * d, type_bytes(type), false, true);
   ops.add(codes, S * d, 1, true, true);
-  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, true, false, 1);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
   if (type == MST_TYPE_FP32) launch_pack(static_cast<const float*>(X), S, d, codes, exps, as_stream(stream));
   else launch_pack(bf(X), S, d, codes, exps, as_stream(stream));
-  return check_launch();
+  return launched();
 }
 
 mst_status mst_ckpt_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, void* X, int32_t type, void* stream) {
@@ -262,11 +191,11 @@ mst_status mst_ckpt_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, 
   Operands ops;
   ops.add(X, S * d, type_bytes(type), true, true);
   ops.add(codes, S * d, 1, false, true);
-  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, false, false, 1);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
   if (type == MST_TYPE_FP32) launch_unpack(codes, exps, S, d, static_cast<float*>(X), as_stream(stream));
   else launch_unpack(codes, exps, S, d, static_cast<__bf16*>(X), as_stream(stream));
-  return check_launch();
+  return launched();
 }
 
 mst_status mst_prenorm_fwd(const void* X, int32_t stream_type, const void* w_pre, float w_offset, float eps,
@@ -280,7 +209,7 @@ mst_status mst_prenorm_fwd(const void* X, int32_t stream_type, const void* w_pre
   ops.add(w_pre, d, 2, false, false);
   ops.add(H, S * d, 2, true, true);
   ops.add(codes, S * d, 1, true, true);
-  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, true, false, 1);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
   NormFwd a = {};
   a.X = X; a.w_pre = bf(w_pre); a.H = static_cast<__bf16*>(H);
@@ -299,7 +228,7 @@ mst_status mst_prenorm_rebuild(const int8_t* codes, const uint8_t* exps, const v
   if (!good_norm(eps, w_offset)) return MST_ERR_BAD_ARGUMENT;
   Operands ops;
   ops.add(codes, S * d, 1, false, true);
-  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, false, false, 1);
   ops.add(w_pre, d, 2, false, false);
   ops.add(H, S * d, 2, true, true);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
@@ -325,7 +254,7 @@ mst_status mst_prenorm_bwd(const void* dH, const void* X, const int8_t* codes, c
   ops.add(dH, S * d, 2, false, true);
   ops.add(X, S * d, type_bytes(stream_type), false, true);
   ops.add(codes, S * d, 1, false, true);
-  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, false, false, 1);
   ops.add(dres, S * d, type_bytes(stream_type), false, true);
   ops.add(w_pre, d, 2, false, false);
   ops.add(workspace, (int64_t)need, 1, true, false, 256);
@@ -356,7 +285,7 @@ mst_status mst_residual_fwd(const void* O, const void* X, int32_t stream_type, i
   ops.add(gate, gate_groups * d, 2, false, false);
   ops.add(Y, S * d, type_bytes(stream_type), true, true);
   ops.add(codes, S * d, 1, true, true);
-  ops.add(exps, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, true, false, 1);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
   NormFwd a = {};
   a.X = X; a.O = bf(O); a.w_post = bf(w_post); a.gate = bf(gate); a.Y = Y;
@@ -389,7 +318,7 @@ mst_status mst_residual_bwd(const void* dY, int32_t stream_type, const void* O, 
   ops.add(dY, S * d, type_bytes(stream_type), false, true);
   ops.add(O, S * d, 2, false, true);
   ops.add(codes, S * d, 1, false, true);
-  ops.add(exps, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps, S * blocks_of_row(d), 1, false, false, 1);
   ops.add(w_post, d, 2, false, false);
   ops.add(gate, gate_groups * d, 2, false, false);
   ops.add(workspace, (int64_t)need, 1, true, false, 256);
@@ -426,9 +355,9 @@ mst_status mst_residual_prenorm_fwd(const void* O, const void* X, int32_t stream
   ops.add(Y, S * d, type_bytes(stream_type), true, true);
   ops.add(H, S * d, 2, true, true);
   ops.add(codes_o, S * d, 1, true, true);
-  ops.add(exps_o, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(exps_o, S * blocks_of_row(d), 1, true, false, 1);
   ops.add(codes_y, S * d, 1, true, true);
-  ops.add(exps_y, S * tail_blocks(d), 1, true, false, 1);
+  ops.add(exps_y, S * blocks_of_row(d), 1, true, false, 1);
   if ((s = ops.check()) != MST_OK || (s = check_device()) != MST_OK) return s;
   NormFwd a = {};
   a.X = X; a.O = bf(O); a.w_post = bf(w_post); a.w_pre = bf(w_pre); a.gate = bf(gate);
@@ -466,10 +395,10 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
   ops.add(dres, S * d, type_bytes(stream_type), false, true);
   ops.add(Y, S * d, type_bytes(stream_type), false, true);
   ops.add(codes_y, S * d, 1, false, true);
-  ops.add(exps_y, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps_y, S * blocks_of_row(d), 1, false, false, 1);
   ops.add(O, S * d, 2, false, true);
   ops.add(codes_o, S * d, 1, false, true);
-  ops.add(exps_o, S * tail_blocks(d), 1, false, false, 1);
+  ops.add(exps_o, S * blocks_of_row(d), 1, false, false, 1);
   ops.add(w_post, d, 2, false, false);
   ops.add(w_pre, d, 2, false, false);
   ops.add(gate, gate_groups * d, 2, false, false);

@@ -1,0 +1,89 @@
+// Host side of the launches that the norm library and the MLP library share: how rows are held, the forward kernels, the
+// checkpoint's kernels.
+#pragma once
+#include "../../include/mst_norm.h"
+#include "mst_norm_kernels.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace mst_norm {
+
+using namespace mst;
+
+// Tensors of a call that are more than the last-level cache holds beside what else is in it are read past the caches: 16384 x
+// 4096, us, pack (201 MB) 35.3 -> 32.9, norm's backward of 8192 x 4096 (236 MB) 47.8 -> 46.4; below, where a call finds
+// what was written just before it, it costs: 8192 x 4096 pack (100 MB) 15.7 -> 17.8, norm's forward (169 MB) 25.7 -> 30.2.
+constexpr int64_t kCacheBytes = 192 << 20;
+
+inline mst_status launched() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
+inline int64_t blocks_of_row(int64_t d) { return (d + 31) / 32; }
+inline bool good_norm(float eps, float offset) { return std::isfinite(eps) && eps >= 0x1p-126f && std::isfinite(offset); }
+
+// How rows are held: chunks of eight columns per lane, and teams of lanes.  A workgroup has as many teams as fit 512 lanes.
+struct RowPlan {
+  int chunks, teams;
+  Team team;
+  explicit RowPlan(int64_t d) {
+    chunks = d <= 8 * 64 * kNormMaxWaves ? 1 : 2;
+    team.lanes = 8;
+    while (team.lanes < 64 && team.lanes * 8 < d) team.lanes *= 2;
+    team.waves = (int)((d + 8 * 64 * chunks - 1) / (8 * 64 * chunks));
+    teams = std::max(1, 512 / (team.lanes * team.waves));
+  }
+  int threads() const { return team.lanes * team.waves * teams; }
+};
+
+constexpr int fwd_rows(bool res, int chunks) { return chunks == 1 && !res ? 2 : 1; }      // of a team
+
+template <class T, bool kRes, bool kPre, bool kRebuild, int kPolicy, int kNc>
+mst_status launch_fwd_chunks(NormFwd a, const RowPlan& p, hipStream_t st) {
+  constexpr int kRb = fwd_rows(kRes, kNc);
+  const int64_t kRows = kRb * p.teams;              // of a workgroup
+  const int64_t most = (int64_t(1) << 31) / p.threads() * kRows;  // a launch has fewer than 2^32 lanes
+  a.team = p.team;
+  for (int64_t r = 0; r < a.S; r += most) {
+    a.row0 = (int)r;
+    hipLaunchKernelGGL((k_norm_fwd<T, kRes, kPre, kRebuild, kPolicy, kNc, kRb>),
+                       dim3((unsigned)((std::min(most, a.S - r) + kRows - 1) / kRows)), dim3(p.threads()), 0, st, a);
+  }
+  return launched();
+}
+template <class T, bool kRes, bool kPre, bool kRebuild>
+mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
+  const RowPlan p(a.d);
+  const int64_t t = kRebuild ? 1 : sizeof(T), n = (int64_t)a.S * a.d;
+  const bool stream = n * (t + (kPre ? 2 : 0) + (kRes ? 2 + t : 0)) > kCacheBytes;
+  if (p.chunks == 2) return launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 2>(a, p, st);
+  return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
+}
+
+// slots of a checkpoint kernel's launch stay below 2^30: rows of one launch
+inline int64_t ckpt_rows(int64_t d) { return (int64_t(1) << 30) / (4 * blocks_of_row(d)); }
+
+template <class T>
+void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
+  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
+  const FastDiv per_row((uint32_t)(4 * blocks_of_row(d)));
+  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
+  for (int64_t r = 0, n; r < S; r += n) {
+    n = std::min(S - r, ckpt_rows(d));
+    const uint32_t slots = (uint32_t)n * per_row.d;
+    hipLaunchKernelGGL((stream ? k_ckpt_pack<T, true> : k_ckpt_pack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
+                       X + r * d, per_row, slots, (int)d, codes + r * d, exps + r * blocks_of_row(d));
+  }
+}
+template <class T>
+void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
+  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
+  const FastDiv per_row((uint32_t)(4 * blocks_of_row(d)));
+  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
+  for (int64_t r = 0, n; r < S; r += n) {
+    n = std::min(S - r, ckpt_rows(d));
+    const uint32_t slots = (uint32_t)n * per_row.d;
+    hipLaunchKernelGGL((stream ? k_ckpt_unpack<T, true> : k_ckpt_unpack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
+                       codes + r * d, exps + r * blocks_of_row(d), per_row, slots, (int)d, X + r * d);
+  }
+}
+
+}  // namespace mst_norm

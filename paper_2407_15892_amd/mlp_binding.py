@@ -12,6 +12,7 @@ import os
 
 from .binding import MST_OK, MstError, _ptr, _stream_handle
 from .binding import load_library as _load_lmhead_library
+from .norm_binding import BAD_ARGUMENT, _Tensors
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 MLP_LIB_PATH = os.path.join(HERE, "libmst_mlp.so")
@@ -46,6 +47,11 @@ def load_mlp_library() -> ctypes.CDLL:
     lib.mst_mlp_bwd.restype = c.c_int
     lib.mst_mlp_bwd.argtypes = [c.c_void_p] * 5 + [c.c_int64, c.c_int64, c.c_int64, c.c_int32,
                                                    c.c_void_p, c.c_size_t] + [c.c_void_p] * 5
+    lib.mst_mlp_ckpt_workspace_bytes.restype = c.c_int
+    lib.mst_mlp_ckpt_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int64, c.c_int32, c.POINTER(c.c_size_t)]
+    lib.mst_mlp_bwd_ckpt.restype = c.c_int
+    lib.mst_mlp_bwd_ckpt.argtypes = ([c.c_void_p, c.c_void_p, c.c_int32, c.c_void_p, c.c_float, c.c_float] + [c.c_void_p] * 4 +
+                                     [c.c_int64, c.c_int64, c.c_int64, c.c_int32, c.c_void_p, c.c_size_t] + [c.c_void_p] * 5)
     lib.mst_mlp_tile_info.restype = c.c_int
     lib.mst_mlp_tile_info.argtypes = [c.c_int64, c.c_int64, c.c_int64, c.POINTER(c.c_int64)]
     lib.mst_mlp_dx_tile.restype = c.c_int32
@@ -117,6 +123,32 @@ def mst_mlp_bwd(X, Wg, Wu, Wd, dO, M: int, workspace, dX, dWg, dWu, dWd, stream=
         _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(dO), S, d, I, M,
         _ptr(workspace), workspace.numel() * workspace.element_size(),
         _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd), _stream_handle(stream)))
+
+
+def mst_mlp_ckpt_workspace_bytes(S: int, d: int, I: int, M: int) -> int:
+    """Bytes of workspace of mst_mlp_bwd_ckpt."""
+    n = ctypes.c_size_t(0)
+    _check(load_mlp_library().mst_mlp_ckpt_workspace_bytes(S, d, I, M, ctypes.byref(n)))
+    return int(n.value)
+
+
+def mst_mlp_bwd_ckpt(codes, exps, w_pre, Wg, Wu, Wd, dO, M: int, workspace, dX, dWg, dWu, dWd, normalize: bool = True, eps: float = 1e-5,
+                     w_offset: float = 0.0, stream=None) -> None:
+    """Enqueue the backward pass from an 8-bit checkpoint (codes int8 [S,d], exps uint8 [S,ceil(d/32)]) of the residual stream, whose
+    norm (w_pre bf16 [d] or None) is the block's input, or of that input itself (normalize False)."""
+    t = _Tensors("dO", dO)
+    S, d = t.S, t.d
+    I = Wg.shape[0]
+    (c, e), w = t.checkpoint(codes, exps), t.weight("w_pre", w_pre)
+    up, down, fp32 = (I, d), (d, I), dWg.dtype
+    if t.stream_dtype is not Wg.dtype or str(fp32) != "torch.float32":
+        raise MstError(BAD_ARGUMENT, f"dO: {t.stream_dtype}, Wg: {Wg.dtype}, dWg: {fp32}; expected bfloat16, bfloat16 and float32")
+    g, u, dn = (t.at(n, x, t.stream_dtype, shape) for n, x, shape in (("Wg", Wg, up), ("Wu", Wu, up), ("Wd", Wd, down)))
+    dg, du, dd = (t.at(n, x, fp32, shape) for n, x, shape in (("dWg", dWg, up), ("dWu", dWu, up), ("dWd", dWd, down)))
+    do, dx = t.rows("dO", dO), t.rows("dX", dX)
+    ws, size = t.workspace(workspace)
+    _check(load_mlp_library().mst_mlp_bwd_ckpt(c, e, int(normalize), w, w_offset, eps, g, u, dn, do, S, d, I, M, ws, size, dx, dg, du, dd,
+                                               t.ready(stream)))
 
 
 MLP_TILES = ("256", "128", "128_lone", "64", "64_lone", "64_long", "32", "128x256")     # MST_MLP_TILE_*
