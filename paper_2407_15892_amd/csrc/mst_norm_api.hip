@@ -54,6 +54,8 @@ mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t 
   return MST_OK;
 }
 
+constexpr int kAloneRows = 2;
+
 // How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate.
 struct BwdPlan {
   RowPlan row;
@@ -69,6 +71,13 @@ struct BwdPlan {
       groups = std::min(most, (gates + row.teams - 1) / row.teams);
       share = 0;
       rows = (int)((gates + groups * row.teams - 1) / (groups * row.teams) * L);
+      return;
+    }
+    const int most_teams = 1024 / (row.team.lanes * row.team.waves);
+    if (gates == 1 && S <= kAloneRows * most_teams) {
+      row.teams = most_teams;
+      rows = (int)((S + most_teams - 1) / most_teams);
+      share = groups = 1;
       return;
     }
     const int64_t wanted = (most + gates - 1) / gates;
