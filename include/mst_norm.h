@@ -52,7 +52,7 @@
  *   - stream_type: type of the residual stream (X, Y, dres, dX, dY), MST_TYPE_BF16
  *     or MST_TYPE_FP32.  H, O, dH, dO, weights and gates are bf16, gradients of
  *     weights and gates fp32 (each fully overwritten).  Everything is computed
- *     in fp32 and rounded once.  Sums over rows have a fixed order that
+ *     in fp32 and rounded once; a row's sum of squares has to be a finite fp32 number.  Sums over rows have a fixed order that
  *     depends on S, d, the gate's rows and the call alone (no atomics:
  *     bit-identical across calls).
  *   - A weight pointer that may be NULL stands for ones: the norm then has the
@@ -61,7 +61,7 @@
  *     two is given (both of codes and exps, or neither).
  *   - Tensors are row-major without padding.  Requirements: 1 <= S < 2^30;
  *     8 <= d <= MST_NORM_MAX_D, d % 8 == 0, S * d <= 2^36; eps, scale and w_offset finite,
- *     eps >= 2^-126; gate_rows >= 1 with a gate (the gate then has
+ *     eps >= 2^-100; gate_rows >= 1 with a gate (the gate then has
  *     ceil(S / gate_rows) rows), 0 without; all tensors 16-byte
  *     aligned but exps (any), workspace 256-byte aligned.
  *   - An output may be the very memory of an input of S * d entries of the same

@@ -64,7 +64,8 @@ struct BwdPlan {
   int rows;                              // that a team takes in turn
   BwdPlan(int64_t S, int64_t d, int64_t gate_rows, bool pre) : row(d) {
     const int64_t L = gate_rows ? std::min(gate_rows, S) : S;
-    const int64_t most = kNumCu * std::max(1, (pre ? 512 : 1024) / row.threads());
+    const int lanes = (int)(row.teams * d / 8);                           // of a workgroup, that have columns
+    const int64_t most = kNumCu * std::max(1, pre ? (512 + lanes / 2) / lanes : 1024 / row.threads());
     gates = (S + L - 1) / L;
     whole = gates > 1 && (2 * gates >= most * row.teams || L < row.teams) && L * row.teams * d < (int64_t(1) << 29);
     if (whole) {

@@ -651,7 +651,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     if (kPre || a.normalize) first_sums(sums);
     float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
     if (kPre) {
-      const float q = rsqrtf(fmaf(sums[0], a.inv_d, a.eps)), c = -q * q * q * sums[1] * a.inv_d;
+      const float q = rsqrtf(fmaf(sums[0], a.inv_d, a.eps)), c = -(sums[1] * a.inv_d * q) * q * q;      // q^3 alone leaves the range
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
 #pragma unroll
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     if (kRes) {
       if (kPre && a.normalize) second_sum(post);
       const float q = a.normalize ? rsqrtf(fmaf(sums[kPre ? 2 : 0], a.inv_d, a.eps)) : 1.f;
-      const float c = a.normalize ? -q * q * q * post[0] * a.inv_d : 0.f;
+      const float c = a.normalize ? -(post[0] * a.inv_d * q) * q * q : 0.f;
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
         float out[8];

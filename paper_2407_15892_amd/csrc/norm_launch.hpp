@@ -18,7 +18,7 @@ constexpr int64_t kCacheBytes = 192 << 20;
 
 inline mst_status launched() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
 inline int64_t blocks_of_row(int64_t d) { return (d + 31) / 32; }
-inline bool good_norm(float eps, float offset) { return std::isfinite(eps) && eps >= 0x1p-126f && std::isfinite(offset); }
+inline bool good_norm(float eps, float offset) { return std::isfinite(eps) && eps >= 0x1p-100f && std::isfinite(offset); }
 
 // How rows are held: chunks of eight columns per lane, and teams of lanes.  A workgroup has as many teams as fit 512 lanes.
 struct RowPlan {

@@ -140,6 +140,8 @@ class _Tensors:
         """Handle of the stream to enqueue on."""
         if self.device < 0 or self.device != torch.cuda.current_device():
             raise MstError(NO_DEVICE, f"tensors on {f'GPU {self.device}' if self.device >= 0 else 'the CPU'}, expected the current GPU")
+        if stream is not None and stream.device.index != self.device:
+            raise MstError(NO_DEVICE, f"stream of {stream.device}, tensors on GPU {self.device}")
         return _raw_stream(self.device) if stream is None and _raw_stream else _stream_handle(stream)
 
 

@@ -240,9 +240,33 @@ def test_rows_of_zeros_and_a_tiny_eps(mst):
     c.y[3] = rounded(np.random.default_rng(1).standard_normal(40))
     check_backward(c, "both", run_backward(mst, c, "both", True), True)
     H = c.rows(torch.bfloat16)
-    mst.mst_prenorm_fwd(c.gpu("y"), None, H.t, 2.0 ** -126)
+    mst.mst_prenorm_fwd(c.gpu("y"), None, H.t, 2.0 ** -100)
     h = f64(H.check())
     assert (h[[0, 1, 2, 4, 5]] == 0).all() and np.isfinite(h).all()
+
+
+@pytest.mark.parametrize("stream", ["bf16", "fp32"])
+def test_rows_of_far_apart_sizes(mst, stream):
+    """Rows of 2^-50 to 2^50: their sums of squares fit, the third power of their root mean square does not."""
+    c = Case(41, 264, stream)
+    scale = 2.0 ** np.linspace(-50, 50, 41).round()[:, None]
+    c.x, c.y, c.o = c.x * scale, c.y * scale, c.o * scale
+    check_forward(c, "pre", run_forward(mst, c, "pre"))
+    for parts in ("pre", "res", "both"):
+        for from_checkpoint in (True, False):
+            check_backward(c, parts, run_backward(mst, c, parts, from_checkpoint), from_checkpoint)
+
+
+def test_gradients_of_rows_of_zeros_with_the_least_eps(mst):
+    """rstd is 2^50 there; what it is multiplied with is 0 or a gradient."""
+    import torch
+    c = Case(3, 40)
+    c.y[:] = 0
+    dX, dw, ws = c.rows(), Out((40,), torch.float32), c.workspace()
+    mst.mst_prenorm_bwd(c.gpu("dh"), c.gpu("w_pre"), dX.t, dw.t, ws.t, 2.0 ** -100, X=c.gpu("y"))
+    want = c.dh * c.w_pre * 2.0 ** 50
+    close(dX.check(), want, np.abs(want), ROW_OPS)
+    assert (f64(dw.check()) == 0).all()
 
 
 def test_outputs_in_place_of_inputs(mst):

@@ -136,7 +136,7 @@ def test_values_are_refused(mst, name):
     if "rebuild" not in name:
         assert call(lib, name, type=2) == ARGUMENT and call(lib, name, type=-1) == ARGUMENT
     if "ckpt" not in name:
-        for eps in (0.0, -1.0, nan, inf, 1e-40):
+        for eps in (0.0, -1.0, nan, inf, 1e-40, 2.0 ** -101):
             assert call(lib, name, eps=eps) == ARGUMENT, eps
         assert call(lib, name, offset=nan) == ARGUMENT
     if name in GATED:
