@@ -6,10 +6,11 @@
 //   k_norm_bwd                   their gradients; per workgroup sums over its rows for those of weights and gates
 //   k_norm_reduce                these sums over the workgroups, in fixed order
 //
-// All of them move data and compute little, so a row is read once: a workgroup holds its columns in registers (8 adjacent ones
-// per lane and chunk of 8 * threads: 16 bytes of bf16), sums over the row go through DPP and LDS, and what is needed
-// of the row is written from the registers.  Four adjacent lanes hold the 32 columns of a checkpoint's block, whose largest
-// magnitude two quad permutations find.
+// All of them move data and compute little, so a row is read once: a team of lanes holds it in registers, sums over the row go
+// through DPP and LDS, and what is needed of the row is written from the registers.  A lane has eight columns of each chunk of
+// the row: adjacent ones (16 bytes of bf16) with a bf16 stream, twice four half a chunk apart with a float32 one, so that a
+// wave's access to its 16 bytes per lane is whole cache lines either way (float32 unpack of 8192 x 4096, half lines 34.6 us, whole
+// ones 24.8).  Four or eight adjacent lanes hold the 32 columns of a checkpoint's block.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -28,10 +29,6 @@ typedef float norm_f32x2 __attribute__((ext_vector_type(2)));
 template <class T> struct Eight;
 template <> struct Eight<__bf16> {
   norm_u32x4 u = {0, 0, 0, 0};
-  __device__ void load(const __bf16* p) { u = *reinterpret_cast<const norm_u32x4*>(p); }
-  __device__ void store(__bf16* p) const { *reinterpret_cast<norm_u32x4*>(p) = u; }
-  __device__ void load_streamed(const __bf16* p) { u = __builtin_nontemporal_load(reinterpret_cast<const norm_u32x4*>(p)); }
-  __device__ void store_streamed(__bf16* p) const { __builtin_nontemporal_store(u, reinterpret_cast<norm_u32x4*>(p)); }
   __device__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -49,16 +46,6 @@ template <> struct Eight<__bf16> {
 };
 template <> struct Eight<float> {
   norm_f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-  __device__ void load(const float* p) {
-    a = *reinterpret_cast<const norm_f32x4*>(p);
-    b = *reinterpret_cast<const norm_f32x4*>(p + 4);
-  }
-  __device__ void store(float* p) const {
-    *reinterpret_cast<norm_f32x4*>(p) = a;
-    *reinterpret_cast<norm_f32x4*>(p + 4) = b;
-  }
-  __device__ void load_streamed(const float* p) { load(p); }            // halves of a line: not past the caches
-  __device__ void store_streamed(float* p) const { store(p); }
   __device__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
@@ -79,20 +66,14 @@ template <int kByte> __device__ __forceinline__ float signed_byte(unsigned u) {
   return f;
 }
 
-// Eight entries of a checkpoint.
+// Eight entries of a checkpoint, each four of them with the exponent of their block.
 struct EightCodes {
-  norm_u32x2 c = {0, 0};
-  unsigned e = 0;
-  template <bool kStream> __device__ void load(const int8_t* codes, const uint8_t* exp) {
-    const norm_u32x2* const p = reinterpret_cast<const norm_u32x2*>(codes);
-    c = kStream ? __builtin_nontemporal_load(p) : *p;
-    e = *exp;
-  }
+  unsigned c[2] = {0, 0}, e[2] = {0, 0};
   __device__ void get(float (&v)[8]) const {
-    // 2^(e - 127): of 0 a subnormal, of 255 NaN
-    const float scale = __uint_as_float(max(e << 23 | ((e + 1) >> 8) << 22, 0x00400000u));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      // 2^(e - 127): of 0 a subnormal, of 255 NaN
+      const float scale = __uint_as_float(max(e[i] << 23 | ((e[i] + 1) >> 8) << 22, 0x00400000u));
       v[4 * i] = signed_byte<0>(c[i]) * scale;
       v[4 * i + 1] = signed_byte<1>(c[i]) * scale;
       v[4 * i + 2] = signed_byte<2>(c[i]) * scale;
@@ -108,32 +89,28 @@ template <int kCtrl> __device__ __forceinline__ float dpp_f32(float x) { return 
 constexpr int kQuadSwap1 = 0xB1, kQuadSwap2 = 0x4E;                 // quad_perm [1 0 3 2], [2 3 0 1]
 constexpr int kHalfMirror = 0x141, kMirror = 0x140;                 // within 8 and 16 lanes
 
-// Codes of eight entries and the exponent byte of their block of 32, whose other entries are in the other lanes of the quad
-// (all four lanes call this; lanes behind the row's end hold zeros).  The least scale whose product with 127.5 is more than
+// Codes of kN entries and the exponent byte of their block of 32, whose other entries are in the 32 / kN lanes around (all of
+// them call this; lanes behind the row's end hold zeros).  The least scale whose product with 127.5 is more than
 // the largest magnitude m * 2^e: 2^(e - 6), or 2^(e - 5) from m = 127.5 / 64 = 1 + 127 / 128 on, where adding the last bit of
 // that mantissa carries into the exponent.  x / scale + 1.5 * 2^23 rounds to the nearest integer, ties to even, and has its
 // two's complement in the low byte.  Measured as integers magnitudes order NaN above infinity above all else.
-struct Packed { norm_u32x2 codes; unsigned exp; };
-__device__ __forceinline__ Packed pack_eight(const float (&v)[8]) {
+template <int kN> struct Packed { unsigned codes[kN / 4], exp; };
+template <int kN> __device__ __forceinline__ Packed<kN> pack(const float* v) {
   unsigned top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const unsigned m = __float_as_uint(v[i]) & 0x7fffffffu;
-    top = top > m ? top : m;
-  }
-  unsigned o = dpp_u32<kQuadSwap1>(top);
-  top = top > o ? top : o;
-  o = dpp_u32<kQuadSwap2>(top);
-  top = top > o ? top : o;
+  for (int i = 0; i < kN; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  top = max(top, dpp_u32<kQuadSwap1>(top));
+  top = max(top, dpp_u32<kQuadSwap2>(top));
+  if (kN == 4) top = max(top, dpp_u32<kHalfMirror>(top));
   const unsigned E = (top + 0x10000u) >> 23;
-  Packed p;
+  Packed<kN> p;
   p.exp = E >= 255 ? 255 : max(E, 6u) - 6;
   const float inverse = __uint_as_float((254u - p.exp) << 23);
-  unsigned b[8];
+  unsigned b[kN];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], inverse, 12582912.f));
+  for (int i = 0; i < kN; ++i) b[i] = __float_as_uint(fmaf(v[i], inverse, 12582912.f));
 #pragma unroll
-  for (int i = 0; i < 2; ++i)      // the low bytes of four words
+  for (int i = 0; i < kN / 4; ++i)      // the low bytes of four words
     p.codes[i] = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u) | __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x04000c0cu);
   return p;
 }
@@ -154,57 +131,83 @@ struct FastDiv {
 };
 
 constexpr int kCkptThreads = 256;
-template <class T> constexpr int kCkptEights = sizeof(T) == 2 ? 2 : 1;      // eights per lane, a workgroup's lanes apart
+constexpr int kCkptParts = 2;                                          // parts of 16 bytes per lane, a workgroup's lanes apart
+template <class T> constexpr int kCkptPart = 16 / sizeof(T);           // entries of one
 
-// One lane per eight entries; a row takes a whole number of quads, so that a quad is a block.
+// One lane per part; a row takes a whole number of blocks, whose 32 entries are in adjacent lanes.
 template <class T, bool kStream>
-__global__ __launch_bounds__(kCkptThreads) void k_ckpt_pack(const T* X, FastDiv per_row, uint32_t slots, int d, int8_t* codes, uint8_t* exps) {
-  constexpr int kEights = kCkptEights<T>;
-  Eight<T> x[kEights];
-  uint32_t n[kEights];
-  size_t at[kEights];
-  bool on[kEights];
+__global__ __launch_bounds__(kCkptThreads) void k_ckpt_pack(const T* X, FastDiv per_row, uint32_t parts, int d, int8_t* codes, uint8_t* exps) {
+  constexpr int kN = kCkptPart<T>;
+  norm_u32x4 x[kCkptParts];
+  uint32_t n[kCkptParts];
+  size_t at[kCkptParts];
+  bool on[kCkptParts];
 #pragma unroll
-  for (int i = 0; i < kEights; ++i) {
-    n[i] = (blockIdx.x * kEights + i) * kCkptThreads + threadIdx.x;
-    const uint32_t row = per_row(n[i] < slots ? n[i] : 0), in_row = n[i] - row * per_row.d;
-    on[i] = n[i] < slots && (int)in_row * 8 < d;
-    at[i] = (size_t)row * d + in_row * 8;
-    if (on[i]) kStream ? x[i].load_streamed(X + at[i]) : x[i].load(X + at[i]);
+  for (int i = 0; i < kCkptParts; ++i) {
+    n[i] = (blockIdx.x * kCkptParts + i) * kCkptThreads + threadIdx.x;
+    const uint32_t row = per_row(n[i] < parts ? n[i] : 0), in_row = n[i] - row * per_row.d;
+    on[i] = n[i] < parts && (int)in_row * kN < d;
+    at[i] = (size_t)row * d + in_row * kN;
+    const norm_u32x4* const p = reinterpret_cast<const norm_u32x4*>(X + at[i]);
+    x[i] = norm_u32x4{0, 0, 0, 0};
+    if (on[i]) x[i] = kStream ? __builtin_nontemporal_load(p) : *p;
   }
 #pragma unroll
-  for (int i = 0; i < kEights; ++i) {
-    float v[8];
-    x[i].get(v);
-    const Packed p = pack_eight(v);
+  for (int i = 0; i < kCkptParts; ++i) {
+    float v[kN];
+    if constexpr (kN == 8) {
+      Eight<__bf16> e;
+      e.u = x[i];
+      e.get(v);
+    } else {
+      for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(x[i][k]);
+    }
+    const Packed<kN> p = pack<kN>(v);
     if (!on[i]) continue;
-    __builtin_nontemporal_store(p.codes, reinterpret_cast<norm_u32x2*>(codes + at[i]));
-    if (threadIdx.x % 4 == 0) exps[n[i] >> 2] = (uint8_t)p.exp;
+    if constexpr (kN == 8) __builtin_nontemporal_store(norm_u32x2{p.codes[0], p.codes[1]}, reinterpret_cast<norm_u32x2*>(codes + at[i]));
+    else __builtin_nontemporal_store(p.codes[0], reinterpret_cast<unsigned*>(codes + at[i]));
+    if (threadIdx.x % (32 / kN) == 0) exps[n[i] / (32 / kN)] = (uint8_t)p.exp;
   }
 }
 
 template <class T, bool kStream>
-__global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* codes, const uint8_t* exps, FastDiv per_row, uint32_t slots, int d, T* X) {
-  constexpr int kEights = kCkptEights<T>;
-  EightCodes c[kEights];
-  size_t at[kEights];
-  bool on[kEights];
+__global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* codes, const uint8_t* exps, FastDiv per_row, uint32_t parts, int d, T* X) {
+  constexpr int kN = kCkptPart<T>;
+  EightCodes c[kCkptParts];
+  size_t at[kCkptParts];
+  bool on[kCkptParts];
 #pragma unroll
-  for (int i = 0; i < kEights; ++i) {
-    const uint32_t n = (blockIdx.x * kEights + i) * kCkptThreads + threadIdx.x;
-    const uint32_t row = per_row(n < slots ? n : 0), in_row = n - row * per_row.d;
-    on[i] = n < slots && (int)in_row * 8 < d;
-    at[i] = (size_t)row * d + in_row * 8;
-    if (on[i]) c[i].template load<kStream>(codes + at[i], exps + (n >> 2));
+  for (int i = 0; i < kCkptParts; ++i) {
+    const uint32_t n = (blockIdx.x * kCkptParts + i) * kCkptThreads + threadIdx.x;
+    const uint32_t row = per_row(n < parts ? n : 0), in_row = n - row * per_row.d;
+    on[i] = n < parts && (int)in_row * kN < d;
+    at[i] = (size_t)row * d + in_row * kN;
+    if (!on[i]) continue;
+    const unsigned* const p = reinterpret_cast<const unsigned*>(codes + at[i]);
+    if constexpr (kN == 8) {
+      const norm_u32x2* const q = reinterpret_cast<const norm_u32x2*>(p);
+      const norm_u32x2 u = kStream ? __builtin_nontemporal_load(q) : *q;
+      c[i].c[0] = u[0];
+      c[i].c[1] = u[1];
+    } else {
+      c[i].c[0] = kStream ? __builtin_nontemporal_load(p) : *p;
+    }
+    c[i].e[0] = c[i].e[1] = exps[n / (32 / kN)];
   }
 #pragma unroll
-  for (int i = 0; i < kEights; ++i) {
+  for (int i = 0; i < kCkptParts; ++i) {
     if (!on[i]) continue;
     float v[8];
     c[i].get(v);
-    Eight<T> x;
-    x.set(v);
-    x.store_streamed(X + at[i]);
+    norm_u32x4 x;
+    if constexpr (kN == 8) {
+      Eight<__bf16> e;
+      e.set(v);
+      x = e.u;
+    } else {
+      for (int k = 0; k < 4; ++k) x[k] = __float_as_uint(v[k]);
+    }
+    __builtin_nontemporal_store(x, reinterpret_cast<norm_u32x4*>(X + at[i]));
   }
 }
 
@@ -246,14 +249,15 @@ template <int kN> struct RowSums {
     add_dpp<kQuadSwap1>(v);
     add_dpp<kQuadSwap2>(v);
     add_dpp<kHalfMirror>(v);
-    if (team.lanes == 8) return;
-    add_dpp<kMirror>(v);
-    if (team.lanes == 16) return;
-    if (team.lanes == 32) {
+    if (__builtin_expect(team.lanes < 64, 0)) {
+      if (team.lanes == 8) return;
+      add_dpp<kMirror>(v);
+      if (team.lanes == 16) return;
 #pragma unroll
       for (int i = 0; i < kN; ++i) v[i] += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v[i]), 0x401f));   // lane ^ 16
       return;
     }
+    add_dpp<kMirror>(v);
 #pragma unroll
     for (int i = 0; i < kN; ++i) v[i] = (lane_of(v[i], 0) + lane_of(v[i], 16)) + (lane_of(v[i], 32) + lane_of(v[i], 48));
     if (team.waves == 1) return;
@@ -294,50 +298,98 @@ template <class T> constexpr int rows_ahead(bool pre, bool res, int chunks) { re
 constexpr int kNonTemporalAccess = 2;         // cache policy of buffer loads and stores
 constexpr int kStorePolicy = kNonTemporalAccess;
 
-template <int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
-  const uint32_t byte = at * (uint32_t)sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, kPolicy));
+// A lane's columns: entries 0..3 from column a on, entries 4..7 from b (kApart: half a chunk apart; else b = a + 4, and the access is
+// one of eight entries).  Also offsets of these entries, and of their blocks' exponents.
+struct Pair { uint32_t a, b; };
+template <bool kApart> __device__ __forceinline__ Pair columns(int chunk, int threads, int lane, int d) {
+  const uint32_t a = kApart ? (2 * chunk * threads + lane) * 4 : (chunk * threads + lane) * 8, b = a + (kApart ? 4 * threads : 4);
+  return {a < (uint32_t)d ? a : kNoColumn, b < (uint32_t)d ? b : kNoColumn};
+}
+__device__ __forceinline__ Pair in_row(Pair columns, uint32_t row_at) {
+  return {columns.a == kNoColumn ? kNoColumn : row_at + columns.a, columns.b == kNoColumn ? kNoColumn : row_at + columns.b};
+}
+__device__ __forceinline__ Pair blocks_in_row(Pair columns, uint32_t row_at) {
+  return {columns.a == kNoColumn ? kNoColumn : row_at + columns.a / 32, columns.b == kNoColumn ? kNoColumn : row_at + columns.b / 32};
+}
+
+template <bool kApart, int kPolicy, class T> __device__ __forceinline__ void load_eight(Eight<T>& e, __amdgpu_buffer_rsrc_t rows, Pair at) {
+  if constexpr (sizeof(T) == 4) {
+    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at.a * 4, 0, kPolicy));
+    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at.b * 4, 0, kPolicy));
+  } else if constexpr (kApart) {
+    const norm_u32x2 a = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at.a * 2, 0, kPolicy));
+    const norm_u32x2 b = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at.b * 2, 0, kPolicy));
+    e.u = norm_u32x4{a[0], a[1], b[0], b[1]};
   } else {
-    e.a = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte, 0, 0));
-    e.b = __builtin_bit_cast(norm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, byte + 16, 0, 0));
+    e.u = __builtin_bit_cast(norm_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at.a * 2, 0, kPolicy));
   }
 }
-template <class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, uint32_t at) {
-  const uint32_t byte = at * (uint32_t)sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, byte, 0, kStorePolicy);
+template <bool kApart, class T> __device__ __forceinline__ void store_eight(const Eight<T>& e, __amdgpu_buffer_rsrc_t rows, Pair at) {
+  if constexpr (sizeof(T) == 4) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, at.a * 4, 0, kStorePolicy);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, at.b * 4, 0, kStorePolicy);
+  } else if constexpr (kApart) {
+    __builtin_amdgcn_raw_buffer_store_b64(norm_u32x2{e.u[0], e.u[1]}, rows, at.a * 2, 0, kStorePolicy);
+    __builtin_amdgcn_raw_buffer_store_b64(norm_u32x2{e.u[2], e.u[3]}, rows, at.b * 2, 0, kStorePolicy);
   } else {
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.a), rows, byte, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(norm_u32x4, e.b), rows, byte + 16, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(e.u, rows, at.a * 2, 0, kStorePolicy);
   }
 }
 
 // A row's eight entries: the tensor's, or those of its checkpoint.
-template <class T, bool kCheckpoint, int kPolicy> struct Source {
+template <class T, bool kCheckpoint, bool kApart, int kPolicy> struct Source {
   Eight<T> e;
-  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, uint32_t at, uint32_t) { load_eight<kPolicy>(e, rows, at); }
+  __device__ void load(__amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t, Pair at, Pair) { load_eight<kApart, kPolicy>(e, rows, at); }
   __device__ void get(float (&v)[8]) const { e.get(v); }
 };
-template <class T, int kPolicy> struct Source<T, true, kPolicy> {
+template <class T, bool kApart, int kPolicy> struct Source<T, true, kApart, kPolicy> {
   EightCodes e;
-  __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
-    e.c = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, kPolicy));
-    e.e = __builtin_amdgcn_raw_buffer_load_b8(exps, block, 0, kPolicy);
+  __device__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, Pair at, Pair block) {
+    if constexpr (kApart) {
+      e.c[0] = __builtin_amdgcn_raw_buffer_load_b32(codes, at.a, 0, kPolicy);
+      e.c[1] = __builtin_amdgcn_raw_buffer_load_b32(codes, at.b, 0, kPolicy);
+      e.e[0] = __builtin_amdgcn_raw_buffer_load_b8(exps, block.a, 0, kPolicy);
+      e.e[1] = __builtin_amdgcn_raw_buffer_load_b8(exps, block.b, 0, kPolicy);
+    } else {
+      const norm_u32x2 u = __builtin_bit_cast(norm_u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes, at.a, 0, kPolicy));
+      e.c[0] = u[0];
+      e.c[1] = u[1];
+      e.e[0] = e.e[1] = __builtin_amdgcn_raw_buffer_load_b8(exps, block.a, 0, kPolicy);
+    }
   }
   __device__ void get(float (&v)[8]) const { e.get(v); }
 };
 
+// The checkpoint of eight entries.
+template <bool kApart> __device__ __forceinline__ void store_checkpoint(const float (&v)[8], __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, Pair at, Pair block) {
+  if constexpr (kApart) {
+    const Packed<4> a = pack<4>(v), b = pack<4>(v + 4);
+    __builtin_amdgcn_raw_buffer_store_b32(a.codes[0], codes, at.a, 0, kStorePolicy);
+    __builtin_amdgcn_raw_buffer_store_b32(b.codes[0], codes, at.b, 0, kStorePolicy);
+    __builtin_amdgcn_raw_buffer_store_b8((unsigned char)a.exp, exps, threadIdx.x % 8 ? kNoColumn : block.a, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b8((unsigned char)b.exp, exps, threadIdx.x % 8 ? kNoColumn : block.b, 0, 0);
+  } else {
+    const Packed<8> p = pack<8>(v);
+    __builtin_amdgcn_raw_buffer_store_b64(norm_u32x2{p.codes[0], p.codes[1]}, codes, at.a, 0, kStorePolicy);
+    __builtin_amdgcn_raw_buffer_store_b8((unsigned char)p.exp, exps, threadIdx.x % 4 ? kNoColumn : block.a, 0, 0);
+  }
+}
+
 // Eight weights (or gates); the buffer of ones that are not there is empty.
-__device__ __forceinline__ Eight<__bf16> load_weights(const __bf16* w, int d, int col) {
+template <bool kApart> __device__ __forceinline__ Eight<__bf16> load_weights(const __bf16* w, int d, Pair columns) {
   Eight<__bf16> e;
-  load_eight<0>(e, rows_of(w, 0, 1, 2 * d), col < d ? col : kNoColumn);
+  load_eight<kApart, 0>(e, rows_of(w, 0, 1, 2 * d), columns);
   return e;
 }
 __device__ __forceinline__ void weights(const Eight<__bf16>& e, bool there, float offset, float (&v)[8]) {
   e.get(v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = offset + (there ? v[i] : 1.f);
+}
+// Eight sums to a row of float32.
+__device__ __forceinline__ void store_sums(const float* v, float* to, Pair columns) {
+  if (columns.a != kNoColumn) *reinterpret_cast<norm_f32x4*>(to + columns.a) = norm_f32x4{v[0], v[1], v[2], v[3]};
+  if (columns.b != kNoColumn) *reinterpret_cast<norm_f32x4*>(to + columns.b) = norm_f32x4{v[4], v[5], v[6], v[7]};
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------------
@@ -359,23 +411,19 @@ struct NormFwd {
   Team team;
 };
 
-__device__ __forceinline__ void store_packed(const Packed& p, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, uint32_t at, uint32_t block) {
-  __builtin_amdgcn_raw_buffer_store_b64(p.codes, codes, at, 0, kStorePolicy);
-  __builtin_amdgcn_raw_buffer_store_b8((unsigned char)p.exp, exps, threadIdx.x % 4 ? kNoColumn : block, 0, 0);
-}
-
 // kRb rows per team, kNc chunks of 8 columns per lane.
 template <class T, bool kRes, bool kPre, bool kRebuild, int kPolicy, int kNc, int kRb>
 __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
   __shared__ float lds[2][kNormMaxWaves][kRb];
+  constexpr bool kApart = sizeof(T) == 4;
   RowSums<kRb> row_sums(lds, a.team);
   const int threads = a.team.threads(), lane = threadIdx.x % threads, teams = blockDim.x / threads, in_block = threadIdx.x / threads;
   const int d = a.d, blocks = (d + 31) / 32;
   const int first = a.row0 + (int)blockIdx.x * teams * kRb;
   const int rows = min(teams * kRb, a.S - first);        // of the workgroup
   const int first_gate = a.gates > 1 ? first / a.gate_rows : 0;
-  uint32_t at[kRb][kNc], block[kRb][kNc], gate_at[kRb][kNc];
-  Source<T, kRebuild, kPolicy> raw[kRb][kNc];
+  Pair at[kRb][kNc], block[kRb][kNc], gate_at[kRb][kNc];
+  Source<T, kRebuild, kApart, kPolicy> raw[kRb][kNc];
   Eight<__bf16> o[kRb][kNc], g[kRb][kNc], w[kNc], wo[kNc];
 #pragma unroll
   for (int r = 0; r < kRb; ++r) {
@@ -383,24 +431,24 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
     const int gate = a.gates > 1 ? (first + row - first_gate * a.gate_rows) / a.gate_rows : 0;
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
-      const int col = (k * threads + lane) * 8;
-      at[r][k] = col < d ? row * d + col : kNoColumn;
-      block[r][k] = col < d ? row * blocks + col / 32 : kNoColumn;
-      gate_at[r][k] = col < d ? gate * d + col : kNoColumn;
+      const Pair col = columns<kApart>(k, threads, lane, d);
+      at[r][k] = in_row(col, row * d);
+      block[r][k] = blocks_in_row(col, row * blocks);
+      gate_at[r][k] = in_row(col, gate * d);
       raw[r][k].load(kRebuild ? rows_of(a.codes_x, first, rows, d) : rows_of(a.X, first, rows, (int)sizeof(T) * d), rows_of(a.exps_x, first, rows, blocks),
                      at[r][k], block[r][k]);
-      if (kRes) load_eight<kPolicy>(o[r][k], rows_of(a.O, first, rows, 2 * d), at[r][k]);
+      if (kRes) load_eight<kApart, kPolicy>(o[r][k], rows_of(a.O, first, rows, 2 * d), at[r][k]);
     }
   }
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    const int col = (k * threads + lane) * 8;
+    const Pair col = columns<kApart>(k, threads, lane, d);
     if (kRes) {
-      wo[k] = load_weights(a.w_post, d, col);
+      wo[k] = load_weights<kApart>(a.w_post, d, col);
 #pragma unroll
-      for (int r = 0; r < kRb; ++r) load_eight<0>(g[r][k], rows_of(a.gate, first_gate, min(teams * kRb, a.gates - first_gate), 2 * d), gate_at[r][k]);
+      for (int r = 0; r < kRb; ++r) load_eight<kApart, 0>(g[r][k], rows_of(a.gate, first_gate, min(teams * kRb, a.gates - first_gate), 2 * d), gate_at[r][k]);
     }
-    if (kPre) w[k] = load_weights(a.w_pre, d, col);
+    if (kPre) w[k] = load_weights<kApart>(a.w_pre, d, col);
   }
   const __amdgpu_buffer_rsrc_t codes_y = rows_of(a.codes_y, first, rows, d), exps_y = rows_of(a.exps_y, first, rows, blocks);
   float x[kRb][kNc][8];
@@ -431,7 +479,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
         float v[8], base[8], gv[8];
         o[r][k].get(v);
         if (a.codes_o)
-          store_packed(pack_eight(v), rows_of(a.codes_o, first, rows, d), rows_of(a.exps_o, first, rows, blocks), at[r][k], block[r][k]);
+          store_checkpoint<kApart>(v, rows_of(a.codes_o, first, rows, d), rows_of(a.exps_o, first, rows, blocks), at[r][k], block[r][k]);
         raw[r][k].get(base);
         weights(g[r][k], a.gate != nullptr, 0.f, gv);
         const float q = a.normalize ? rstd[r] : 1.f;
@@ -439,10 +487,10 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
         for (int i = 0; i < 8; ++i) x[r][k][i] = fmaf(a.scale * gv[i], v[i] * q * wv[i], base[i]);
         Eight<T> y;
         y.set(x[r][k]);
-        store_eight(y, rows_of(a.Y, first, rows, (int)sizeof(T) * d), at[r][k]);
+        store_eight<kApart>(y, rows_of(a.Y, first, rows, (int)sizeof(T) * d), at[r][k]);
         if (kPre && a.codes_y) {
           y.get(base);
-          store_packed(pack_eight(base), codes_y, exps_y, at[r][k], block[r][k]);
+          store_checkpoint<kApart>(base, codes_y, exps_y, at[r][k], block[r][k]);
         }
       }
     }
@@ -452,7 +500,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
         raw[r][k].get(x[r][k]);
-        if (!kRebuild && a.codes_y) store_packed(pack_eight(x[r][k]), codes_y, exps_y, at[r][k], block[r][k]);
+        if (!kRebuild && a.codes_y) store_checkpoint<kApart>(x[r][k], codes_y, exps_y, at[r][k], block[r][k]);
       }
   }
   if (!kPre) return;
@@ -478,7 +526,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
       for (int i = 0; i < 8; ++i) h[i] = x[r][k][i] * q * wv[i];
       Eight<__bf16> e;
       e.set(h);
-      store_eight(e, rows_of(a.H, first, rows, 2 * d), at[r][k]);
+      store_eight<kApart>(e, rows_of(a.H, first, rows, 2 * d), at[r][k]);
     }
   }
 }
@@ -503,22 +551,6 @@ struct NormBwd {
   Team team;
 };
 
-// dw_post and dgate of kN columns from t = sum of dY * N / w_post over the rows of a row of the gate (dw_post: if it is the
-// only one, or there is no gate).
-__device__ __forceinline__ float post_weight(const NormBwd& a, int col) {
-  return a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[col] : 1.f) : 1.f);
-}
-__device__ __forceinline__ float gate_factor(const NormBwd& a, int group, int col) {
-  return a.scale * (a.gate ? (float)a.gate[(size_t)group * a.d + col] : 1.f);
-}
-template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, int col, const float* t) {
-#pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    if (a.dw_post) a.dw_post[col + i] = gate_factor(a, 0, col + i) * t[i];
-    if (a.dgate) a.dgate[col + i] = post_weight(a, col + i) * t[i];
-  }
-}
-
 // A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
 // for their columns.
 //   kWhole = false  `share` workgroups have the rows of one row of the gate (all rows without a gate), adjacent rows in
@@ -530,8 +562,9 @@ template <int kN> __device__ __forceinline__ void finish_post(const NormBwd& a, 
 template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
+  constexpr bool kApart = sizeof(T) == 4;
   __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
-  extern __shared__ float lds_columns[];
+  extern __shared__ norm_f32x4 lds_columns[];
   RowSums<kFirst> first_sums(lds1, a.team);
   RowSums<1> second_sum(lds2, a.team);
   const int d = a.d, blocks = (d + 31) / 32, threads = a.team.threads(), lane = threadIdx.x % threads;
@@ -555,11 +588,11 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   };
   float acc_pre[kNc][8] = {}, acc_group[kNc][8] = {}, acc_post[kNc][8] = {};
   float w[kNc][8], f[kNc][8];
-  auto column = [&](int k) { return (k * threads + lane) * 8; };
+  Pair col[kNc], at[kNc], block[kNc];
   // The gate's rows of the workgroup's teams.
   auto load_gate = [&](int k) {
     Eight<__bf16> g;
-    load_eight<0>(g, rows_of(a.gate, group, max(0, min(kWhole ? teams : 1, a.gates - group)), 2 * d), column(k) < d ? (kWhole ? in_block * d : 0) + column(k) : kNoColumn);
+    load_eight<kApart, 0>(g, rows_of(a.gate, group, max(0, min(kWhole ? teams : 1, a.gates - group)), 2 * d), in_row(col[k], kWhole ? in_block * d : 0));
     return g;
   };
   auto set_f = [&](int k, const Eight<__bf16>& gate, const Eight<__bf16>& weight) {
@@ -569,12 +602,11 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] *= a.scale * wo[i];
   };
-  uint32_t at[kNc], block[kNc];
   constexpr int kAhead = rows_ahead<T>(kPre, kRes, kNc);
   Eight<__bf16> dh_next[kAhead][kNc];
-  Source<T, kCkptX, kPolicy> x_next[kAhead][kNc];
+  Source<T, kCkptX, kApart, kPolicy> x_next[kAhead][kNc];
   Eight<T> dy_next[kAhead][kNc];
-  Source<__bf16, kCkptO, kPolicy> o_next[kAhead][kNc];
+  Source<__bf16, kCkptO, kApart, kPolicy> o_next[kAhead][kNc];
   auto rows_at = [&](int64_t r) { return (int)max((int64_t)0, min((int64_t)(teams - 1) * apart + 1, end - r)); };
   auto load = [&](int slot) {
     const int rows = rows_at(next);
@@ -582,11 +614,11 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
       if (kPre) {
-        load_eight<kPolicy>(dh_next[slot][k], rows_of(a.dH, next, rows, 2 * d), at[k]);
+        load_eight<kApart, kPolicy>(dh_next[slot][k], rows_of(a.dH, next, rows, 2 * d), at[k]);
         x_next[slot][k].load(kCkptX ? rows_of(a.codes_x, next, rows, d) : rows_of(a.X, next, rows, (int)sizeof(T) * d),
                        rows_of(a.exps_x, next, rows, blocks), at[k], block[k]);
       }
-      load_eight<kPolicy>(dy_next[slot][k], dy_rows, at[k]);
+      load_eight<kApart, kPolicy>(dy_next[slot][k], dy_rows, at[k]);
       if (kRes)
         o_next[slot][k].load(kCkptO ? rows_of(a.codes_o, next, rows, d) : rows_of(a.O, next, rows, 2 * d), rows_of(a.exps_o, next, rows, blocks),
                        at[k], block[k]);
@@ -595,18 +627,20 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   };
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    const bool on = column(k) < d;
-    at[k] = on ? in_block * apart * d + column(k) : kNoColumn;
-    block[k] = on ? in_block * apart * blocks + column(k) / 32 : kNoColumn;
+    col[k] = columns<kApart>(k, threads, lane, d);
+    at[k] = in_row(col[k], in_block * apart * d);
+    block[k] = blocks_in_row(col[k], in_block * apart * blocks);
   }
 #pragma unroll
   for (int slot = 0; slot < kAhead; ++slot) load(slot);
   Eight<__bf16> w_raw[kNc], wo_raw[kNc], g_raw[kNc];
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    if (kPre) w_raw[k] = load_weights(a.w_pre, d, column(k));
-    if (kRes) wo_raw[k] = load_weights(a.w_post, d, column(k));
-    if (kRes && !kWhole) g_raw[k] = load_gate(k);
+    if (kPre) w_raw[k] = load_weights<kApart>(a.w_pre, d, col[k]);
+    if (kRes && !kWhole) {
+      wo_raw[k] = load_weights<kApart>(a.w_post, d, col[k]);
+      g_raw[k] = load_gate(k);
+    }
   }
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
@@ -621,8 +655,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     if (kWhole && in_group == 0) {
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
-        g_raw[k] = load_gate(k);
-        set_f(k, g_raw[k], wo_raw[k]);
+        set_f(k, load_gate(k), load_weights<kApart>(a.w_post, d, col[k]));
       }
     }
 #pragma unroll
@@ -664,7 +697,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
         Eight<T> e;
         e.set(dy[k]);
-        store_eight(e, rows_of(a.dX, row, rows, (int)sizeof(T) * d), at[k]);
+        store_eight<kApart>(e, rows_of(a.dX, row, rows, (int)sizeof(T) * d), at[k]);
       }
     }
     if (kRes) {
@@ -682,26 +715,22 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
         Eight<__bf16> e;
         e.set(out);
-        store_eight(e, rows_of(a.dO, row, rows, 2 * d), at[k]);
+        store_eight<kApart>(e, rows_of(a.dO, row, rows, 2 * d), at[k]);
       }
       const int64_t mine = row + (int64_t)in_block * apart;
       if (kWhole && (in_group == a.gate_rows - 1 || mine == end - 1) && mine < end) {      // the last row of its row of the gate
 #pragma unroll
         for (int k = 0; k < kNc; ++k) {
-          const int col = column(k);
-          if (col >= d) continue;
-          Eight<float> e;
           float v[8], gv[8];
-          weights(wo_raw[k], a.normalize && a.w_post, a.normalize ? a.offset : 0.f, v);
-          weights(g_raw[k], true, 0.f, gv);
+          weights(load_weights<kApart>(a.w_post, d, col[k]), a.normalize && a.w_post, a.normalize ? a.offset : 0.f, v);      // again: registers are short
+          weights(load_gate(k), true, 0.f, gv);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             acc_post[k][i] = fmaf(a.scale * gv[i], acc_group[k][i], acc_post[k][i]);
             v[i] *= a.scale * acc_group[k][i];
             acc_group[k][i] = 0.f;
           }
-          e.set(v);
-          e.store(a.dgate + (size_t)(group + in_block) * d + col);
+          store_sums(v, a.dgate + (size_t)(group + in_block) * d, col[k]);
         }
       }
     }
@@ -715,39 +744,44 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     for (int slot = 0; slot < kAhead; ++slot) one_row(slot);
   }
   if (kAhead > 1 && i_row < a.rows) one_row(0);
-  // the teams' sums, then to the workspace, or where they belong if this is the only workgroup
-  auto add_teams = [&](const float (&acc)[kNc][8], auto put) {
+  // the teams' sums, then to the workspace, or where they belong if this is the only workgroup: each times factor(column)
+  auto put_sums = [&](const float (&acc)[kNc][8], float* to, auto factor) {
     if (teams == 1) {
 #pragma unroll
-      for (int k = 0; k < kNc; ++k)
-        if (column(k) < d) put(column(k), acc[k], std::integral_constant<int, 8>());
+      for (int k = 0; k < kNc; ++k) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t c = (i < 4 ? col[k].a : col[k].b) + i % 4;
+          v[i] = acc[k][i] * (c < (uint32_t)d ? factor(c) : 0.f);
+        }
+        store_sums(v, to, col[k]);
+      }
       return;
     }
     __syncthreads();
-    if (column(0) < d) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) lds_columns[in_block * d + column(0) + i] = acc[0][i];
-    }
+    if (col[0].a != kNoColumn) lds_columns[(in_block * d + col[0].a) / 4] = norm_f32x4{acc[0][0], acc[0][1], acc[0][2], acc[0][3]};
+    if (col[0].b != kNoColumn) lds_columns[(in_block * d + col[0].b) / 4] = norm_f32x4{acc[0][4], acc[0][5], acc[0][6], acc[0][7]};
     __syncthreads();
-    for (int col = threadIdx.x; col < d; col += blockDim.x) {
-      float sum[1] = {0.f};
+    for (int c = threadIdx.x; c < d; c += blockDim.x) {
+      float sum = 0.f;
 #pragma unroll 4
-      for (int t = 0; t < teams; ++t) sum[0] += lds_columns[t * d + col];
-      put(col, sum, std::integral_constant<int, 1>());
+      for (int t = 0; t < teams; ++t) sum += lds_columns[(t * d + c) / 4][c % 4];
+      to[c] = sum * factor(c);
     }
-  };
-  auto store = [&](float* to) {
-    return [=](int col, const float* v, auto n) {
-#pragma unroll
-      for (int i = 0; i < decltype(n)::value; ++i) to[col + i] = v[i];
-    };
   };
   const bool alone = gridDim.x == 1;
-  if (kPre && a.dw_pre) add_teams(acc_pre, store(alone ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d));
-  if (kRes && kWhole && a.dw_post) add_teams(acc_post, store(alone ? a.dw_post : a.part_post + (size_t)blockIdx.x * d));
+  auto one = [](int) { return 1.f; };
+  auto gate_factor = [&](int c) { return a.scale * (a.gate ? (float)a.gate[c] : 1.f); };
+  auto post_factor = [&](int c) { return a.scale * (a.normalize ? a.offset + (a.w_post ? (float)a.w_post[c] : 1.f) : 1.f); };
+  if (kPre && a.dw_pre) put_sums(acc_pre, alone ? a.dw_pre : a.part_pre + (size_t)blockIdx.x * d, one);
+  if (kRes && kWhole && a.dw_post) put_sums(acc_post, alone ? a.dw_post : a.part_post + (size_t)blockIdx.x * d, one);
   if (kRes && !kWhole && (a.dw_post || a.dgate)) {
-    if (alone) add_teams(acc_group, [&](int col, const float* v, auto n) { finish_post<decltype(n)::value>(a, col, v); });
-    else add_teams(acc_group, store(a.part_post + (size_t)blockIdx.x * d));
+    if (!alone) put_sums(acc_group, a.part_post + (size_t)blockIdx.x * d, one);
+    else {
+      if (a.dw_post) put_sums(acc_group, a.dw_post, gate_factor);
+      if (a.dgate) put_sums(acc_group, a.dgate, post_factor);
+    }
   }
 }
 

@@ -58,32 +58,28 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
 }
 
-// slots of a checkpoint kernel's launch stay below 2^30: rows of one launch
-inline int64_t ckpt_rows(int64_t d) { return (int64_t(1) << 30) / (4 * blocks_of_row(d)); }
-
-template <class T>
-void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
-  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
-  const FastDiv per_row((uint32_t)(4 * blocks_of_row(d)));
-  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
+// A checkpoint kernel's launches: parts of 16 bytes, fewer than 2^30 of them in one.
+template <class T, class Launch> void launch_ckpt(int64_t S, int64_t d, Launch launch) {
+  constexpr uint32_t kPer = kCkptThreads * kCkptParts;                // of a workgroup
+  const FastDiv per_row((uint32_t)(32 / kCkptPart<T> * blocks_of_row(d)));
+  const int64_t most = (int64_t(1) << 30) / per_row.d;
   for (int64_t r = 0, n; r < S; r += n) {
-    n = std::min(S - r, ckpt_rows(d));
-    const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL((stream ? k_ckpt_pack<T, true> : k_ckpt_pack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
-                       X + r * d, per_row, slots, (int)d, codes + r * d, exps + r * blocks_of_row(d));
+    n = std::min(S - r, most);
+    const uint32_t parts = (uint32_t)n * per_row.d;
+    launch(r, dim3((parts + kPer - 1) / kPer), per_row, parts);
   }
 }
-template <class T>
-void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
-  constexpr uint32_t kPer = kCkptThreads * kCkptEights<T>;
-  const FastDiv per_row((uint32_t)(4 * blocks_of_row(d)));
-  const bool stream = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes;
-  for (int64_t r = 0, n; r < S; r += n) {
-    n = std::min(S - r, ckpt_rows(d));
-    const uint32_t slots = (uint32_t)n * per_row.d;
-    hipLaunchKernelGGL((stream ? k_ckpt_unpack<T, true> : k_ckpt_unpack<T, false>), dim3((slots + kPer - 1) / kPer), dim3(kCkptThreads), 0, st,
-                       codes + r * d, exps + r * blocks_of_row(d), per_row, slots, (int)d, X + r * d);
-  }
+template <class T> void launch_pack(const T* X, int64_t S, int64_t d, int8_t* codes, uint8_t* exps, hipStream_t st) {
+  const auto kernel = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes ? k_ckpt_pack<T, true> : k_ckpt_pack<T, false>;
+  launch_ckpt<T>(S, d, [&](int64_t r, dim3 grid, FastDiv per_row, uint32_t parts) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kCkptThreads), 0, st, X + r * d, per_row, parts, (int)d, codes + r * d, exps + r * blocks_of_row(d));
+  });
+}
+template <class T> void launch_unpack(const int8_t* codes, const uint8_t* exps, int64_t S, int64_t d, T* X, hipStream_t st) {
+  const auto kernel = S * d * (int64_t)(sizeof(T) + 1) > kCacheBytes ? k_ckpt_unpack<T, true> : k_ckpt_unpack<T, false>;
+  launch_ckpt<T>(S, d, [&](int64_t r, dim3 grid, FastDiv per_row, uint32_t parts) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kCkptThreads), 0, st, codes + r * d, exps + r * blocks_of_row(d), per_row, parts, (int)d, X + r * d);
+  });
 }
 
 }  // namespace mst_norm
