@@ -375,6 +375,11 @@ template <bool kApart> __device__ __forceinline__ void store_checkpoint(const fl
   }
 }
 
+// Registers whose contents the compiler takes for new ones: what was derived from them before is derived again, not kept.
+__device__ __forceinline__ void renew(Eight<__bf16>& e) { asm volatile("" : "+v"(e.u)); }
+__device__ __forceinline__ void renew(Eight<float>& e) { asm volatile("" : "+v"(e.a), "+v"(e.b)); }
+__device__ __forceinline__ void renew(EightCodes& e) { asm volatile("" : "+v"(e.c[0]), "+v"(e.c[1]), "+v"(e.e[0]), "+v"(e.e[1])); }
+
 // Eight weights (or gates); the buffer of ones that are not there is empty.
 template <bool kApart> __device__ __forceinline__ Eight<__bf16> load_weights(const __bf16* w, int d, Pair columns) {
   Eight<__bf16> e;
@@ -552,7 +557,9 @@ struct NormBwd {
 };
 
 // A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
-// for their columns.
+// for their columns.  Of long rows (two chunks, d > 8192) with two norms or in float32 only what was loaded stays in registers, and
+// is converted for each use (kLean): with 16 waves a wave has 128 of them.  2048 x 12288, both norms: 169 us -> 121, float32 and
+// gated 267 -> 152, its norm alone 78 -> 60; bf16's norm alone 42 -> 45, and the residual's 31 -> 38, do not.
 //   kWhole = false  `share` workgroups have the rows of one row of the gate (all rows without a gate), adjacent rows in
 //                   adjacent teams: memory is passed through in a few streams.  Sums of dY * N, without the gate, to the workspace.
 //   kWhole = true   for many short rows of gates: a team has all rows of one, then those of another; it writes their gradient
@@ -562,7 +569,7 @@ struct NormBwd {
 template <class T, bool kPre, bool kRes, bool kWhole, bool kCkptX, bool kCkptO, int kPolicy, int kNc>
 __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   constexpr int kFirst = (kPre ? 2 : 0) + (kRes ? kPre ? 1 : 2 : 0);   // sums over a row that wait for nothing
-  constexpr bool kApart = sizeof(T) == 4;
+  constexpr bool kApart = sizeof(T) == 4, kLean = kNc > 1 && kPre && (kRes || kApart);
   __shared__ float lds1[2][kNormMaxWaves][kFirst], lds2[2][kNormMaxWaves][1];
   extern __shared__ norm_f32x4 lds_columns[];
   RowSums<kFirst> first_sums(lds1, a.team);
@@ -631,8 +638,10 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
     at[k] = in_row(col[k], in_block * apart * d);
     block[k] = blocks_in_row(col[k], in_block * apart * blocks);
   }
+  if (!kLean) {
 #pragma unroll
-  for (int slot = 0; slot < kAhead; ++slot) load(slot);
+    for (int slot = 0; slot < kAhead; ++slot) load(slot);
+  }
   Eight<__bf16> w_raw[kNc], wo_raw[kNc], g_raw[kNc];
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
@@ -644,24 +653,40 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   }
 #pragma unroll
   for (int k = 0; k < kNc; ++k) {
-    if (kPre) weights(w_raw[k], a.w_pre != nullptr, a.offset, w[k]);
-    if (kRes && !kWhole) set_f(k, g_raw[k], wo_raw[k]);
+    if (kPre && !kLean) weights(w_raw[k], a.w_pre != nullptr, a.offset, w[k]);
+    if (kRes && !kWhole && !kLean) set_f(k, g_raw[k], wo_raw[k]);
   }
+  auto again_w = [&](int k) {                 // kLean: before each use
+    if (!kLean) return;
+    renew(w_raw[k]);
+    weights(w_raw[k], a.w_pre != nullptr, a.offset, w[k]);
+  };
+  auto again_f = [&](int k) {
+    if (!kLean) return;
+    renew(g_raw[k]);
+    renew(wo_raw[k]);
+    set_f(k, g_raw[k], wo_raw[k]);
+  };
   auto one_row = [&](int slot) {
     float dh[kNc][8], x[kNc][8], dy[kNc][8], o[kNc][8];
     float sums[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; ++i) sums[i] = 0.f;
+    if (kLean) load(slot);
     if (kWhole && in_group == 0) {
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
-        set_f(k, load_gate(k), load_weights<kApart>(a.w_post, d, col[k]));
+        g_raw[k] = load_gate(k);
+        wo_raw[k] = load_weights<kApart>(a.w_post, d, col[k]);
+        if (!kLean) set_f(k, g_raw[k], wo_raw[k]);
       }
     }
 #pragma unroll
     for (int k = 0; k < kNc; ++k) {
+      if (kLean) __builtin_amdgcn_sched_barrier(0);
       dy_next[slot][k].get(dy[k]);
       if (kPre) {
+        again_w(k);
         x_next[slot][k].get(x[k]);
         dh_next[slot][k].get(dh[k]);
 #pragma unroll
@@ -672,6 +697,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       }
       if (kRes) {
         o_next[slot][k].get(o[k]);
+        if (!kPre) again_f(k);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPre ? 2 : 0] = fmaf(o[k][i], o[k][i], sums[kPre ? 2 : 0]);
@@ -679,7 +705,7 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
         }
       }
     }
-    load(slot);
+    if (!kLean) load(slot);
     const int rows = rows_at(row);
     if (kPre || a.normalize) first_sums(sums);
     float post[1] = {kPre ? 0.f : sums[1]};      // sum of b * O
@@ -687,6 +713,21 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       const float q = rsqrtf(fmaf(sums[0], a.inv_d, a.eps)), c = -(sums[1] * a.inv_d * q) * q * q;      // q^3 alone leaves the range
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
+        if (kLean) {
+          __builtin_amdgcn_sched_barrier(0);          // one chunk after the other
+          renew(dy_next[slot][k]);
+          renew(x_next[slot][k].e);
+          renew(dh_next[slot][k]);
+          dy_next[slot][k].get(dy[k]);
+          x_next[slot][k].get(x[k]);
+          dh_next[slot][k].get(dh[k]);
+          again_w(k);
+        }
+        if (kLean && kRes) {
+          renew(o_next[slot][k].e);
+          o_next[slot][k].get(o[k]);
+          again_f(k);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float u = dh[k][i] * q;
@@ -706,6 +747,16 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       const float c = a.normalize ? -(post[0] * a.inv_d * q) * q * q : 0.f;
 #pragma unroll
       for (int k = 0; k < kNc; ++k) {
+        if (kLean) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (!kPre) {
+            renew(dy_next[slot][k]);
+            dy_next[slot][k].get(dy[k]);
+          }
+          renew(o_next[slot][k].e);
+          o_next[slot][k].get(o[k]);
+          again_f(k);
+        }
         float out[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
