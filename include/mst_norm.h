@@ -45,30 +45,31 @@
  *
  * Conventions (where not said otherwise, those of mst_lmhead.h)
  *   - Every pointer is a DEVICE pointer owned by the caller.  The calls only
- *     enqueue kernels on `stream` (capturable into a HIP graph); they allocate
- *     nothing and keep nothing.  Nothing but the checkpoint is handed from a
- *     forward to a backward call.  A workspace must not be shared by calls
- *     (or replays of graphs) that may run at the same time.
+ *     enqueue kernels on `stream` (capturable into a HIP graph after one eager
+ *     call in the process); they allocate nothing and keep nothing.  Nothing
+ *     but the checkpoint is handed from a forward to a backward call.  A
+ *     workspace must not be shared by calls (or replays of graphs) that may run
+ *     at the same time.
  *   - stream_type: type of the residual stream (X, Y, dres, dX, dY), MST_TYPE_BF16
  *     or MST_TYPE_FP32.  H, O, dH, dO, weights and gates are bf16, gradients of
  *     weights and gates fp32 (each fully overwritten).  Everything is computed
- *     in fp32 and rounded once; a row's sum of squares has to be a finite fp32 number.  Sums over rows have a fixed order that
- *     depends on S, d, the gate's rows and the call alone (no atomics:
- *     bit-identical across calls).
+ *     in fp32 and rounded once; a row's sum of squares has to be a finite fp32
+ *     number.  Sums over rows have a fixed order that depends on S, d, the gate's
+ *     rows and the call alone (no atomics: bit-identical across calls).
  *   - A weight pointer that may be NULL stands for ones: the norm then has the
  *     factor w_offset + 1, and its gradient's pointer must be NULL too.
  *   - Where a backward call takes a tensor or its checkpoint, exactly one of the
  *     two is given (both of codes and exps, or neither).
  *   - Tensors are row-major without padding.  Requirements: 1 <= S < 2^30;
- *     8 <= d <= MST_NORM_MAX_D, d % 8 == 0, S * d <= 2^36; eps, scale and w_offset finite,
- *     eps >= 2^-100; gate_rows >= 1 with a gate (the gate then has
+ *     8 <= d <= MST_NORM_MAX_D, d % 8 == 0, S * d <= 2^36; eps, scale and
+ *     w_offset finite, eps >= 2^-100; gate_rows >= 1 with a gate (which has
  *     ceil(S / gate_rows) rows), 0 without; all tensors 16-byte
  *     aligned but exps (any), workspace 256-byte aligned.
  *   - An output may be the very memory of an input of S * d entries of the same
  *     size (Y of X, dX of dres, ...); no output may overlap anything otherwise.
- *   - Return value: MST_OK or a negative error code of mst_lmhead.h, found on the host
- *     before anything is launched; MST_ERR_BAD_ARGUMENT for values out of
- *     range, pointers that exclude or need each other, and overlaps.
+ *   - Return value: MST_OK or a negative error code of mst_lmhead.h, found on
+ *     the host before anything is launched; MST_ERR_BAD_ARGUMENT for values out
+ *     of range, pointers that exclude or need each other, and overlaps.
  */
 #ifndef MST_NORM_H
 #define MST_NORM_H

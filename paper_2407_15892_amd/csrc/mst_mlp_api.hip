@@ -737,6 +737,7 @@ mst_status mst_mlp_bwd_ckpt(const int8_t* codes, const uint8_t* exps, int32_t no
   if ((s = prepare_device()) != MST_OK) return s;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   __bf16* const X = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + 3 * p.slot);
+  mst_status rebuilt = MST_OK;                  // launch_fwd takes note of what the runtime refused, so that the check at the end would not
   auto rebuild = [&](int64_t r0, int rows) -> const __bf16* {
     const int8_t* const c = codes + r0 * d;
     const uint8_t* const e = exps + r0 * blocks;
@@ -748,10 +749,12 @@ mst_status mst_mlp_bwd_ckpt(const int8_t* codes, const uint8_t* exps, int32_t no
     a.codes_x = c; a.exps_x = e; a.w_pre = static_cast<const __bf16*>(w_pre); a.H = X;
     a.offset = w_offset; a.eps = eps; a.inv_d = 1.f / (float)d;
     a.S = rows; a.d = (int)d; a.gate_rows = rows; a.gates = 1;
-    (void)mst_norm::launch_fwd<__bf16, false, true, true>(a, st);      // reported by the check behind all launches
+    const mst_status one = mst_norm::launch_fwd<__bf16, false, true, true>(a, st);
+    if (one != MST_OK) rebuilt = one;
     return X;
   };
-  return mlp_backward(p, rebuild, nullptr, Wg, Wu, Wd, dO, workspace, dX, dWg, dWu, dWd, st);
+  s = mlp_backward(p, rebuild, nullptr, Wg, Wu, Wd, dO, workspace, dX, dWg, dWu, dWd, st);
+  return rebuilt != MST_OK ? rebuilt : s;
 }
 
 mst_status mst_mlp_tile_info(int64_t rows, int64_t d, int64_t I, int64_t* info) {

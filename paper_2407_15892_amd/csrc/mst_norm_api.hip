@@ -54,9 +54,18 @@ mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t 
   return MST_OK;
 }
 
+// Up to so many rows of each team that a workgroup has room for are left to one workgroup: no sums to join, one launch.  2 rows of
+// 4096, norm: 5.4 us, in workgroups of their own 6.6; 4 rows of a team 10.8.
 constexpr int kAloneRows = 2;
 
-// How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate.
+// How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate; pre: with the norm before a block.
+//   Workgroups: a compute unit is given teams whose lanes have 512 times eight columns (1024 in the residual's backward alone, which loads half
+//   as much), about 40 KB of loads under way.  More of them pass through more rows at a time and are slower for it: 32768 x 4096, us, with one
+//   and with two workgroups of 512 lanes: norm 160, 162 (155, 180 with two rows ahead), both norms 243, 263, residual 138, 118.
+//   Rows of the gate: whole ones to a team where there are as many as teams (half as many for the residual's backward), or where a row of the gate
+//   has fewer rows than a workgroup has teams; else `share` workgroups each.  Whole against shared, us, 8192 x 1024, both
+//   norms, 1 row of the gate for 8 rows: 27, 29, for 16: 37, 23; residual: for 8 18, 20, for 16 24, 17; 32768 x 256, both
+//   norms, for 8 28, 60.
 struct BwdPlan {
   RowPlan row;
   bool whole;                            // teams take whole rows of the gate
@@ -67,7 +76,7 @@ struct BwdPlan {
     const int lanes = (int)(row.teams * d / 8);                           // of a workgroup, that have columns
     const int64_t most = kNumCu * std::max(1, pre ? (512 + lanes / 2) / lanes : 1024 / row.threads());
     gates = (S + L - 1) / L;
-    whole = gates > 1 && (2 * gates >= most * row.teams || L < row.teams) && L * row.teams * d < (int64_t(1) << 29);
+    whole = gates > 1 && ((pre ? 1 : 2) * gates >= most * row.teams || L < row.teams) && L * row.teams * d < (int64_t(1) << 29);
     if (whole) {
       groups = std::min(most, (gates + row.teams - 1) / row.teams);
       share = 0;
