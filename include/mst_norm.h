@@ -162,8 +162,9 @@ mst_status mst_residual_prenorm_bwd(const void* dH, const void* dres, int32_t st
                                     float* dw_pre, float* dw_post, float* dgate, void* stream);
 
 /*
- * How a backward call goes over the rows (host, pure; a test aid; prenorm: 0 for mst_residual_bwd): info = {threads of a workgroup, teams of lanes in it that
- * hold a row each, rows that a team takes in turn, workgroups, 1 where a team takes whole rows of the gate}.
+ * How a backward call goes over the rows (host, pure; a test aid; prenorm: 0 for mst_residual_bwd): info = {threads of
+ * a workgroup, teams of lanes in it that hold a row each, rows that a team takes in turn, workgroups, 1 where a team takes
+ * whole rows of the gate}.
  */
 mst_status mst_norm_bwd_info(int64_t S, int64_t d, int64_t gate_rows, int32_t prenorm, int64_t* info);
 

@@ -109,7 +109,7 @@ mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t 
   a.part_pre = static_cast<float*>(workspace);
   a.part_post = a.part_pre + (size_t)p.groups * a.d;
   const dim3 grid((unsigned)p.groups), block(p.row.threads());
-  const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // at most 16 KB
+  const size_t lds = p.row.teams > 1 ? (size_t)p.row.teams * a.d * 4 : 0;      // 16 KB of 512 lanes, 32 of a lone workgroup
   if (p.row.chunks == 1)
     hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, kPolicy, 1>), grid, block, lds, st, a);
   else

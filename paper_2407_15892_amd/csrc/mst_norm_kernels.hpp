@@ -172,7 +172,8 @@ __global__ __launch_bounds__(kCkptThreads) void k_ckpt_pack(const T* X, FastDiv 
 }
 
 template <class T, bool kStream>
-__global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* codes, const uint8_t* exps, FastDiv per_row, uint32_t parts, int d, T* X) {
+__global__ __launch_bounds__(kCkptThreads) void k_ckpt_unpack(const int8_t* codes, const uint8_t* exps, FastDiv per_row, uint32_t parts, int d,
+                                                             T* X) {
   constexpr int kN = kCkptPart<T>;
   EightCodes c[kCkptParts];
   size_t at[kCkptParts];
@@ -365,7 +366,9 @@ template <class T, bool kApart, int kPolicy> struct Source<T, true, kApart, kPol
 };
 
 // The checkpoint of eight entries.
-template <bool kApart> __device__ __forceinline__ void store_checkpoint(const float (&v)[8], __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, Pair at, Pair block) {
+template <bool kApart>
+__device__ __forceinline__ void store_checkpoint(const float (&v)[8], __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t exps, Pair at,
+                                                 Pair block) {
   if constexpr (kApart) {
     const Packed<4> a = pack<4>(v), b = pack<4>(v + 4);
     __builtin_amdgcn_raw_buffer_store_b32(a.codes[0], codes, at.a, 0, kStorePolicy);
@@ -445,8 +448,8 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
       at[r][k] = in_row(col, row * d);
       block[r][k] = blocks_in_row(col, row * blocks);
       gate_at[r][k] = in_row(col, gate * d);
-      raw[r][k].load(kRebuild ? rows_of(a.codes_x, first, rows, d) : rows_of(a.X, first, rows, (int)sizeof(T) * d), rows_of(a.exps_x, first, rows, blocks),
-                     at[r][k], block[r][k]);
+      raw[r][k].load(kRebuild ? rows_of(a.codes_x, first, rows, d) : rows_of(a.X, first, rows, (int)sizeof(T) * d),
+                     rows_of(a.exps_x, first, rows, blocks), at[r][k], block[r][k]);
       if (kRes) load_eight<kApart, kPolicy>(o[r][k], rows_of(a.O, first, rows, 2 * d), at[r][k]);
     }
   }
@@ -456,7 +459,8 @@ __global__ __launch_bounds__(1024) void k_norm_fwd(const NormFwd a) {
     if (kRes) {
       wo[k] = load_weights<kApart>(a.w_post, d, col);
 #pragma unroll
-      for (int r = 0; r < kRb; ++r) load_eight<kApart, 0>(g[r][k], rows_of(a.gate, first_gate, min(teams * kRb, a.gates - first_gate), 2 * d), gate_at[r][k]);
+      for (int r = 0; r < kRb; ++r)
+        load_eight<kApart, 0>(g[r][k], rows_of(a.gate, first_gate, min(teams * kRb, a.gates - first_gate), 2 * d), gate_at[r][k]);
     }
     if (kPre) w[k] = load_weights<kApart>(a.w_pre, d, col);
   }
@@ -606,7 +610,8 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
   // The gate's rows of the workgroup's teams.
   auto load_gate = [&](int k) {
     Eight<__bf16> g;
-    load_eight<kApart, 0>(g, rows_of(a.gate, group, max(0, min(kWhole ? teams : 1, a.gates - group)), 2 * d), in_row(col[k], kWhole ? in_block * d : 0));
+    load_eight<kApart, 0>(g, rows_of(a.gate, group, max(0, min(kWhole ? teams : 1, a.gates - group)), 2 * d),
+                          in_row(col[k], kWhole ? in_block * d : 0));
     return g;
   };
   auto set_f = [&](int k, const Eight<__bf16>& gate, const Eight<__bf16>& weight) {
@@ -780,7 +785,8 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 #pragma unroll
         for (int k = 0; k < kNc; ++k) {
           float v[8], gv[8];
-          weights(load_weights<kApart>(a.w_post, d, col[k]), a.normalize && a.w_post, a.normalize ? a.offset : 0.f, v);      // again: registers are short
+          // again: registers are short
+          weights(load_weights<kApart>(a.w_post, d, col[k]), a.normalize && a.w_post, a.normalize ? a.offset : 0.f, v);
           weights(load_gate(k), true, 0.f, gv);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {

@@ -56,7 +56,8 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   const int64_t t = kRebuild ? 1 : sizeof(T), n = (int64_t)a.S * a.d;
   const bool stream = n * (t + (kPre ? 2 : 0) + (kRes ? 2 + t : 0)) > kCacheBytes;
   if (p.chunks == 2) return launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 2>(a, p, st);
-  return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st) : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
+  return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st)
+                : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
 }
 
 // A checkpoint kernel's launches: parts of 16 bytes, fewer than 2^30 of them in one.
