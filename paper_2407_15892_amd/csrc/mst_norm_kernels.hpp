@@ -773,8 +773,12 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float u = dy[k][i] * q;
-          out[i] = fmaf(o[k][i], c, u * f[k][i]);
+          out[i] = u * f[k][i];
           acc_group[k][i] = fmaf(u, o[k][i], acc_group[k][i]);
+        }
+        if (a.normalize) {              // without the norm dO does not depend on O: 0 times an infinity or a NaN is a NaN
+#pragma unroll
+          for (int i = 0; i < 8; ++i) out[i] = fmaf(o[k][i], c, out[i]);
         }
         Eight<__bf16> e;
         e.set(out);
