@@ -114,7 +114,7 @@ mst_status launch_bwd(NormBwd a, const BwdPlan& p, void* workspace, hipStream_t 
     hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, kPolicy, 1>), grid, block, lds, st, a);
   else
     hipLaunchKernelGGL((k_norm_bwd<T, kPre, kRes, kWhole, kCkptX, kCkptO, kPolicy, 2>), grid, block, lds, st, a);
-  if (p.groups > 1 && (a.dw_pre || a.dw_post || a.dgate)) {
+  if (p.groups > 1 && (a.dw_pre || a.dw_post || (a.dgate && !kWhole))) {      // teams of whole rows of the gate have written dgate
     int slices = 1;                                       // of the sums of a row of the gate
     while (slices < kReduceSlices && slices < p.share) slices *= 2;
     const int64_t per_block = kReduceSlices / slices, gates = a.dgate && !kWhole && p.gates > 1 ? (p.gates + per_block - 1) / per_block : 0;

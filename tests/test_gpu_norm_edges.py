@@ -58,3 +58,37 @@ def test_without_a_norm_dO_does_not_depend_on_O(mst, S, d, gate_rows, whole, str
     ops += column_ops(S, d, gate_rows, parts == "both") + ROW_OPS
     close(np.where(bad, 0, got), np.where(bad, 0, want["dgate"]), want["dgate_reach"], ops, "fp32")
     ws.check()
+
+
+def launches_of(call):
+    """Kernels that a call enqueues: the nodes of the HIP graph that it is captured into."""
+    import ctypes
+    import torch
+    call()                                      # eager once, as the header asks
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    n = ctypes.c_size_t(0)
+    status = ctypes.CDLL(None).hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(n))
+    assert status == 0
+    return n.value
+
+
+# whether teams take whole rows of the gate and write their gradients; workgroups; with a weight's gradient to sum up
+@pytest.mark.parametrize("S,gate_rows,whole,normalize,launches", [
+    (37, 1, True, False, 1), (37, 1, True, True, 2), (37, 10, False, False, 2), (37, 10, False, True, 2), (3, 1, True, True, 1), (3, 3, False, True, 1)])
+def test_sums_of_workgroups_are_launched_only_where_there_are_any(mst, S, gate_rows, whole, normalize, launches):
+    import torch
+    d, f32 = 264, torch.float32
+    info = mst.mst_norm_bwd_info(S, d, gate_rows, False)
+    assert info["whole"] == whole and (info["workgroups"] == 1) == (S == 3)
+    c = Case(S, d, gate_rows=gate_rows, normalize=normalize)
+    dO, dg, ws = c.rows(torch.bfloat16), Out(c.gate.shape, f32), c.workspace()
+    dw = Out((d,), f32).t if normalize else None
+    args = dict(dY=c.gpu("dres"), O=c.gpu("o"), w=c.gpu("w_post"), gate=c.gpu("gate"))
+    assert launches_of(lambda: mst.mst_residual_bwd(dO=dO.t, workspace=ws.t, dw=dw, dgate=dg.t, gate_rows=gate_rows, normalize=normalize,
+                                                    eps=EPS, **args)) == launches
+    torch.cuda.synchronize()
+    want = orc.residual_bwd(c.dres, c.o, normalize, c.w_post, 0.0, EPS, c.gate, gate_rows, 1.0)
+    close(dg.check(), want["dgate"], want["dgate_reach"], column_ops(S, d, gate_rows, False) + ROW_OPS, "fp32")
