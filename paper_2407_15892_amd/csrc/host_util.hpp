@@ -28,6 +28,13 @@ struct PerDeviceOnce {
   }
 };
 
+// Whether a device has so many compute units.  What is planned for a whole chip would be mis-tiled on a partition of one (fewer compute
+// units behind one HIP device).
+inline bool has_compute_units(int dev, int n) {
+  int cus = 0;
+  return hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus == n;
+}
+
 // Per-launch timing with HIP events.  `every` = n brackets every n-th launch of each kind (the first, the n + 1st, ...):
 // events between launches cost a few microseconds each on the stream, about half a percent of a step made of 100
 // GEMM launches when every launch carries them; `issued` counts all launches of a kind while timing is on.

@@ -570,12 +570,8 @@ struct Scope : mst_host::Scope {
 
 mst_host::PerDeviceOnce g_attr_once, g_shape_once;
 // The tile maps and the schedule's cost model are written for the whole chip: kNumCu compute units in kNumXcd
-// XCDs.  A partitioned device (fewer compute units behind one HIP device) would be mis-tiled, so it is refused.
-bool device_is_whole_chip(int dev) {
-  int cus = 0;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return false;
-  return cus == kNumCu;
-}
+// XCDs.  A partitioned device is refused.
+bool device_is_whole_chip(int dev) { return mst_host::has_compute_units(dev, kNumCu); }
 bool set_kernel_attributes() {   // on the current device
   bool ok = true;
   auto set = [&ok](const void* f) {

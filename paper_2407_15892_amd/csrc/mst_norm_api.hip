@@ -149,9 +149,14 @@ mst_status dispatch_bwd(const NormBwd& a, int32_t type, int64_t gate_rows, void*
                                : dispatch_bwd<__bf16, kPre, kRes>(a, gate_rows, workspace, st);
 }
 
+// The rows are dealt out to the workgroups of a whole chip (BwdPlan): a partitioned device is refused.
+mst_host::PerDeviceOnce g_shape_once;
 mst_status check_device() {
   int dev = 0;
-  return hipGetDevice(&dev) == hipSuccess ? MST_OK : MST_ERR_NO_DEVICE;
+  if (hipGetDevice(&dev) != hipSuccess) return MST_ERR_NO_DEVICE;
+  if (g_shape_once.run(dev, [dev] { return mst_host::has_compute_units(dev, kNumCu); })) return MST_OK;
+  (void)hipGetLastError();
+  return MST_ERR_NO_DEVICE;
 }
 
 bool both_or_neither(const void* a, const void* b) { return !a == !b; }
