@@ -125,7 +125,7 @@ class _Tensors:
     def gate(self, name: str, t, gate_rows: int, dtype=_BF16):
         if t is None:
             return None
-        if gate_rows < 1:
+        if not 1 <= gate_rows < 1 << 63:      # ctypes keeps the low 64 bits
             raise MstError(BAD_ARGUMENT, f"{name}: gate_rows is {gate_rows}")
         return self.at(name, t, dtype, (-(-self.S // gate_rows), self.d))
 
