@@ -37,7 +37,8 @@
  *                             even: -127 .. 127
  *
  * Both divisions and products by a power of two are exact, so the error is half
- * a step, at most 1 / 127.5 of the block's largest magnitude, the codes are a
+ * a step: at most 1 / 127.5 of the block's largest magnitude, or, with E = 0
+ * (largest magnitudes below 127.5 * 2^-127), at most 2^-128.  The codes are a
  * function of the tensor alone, and what a code stands for fits bf16 without a
  * second rounding: 33 bytes for 32 entries.  A block with a NaN, an infinity or
  * a magnitude from 127.5 * 2^121 on (3.39e38, which would be rounded to 2^128) has
