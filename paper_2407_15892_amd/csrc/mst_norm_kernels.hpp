@@ -709,7 +709,6 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       }
       if (kRes) {
         o_next[slot][k].get(o[k]);
-        if (!kPre) again_f(k);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           sums[kPre ? 2 : 0] = fmaf(o[k][i], o[k][i], sums[kPre ? 2 : 0]);
@@ -761,10 +760,6 @@ __global__ __launch_bounds__(1024) void k_norm_bwd(const NormBwd a) {
       for (int k = 0; k < kNc; ++k) {
         if (kLean) {
           __builtin_amdgcn_sched_barrier(0);
-          if (!kPre) {
-            renew(dy_next[slot][k]);
-            dy_next[slot][k].get(dy[k]);
-          }
           renew(o_next[slot][k].e);
           o_next[slot][k].get(o[k]);
           again_f(k);
