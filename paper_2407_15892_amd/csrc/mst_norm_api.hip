@@ -59,9 +59,10 @@ mst_status check_gate(const void* gate, int64_t gate_rows, float scale, int64_t 
 constexpr int kAloneRows = 2;
 
 // How the backward calls deal out the rows (k_norm_bwd).  gate_rows: 0 without a gate; pre: with the norm before a block.
-//   Workgroups: a compute unit is given teams whose lanes have 512 times eight columns (1024 in the residual's backward alone, which loads half
-//   as much), about 40 KB of loads under way.  More of them pass through more rows at a time and are slower for it: 32768 x 4096, us, with one
-//   and with two workgroups of 512 lanes: norm 160, 162 (155, 180 with two rows ahead), both norms 243, 263, residual 138, 118.
+//   Workgroups: a compute unit is given one or more whose lanes have 512 times eight columns together (lanes behind a row's end not counted); in the
+//   residual's backward alone, which loads half as much, as many as fit 1024 lanes (all counted).  That is about 40 KB of loads under way.  More of them
+//   pass through more rows at a time and are slower for it: 32768 x 4096, us, with one and with two workgroups of 512 lanes: norm 160, 162 (155, 180
+//   with two rows ahead), both norms 243, 263, residual 138, 118.
 //   Rows of the gate: whole ones to a team where there are as many as teams (half as many for the residual's backward), or where a row of the gate
 //   has fewer rows than a workgroup has teams; else `share` workgroups each.  Whole against shared, us, 8192 x 1024, both
 //   norms, 1 row of the gate for 8 rows: 27, 29, for 16: 37, 23; residual: for 8 18, 20, for 16 24, 17; 32768 x 256, both

@@ -299,8 +299,10 @@ constexpr uint32_t kNoColumn = 1u << 29;
 template <class T> constexpr int rows_ahead(bool pre, bool res, int chunks) { return pre && !res && chunks == 1 && sizeof(T) == 2 ? 2 : 1; }
 
 constexpr int kNonTemporalAccess = 2;         // cache policy of buffer loads and stores
-// Results are written past the caches: a matrix product reads them next, which has time for it, or a pass much later, and the caches
-// keep what comes in.  8192 x 4096, norm with checkpoint: 35 us -> 26.  (A pass that only reads H right behind it takes 26 us then, not 14.)
+// Results are written past the caches, which keep what comes in: 8192 x 4096, norm with checkpoint 33.4 us -> 29.7.  What reads them much later, as a
+// backward pass does, loses nothing; a pass right behind this one reads from memory what the caches might have held.  The norm with checkpoint and the
+// MLP's forward on its H, in a captured graph, us, past the caches and through them: d = 4096, I = 14336: 1 and 64 rows the same, 512 rows 222, 215, 2048 rows
+// 568, 566, 8192 rows 2072, 2067; d = 1024, I = 2816: 1 and 64 rows the same, 512 rows 30.0, 27.1, 2048 rows 63.4, 60.3, 8192 rows 242, 229.
 constexpr int kStorePolicy = kNonTemporalAccess;
 
 // A lane's columns: entries 0..3 from column a on, entries 4..7 from b (kApart: half a chunk apart; else b = a + 4, and the access is

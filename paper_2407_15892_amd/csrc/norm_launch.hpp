@@ -11,9 +11,15 @@ namespace mst_norm {
 
 using namespace mst;
 
-// Tensors of a call that are more than the last-level cache holds beside what else is in it are read past the caches: 16384 x
-// 4096, us, pack (201 MB) 35.3 -> 32.9, norm's backward of 8192 x 4096 (236 MB) 47.8 -> 46.4; below, where a call finds
-// what was written just before it, it costs: 8192 x 4096 pack (100 MB) 15.7 -> 17.8, norm's forward (169 MB) 25.7 -> 30.2.
+// A call whose tensors are more than this reads its inputs past the caches, which cannot hold them beside what else is in there; below
+// it a call may find in them what was written just before.  Counted is what it reads and writes, but for the checkpoint that a norm's or a
+// residual's forward leaves.  Rows of 4096, bf16, us, through the caches and past them:
+//   below   2048 rows: backward of the norm 17.4, 18.4, of the residual 16.1, 17.6, of both 23.6, 24.6; 4096 rows: forward of the norm
+//           13.7, 16.7, of the residual 21.2, 23.0, of both 29.8, 32.1; 8192 rows: pack 16.5, 17.7, unpack 15.6, 18.1
+//   beyond  12300 rows: backward of the norm 67.0, 63.0, of both 97.4, 90.4; 32768 rows: residual 156.5, 152.1, its backward 124.9, 118.0;
+//           131072 rows: pack 269, 252, unpack 258, 250, forward of the norm 437, 433
+// Not all of them have their border here: pack gains from 150 MB on (12288 rows 26.4, 25.2), the backward of both norms from 160 (4096 rows
+// 40.0, 38.3), unpack from 300 (16400 rows 31.8, 33.3, 24576 rows 49.1, 48.5), and the norm of a checkpoint nowhere (131072 rows 263, 267).
 constexpr int64_t kCacheBytes = 192 << 20;
 
 inline mst_status launched() { return hipGetLastError() == hipSuccess ? MST_OK : MST_ERR_LAUNCH; }
@@ -55,6 +61,8 @@ mst_status launch_fwd(const NormFwd& a, hipStream_t st) {
   const RowPlan p(a.d);
   const int64_t t = kRebuild ? 1 : sizeof(T), n = (int64_t)a.S * a.d;
   const bool stream = n * (t + (kPre ? 2 : 0) + (kRes ? 2 + t : 0)) > kCacheBytes;
+  // Long rows always through the caches.  us, through them and past them, bf16: 2048 x 12288 norm with checkpoint 20.0, 24.8, rebuilt 13.2, 17.8;
+  // 8192 x 16384 norm 113.0, 113.4, residual 166, 163, both 254, 252, rebuilt 77, 81; 4096 x 12288 float32, gated: 61.5, 60.4, 98.9, 97.6, both 140, 139.
   if (p.chunks == 2) return launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 2>(a, p, st);
   return stream ? launch_fwd_chunks<T, kRes, kPre, kRebuild, kNonTemporalAccess, 1>(a, p, st)
                 : launch_fwd_chunks<T, kRes, kPre, kRebuild, 0, 1>(a, p, st);
