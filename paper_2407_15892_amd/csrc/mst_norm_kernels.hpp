@@ -571,7 +571,8 @@ struct NormBwd {
 // vector units' time used), by latency where they are few (a row takes 2 us from its loads to its last store).
 // A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
 // for their columns.  Of long rows (two chunks, d > 8192) with two norms or in float32 only what was loaded stays in registers, and
-// is converted for each use (kLean): with 16 waves a wave has 128 of them.  2048 x 12288, both norms: 169 us -> 121, float32 and
+// is converted for each use (kLean): with 16 waves a lane has 128 of them, and what does not fit goes to scratch memory all the same (both norms: bf16 54 to 59
+// registers of a lane, with whole rows of the gate 94 to 102, float32 62 to 78 and 109 to 121; residual alone with whole rows of the gate 3 to 33).  2048 x 12288, both norms: 169 us -> 121, float32 and
 // gated 267 -> 152, its norm alone 78 -> 60; bf16's norm alone 42 -> 45, and the residual's 31 -> 38, do not.
 //   kWhole = false  `share` workgroups have the rows of one row of the gate (all rows without a gate), adjacent rows in
 //                   adjacent teams: memory is passed through in a few streams.  Sums of dY * N, without the gate, to the workspace.
@@ -865,7 +866,7 @@ struct Four {
 // workgroups have not done that (and the gradient of a single row of gates); from 2 on the gradients of several rows of gates, `share` sums
 // each.  A workgroup takes 32 columns (a cache line of each sum): 8 lanes of four, and 128 groups of 8 lanes; of these `slices`
 // (a power of two) share out the sums of a result, and are added up in one order.  512 sums of 4096
-// columns: 4.2 us, 2 of them a launch's.
+// columns: 4.2 us, 2 of them a launch's; with 8 rows of the gate, whose sums the workgroups of dw_post and those of dgate each read, 8.2.
 constexpr int kReduceThreads = 1024, kReduceCols = 32, kReduceSlices = kReduceThreads / 8;
 __global__ __launch_bounds__(kReduceThreads) void k_norm_reduce(const NormBwd a, int n, int whole, int gate_slices) {
   __shared__ norm_f32x4 lds[kReduceSlices / 8][8];
