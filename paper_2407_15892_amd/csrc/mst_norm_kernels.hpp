@@ -571,9 +571,10 @@ struct NormBwd {
 // vector units' time used), by latency where they are few (a row takes 2 us from its loads to its last store).
 // A team takes `rows` rows in turn, the next one's loads on their way while it computes; its lanes keep the sums over them
 // for their columns.  Of long rows (two chunks, d > 8192) with two norms or in float32 only what was loaded stays in registers, and
-// is converted for each use (kLean): with 16 waves a lane has 128 of them, and what does not fit goes to scratch memory all the same (both norms: bf16 54 to 59
-// registers of a lane, with whole rows of the gate 94 to 102, float32 62 to 78 and 109 to 121; residual alone with whole rows of the gate 3 to 33).  2048 x 12288, both norms: 169 us -> 121, float32 and
-// gated 267 -> 152, its norm alone 78 -> 60; bf16's norm alone 42 -> 45, and the residual's 31 -> 38, do not.
+// is converted for each use (kLean): with 16 waves a lane has 128 of them, and what does not fit goes to scratch memory all the same
+// (both norms: bf16 54 to 59 registers of a lane, with whole rows of the gate 94 to 102, float32 62 to 78 and 109 to 121; residual alone with
+// whole rows of the gate 3 to 33).  2048 x 12288, both norms: 169 us -> 121, float32 and gated 267 -> 152, its norm alone 78 -> 60;
+// bf16's norm alone 42 -> 45, and the residual's 31 -> 38, do not.
 //   kWhole = false  `share` workgroups have the rows of one row of the gate (all rows without a gate), adjacent rows in
 //                   adjacent teams: memory is passed through in a few streams.  Sums of dY * N, without the gate, to the workspace.
 //   kWhole = true   for many short rows of gates: a team has all rows of one, then those of another; it writes their gradient
