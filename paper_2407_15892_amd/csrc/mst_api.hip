@@ -7,6 +7,7 @@
 #include "../../include/mst_lmhead.h"
 #include "host_util.hpp"
 #include "launch_model.hpp"
+#include "mst_objective_kernels.hpp"
 #include "mst_small_kernels.hpp"
 #include "mst_stream_kernels.hpp"
 
@@ -572,18 +573,25 @@ mst_host::PerDeviceOnce g_attr_once, g_shape_once;
 // The tile maps and the schedule's cost model are written for the whole chip: kNumCu compute units in kNumXcd
 // XCDs.  A partitioned device is refused.
 bool device_is_whole_chip(int dev) { return mst_host::has_compute_units(dev, kNumCu); }
+template <class E, class D, class Set>       // the kernels that form logits, for one objective
+void set_logits_kernels(Set set) {
+  set((const void*)k_fwd_gemm_lse<false, E>);
+  set((const void*)k_fwd_gemm_lse<true, E>);
+  set((const void*)k_fwd_gemm_lse_small<TileFwd64, E>);
+  set((const void*)k_fwd_gemm_lse_small<TileFwd32, E>);
+  set((const void*)k_fwd_gemm_lse_rows128<E>);
+  set((const void*)k_bwd_gemm_dlogits_small<Tile64, D>);
+  set((const void*)k_bwd_gemm_dlogits_small<Tile64Lone, D>);
+  set((const void*)k_bwd_gemm_dlogits<false, D>);
+  set((const void*)k_bwd_gemm_dlogits<true, D>);
+}
 bool set_kernel_attributes() {   // on the current device
   bool ok = true;
   auto set = [&ok](const void* f) {
     if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes) != hipSuccess) ok = false;
   };
-  set((const void*)k_fwd_gemm_lse<false>);
-  set((const void*)k_fwd_gemm_lse<true>);
-  set((const void*)k_fwd_gemm_lse_small<TileFwd64>);
-  set((const void*)k_fwd_gemm_lse_small<TileFwd32>);
-  set((const void*)k_fwd_gemm_lse_rows128);
-  set((const void*)k_bwd_gemm_dlogits_small<Tile64>);
-  set((const void*)k_bwd_gemm_dlogits_small<Tile64Lone>);
+  set_logits_kernels<LseEpilogue, CeGrad>(set);
+  set_logits_kernels<ObjEpilogue, ObjGrad>(set);
   set((const void*)k_bwd_gemm_dh_small<Tile64>);
   set((const void*)k_bwd_gemm_dh_small<Tile64Lone>);
   set((const void*)k_bwd_gemm_dw_small<Tile64>);
@@ -599,8 +607,6 @@ bool set_kernel_attributes() {   // on the current device
   set((const void*)k_bwd_stream<Stream384Split, Stream384Split>);
   set((const void*)k_bwd_stream<Stream512, Stream512>);
   set((const void*)k_bwd_stream<Stream512Split, Stream512Split>);
-  set((const void*)k_bwd_gemm_dlogits<false>);
-  set((const void*)k_bwd_gemm_dlogits<true>);
   set((const void*)k_bwd_gemm_dh<false>);
   set((const void*)k_bwd_gemm_dh<true>);
   set((const void*)k_bwd_gemm_dw<false, false>);
@@ -618,7 +624,6 @@ bool set_kernel_attributes() {   // on the current device
   return ok;
 }
 
-auto dlogits_kernel(bool even) { return even ? k_bwd_gemm_dlogits<true> : k_bwd_gemm_dlogits<false>; }
 auto dw_kernel(bool store_only, bool even) {
   return even ? (store_only ? k_bwd_gemm_dw<true, true> : k_bwd_gemm_dw<false, true>)
               : (store_only ? k_bwd_gemm_dw<true, false> : k_bwd_gemm_dw<false, false>);
@@ -669,13 +674,12 @@ bool finalize_in_one(const Plan& p) {
   return p.S <= 1024 && p.S <= p.fwd_group_rows && p.n_vt <= kFinOneTiles && p.S * p.n_vt <= 12288;
 }
 
-// forward pass over all chunks: writes lse (if non-null) and nll (if non-null)
-// `ctl`: its queues serve persistent forward launches (nullptr: one workgroup per tile)
-mst_status run_forward_chunks(const Plan& p, const __bf16* H, const __bf16* W, const int32_t* labels,
-                              int ignore_index, char* ws, float* lse, float* nll, hipStream_t st, Control* ctl = nullptr, bool finalize = true) {
-  float* tgt = reinterpret_cast<float*>(ws + p.f_tgt);
-  float2* part = reinterpret_cast<float2*>(ws + p.f_part);
-  const size_t stride = (size_t)p.fwd_group_rows;
+// Forward over all chunks, group by group: before(g0, rows), the logits with epilogue_of(g0), after(g0, rows).
+// `ctl`: its queues serve persistent launches (nullptr: one workgroup per tile)
+template <class EpilogueOf, class Before, class After>
+mst_status run_forward_groups(const Plan& p, const __bf16* H, const __bf16* W, hipStream_t st, Control* ctl,
+                              EpilogueOf epilogue_of, Before before, After after) {
+  typedef decltype(epilogue_of(int64_t(0))) E;
   const int tile_rows = forward_tile_rows(p);
   int* queue = ctl && persistent_forward(p) ? ctl->queue : nullptr;
   int queue_base = 0;
@@ -685,6 +689,8 @@ mst_status run_forward_chunks(const Plan& p, const __bf16* H, const __bf16* W, c
   }
   for (int64_t g0 = 0; g0 < p.S; g0 += p.fwd_group_rows) {
     const int64_t g_rows = forward_group_rows(p, g0);
+    const E epilogue = epilogue_of(g0);
+    before(g0, (int)g_rows);
     // One launch for the group's mini-sequences.  Rows are independent and no logits are stored, so the row tiles
     // of the launch need not respect the boundaries between the mini-sequences of the group: a mini-sequence
     // shorter than a 256-row tile costs no idle tile rows, and every row's result is bit-identical for every M.
@@ -694,27 +700,39 @@ mst_status run_forward_chunks(const Plan& p, const __bf16* H, const __bf16* W, c
       const bool even = !queue && forward_even_map(p.n_vt, n_st);
       const int tiles = launch_grid(even, p.n_vt, n_st);
       const int grid = queue && tiles > kNumCu ? kNumCu : tiles;
-      hipLaunchKernelGGL(even ? k_fwd_gemm_lse<true> : k_fwd_gemm_lse<false>, dim3(grid), dim3(kThreads), kLdsBytes, st,
-                         H + g0 * p.d, W, labels + g0, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt,
-                         part, stride, tgt, queue, queue_base);
+      const auto kernel = even ? k_fwd_gemm_lse<true, E> : k_fwd_gemm_lse<false, E>;
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), kLdsBytes, st,
+                         H + g0 * p.d, W, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt, epilogue, queue, queue_base);
       queue_base += tiles / kNumXcd + grid;
     } else {
       Scope sc(st, MST_K_FWD_GEMM_LSE);
-      const auto kernel = tile_rows == 128 ? k_fwd_gemm_lse_rows128
-                        : tile_rows == 64 ? k_fwd_gemm_lse_small<TileFwd64> : k_fwd_gemm_lse_small<TileFwd32>;
+      const auto kernel = tile_rows == 128 ? k_fwd_gemm_lse_rows128<E>
+                        : tile_rows == 64 ? k_fwd_gemm_lse_small<TileFwd64, E> : k_fwd_gemm_lse_small<TileFwd32, E>;
       const int threads = tile_rows == 128 ? kThreads : TileFwd64::kThreads;
       const int lds = tile_rows == 128 ? Tile16Rows128::kLds : tile_rows == 64 ? TileFwd64::kLds : TileFwd32::kLds;
       hipLaunchKernelGGL(kernel, dim3(even_grid(p.n_vt, n_st)), dim3(threads), lds, st,
-                         H + g0 * p.d, W, labels + g0, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt, part, stride, tgt);
+                         H + g0 * p.d, W, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt, epilogue);
     }
-    if (finalize) {
-      Scope sc(st, MST_K_LSE_FINALIZE);
-      hipLaunchKernelGGL(k_lse_finalize, dim3((unsigned)((g_rows + kFinRows - 1) / kFinRows)), dim3(kFinRows * kFinGroups), 0, st,
-                         part, stride, p.n_vt, tgt, labels + g0, (int)g_rows, (int)p.V, ignore_index,
-                         lse ? lse + g0 : nullptr, nll ? nll + g0 : nullptr);
-    }
+    after(g0, (int)g_rows);
   }
   return check_launch();
+}
+
+// that of the cross-entropy: writes lse (if non-null) and nll (if non-null)
+mst_status run_forward_chunks(const Plan& p, const __bf16* H, const __bf16* W, const int32_t* labels,
+                              int ignore_index, char* ws, float* lse, float* nll, hipStream_t st, Control* ctl = nullptr, bool finalize = true) {
+  float* tgt = reinterpret_cast<float*>(ws + p.f_tgt);
+  float2* part = reinterpret_cast<float2*>(ws + p.f_part);
+  const size_t stride = (size_t)p.fwd_group_rows;
+  return run_forward_groups(
+      p, H, W, st, ctl, [&](int64_t g0) { return LseEpilogue{labels + g0, part, stride, tgt}; }, [](int64_t, int) {},
+      [&](int64_t g0, int rows) {
+        if (!finalize) return;
+        Scope sc(st, MST_K_LSE_FINALIZE);
+        hipLaunchKernelGGL(k_lse_finalize, dim3((unsigned)((rows + kFinRows - 1) / kFinRows)), dim3(kFinRows * kFinGroups), 0, st,
+                           part, stride, p.n_vt, tgt, labels + g0, rows, (int)p.V, ignore_index,
+                           lse ? lse + g0 : nullptr, nll ? nll + g0 : nullptr);
+      });
 }
 
 // dH and dW of the rows whose dlogits are at G, one launch of small tiles
@@ -726,6 +744,215 @@ void launch_ksplit(hipStream_t st, const Plan& p, const __bf16* G, const __bf16*
   hipLaunchKernelGGL((k_bwd_gemm_dh_dw_small<CH, Tile64>), dim3(dh_grid + even_grid(n_vh, n_jw)), dim3(Tile64::kThreads),
                      CH::kLds > Tile64::kLds ? CH::kLds : Tile64::kLds, st, G, p.ldg, W, H, rows, (int)p.d, (int)p.V,
                      n_sh, n_jh, dh_grid, n_vh, n_jw, accumulate, last, n_valid, grad_loss, dH, dW);
+}
+
+// Backward in the order that the plan has, of an objective whose gradient grad_of(r0) gives (rows from r0 on, see CeGrad).
+// after_dlogits(r0, rows, v_base, V, G, ldg): behind every launch that has formed the dlogits of those rows and vocabulary entries.
+template <class GradOf, class After>
+mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb, const long long* nv, float grad_loss, char* ws, __bf16* dHb,
+                               float* dW, hipStream_t st, GradOf grad_of, After after_dlogits) {
+  typedef decltype(grad_of(int64_t(0))) D;
+  __bf16* slot[2] = {reinterpret_cast<__bf16*>(ws), reinterpret_cast<__bf16*>(ws + p.b_slot)};
+  auto dlogits_kernel = [](bool even) { return even ? k_bwd_gemm_dlogits<true, D> : k_bwd_gemm_dlogits<false, D>; };
+  auto rows_of = [&](int i) { const int64_t r0 = (int64_t)i * p.C; return (int)((p.S - r0) < p.C ? (p.S - r0) : p.C); };
+  auto dlogits = [&](int i, int rows, __bf16* G) {        // of `rows` rows from chunk i on
+    const int64_t r0 = (int64_t)i * p.C;
+    const int n_st = (rows + kTile - 1) / kTile;
+    if (p.joint == MST_PAIR_DH128 ? small_pair_dlogits(p, rows) : p.small_dlogits) {
+      Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
+      const int n_vh = (int)((p.V + Tile64::EA - 1) / Tile64::EA), n_sh = (rows + Tile64::EB - 1) / Tile64::EB;
+      const bool lone = lone_small((double)n_vh * n_sh);
+      const auto kernel = lone ? k_bwd_gemm_dlogits_small<Tile64Lone, D> : k_bwd_gemm_dlogits_small<Tile64, D>;
+      hipLaunchKernelGGL(kernel, dim3(even_grid(n_vh, n_sh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
+                         Hb + r0 * p.d, Wb, grad_of(r0), rows, (int)p.d, (int)p.V, n_sh, n_vh, G, p.ldg);
+    } else {
+      Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
+      const bool even = use_even_map(p.n_vt, n_st);
+      hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, p.n_vt, n_st)), dim3(kThreads), kLdsBytes, st,
+                         Hb + r0 * p.d, Wb, grad_of(r0), rows, (int)p.d, (int)p.V, 0, n_st, p.n_vt, G, p.ldg);
+    }
+    after_dlogits(r0, rows, 0, (int)p.V, G, p.ldg);
+  };
+  auto dh_reduce = [&](int i, int rows, const void* partial, int split) {
+    Scope sc(st, MST_K_BWD_DH_REDUCE);
+    const size_t n = (size_t)rows * p.d;
+    hipLaunchKernelGGL(k_bwd_dh_reduce, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st,
+                       static_cast<const float*>(partial), split, (size_t)p.C * p.d, n, nv, grad_loss, dHb + (int64_t)i * p.C * p.d);
+  };
+  auto grad_h = [&](int i, const __bf16* G, void* partial_space) {
+    const int64_t r0 = (int64_t)i * p.C;
+    const int rows = rows_of(i), n_st = (rows + kTile - 1) / kTile;
+    float* partial = static_cast<float*>(partial_space);
+    const int split = p.small_dh ? p.small_dh_split : p.dh_split;
+    {
+      Scope sc(st, MST_K_BWD_GEMM_DH);
+      if (p.small_dh) {
+        const int n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA), n_sh = (rows + Tile64::EB - 1) / Tile64::EB;
+        const bool lone = lone_small((double)n_jh * n_sh * split);
+        hipLaunchKernelGGL(lone ? k_bwd_gemm_dh_small<Tile64Lone> : k_bwd_gemm_dh_small<Tile64>,
+                           dim3(even_grid(n_jh * split, n_sh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
+                           G, p.ldg, Wb, rows, (int)p.d, (int)p.V, n_sh, n_jh, split, p.small_dh_ksteps, nv, grad_loss,
+                           partial, p.C, dHb + r0 * p.d);
+      } else {
+        hipLaunchKernelGGL(k_bwd_gemm_dh<false>, dim3(xcd_grid(n_st * p.n_jt * p.dh_split)), dim3(kThreads), kLdsBytes, st,
+                           G, p.ldg, Wb, rows, (int)p.d, (int)p.V, n_st, p.n_jt, p.dh_split, p.dh_ksteps, kDhSplit,
+                           nv, grad_loss, partial, p.C, dHb + r0 * p.d);
+      }
+    }
+    if (split > 1) dh_reduce(i, rows, partial, split);
+  };
+  auto grad_w = [&](int i_first, int i_last, int rows) {
+    const int64_t r0 = (int64_t)i_first * p.C;
+    Scope sc(st, MST_K_BWD_GEMM_DW);
+    if (p.small_dw) {
+      const int n_vh = (int)((p.V + Tile64::EB - 1) / Tile64::EB), n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA);
+      const bool lone = lone_small((double)n_vh * n_jh);
+      hipLaunchKernelGGL(lone ? k_bwd_gemm_dw_small<Tile64Lone> : k_bwd_gemm_dw_small<Tile64>,
+                         dim3(even_grid(n_vh, n_jh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
+                         slot[0], p.ldg, Hb + r0 * p.d, rows, (int)p.d, (int)p.V, n_vh, n_jh, i_first > 0 ? 1 : 0,
+                         i_last == p.n_chunks - 1 ? 1 : 0, nv, grad_loss, dW);
+      return;
+    }
+    const bool even = use_even_map(p.n_vt, p.n_jt);
+    hipLaunchKernelGGL(dw_kernel(i_first == 0, even), dim3(launch_grid(even, p.n_vt, p.n_jt)),
+                       dim3(kThreads), kLdsBytes, st,
+                       slot[0], p.ldg, Hb + r0 * p.d, rows, (int)p.d, (int)p.V, p.n_vt, p.n_jt,
+                       i_last == p.n_chunks - 1 ? 1 : 0, nv, grad_loss, dW);
+  };
+
+  if (p.blk_use) {
+    // Block schedule: for each block of rows, walk the vocabulary windows.  Per (row block, window):
+    //   dlogits of the block -> workspace | dH sums of the row block (+)= G W_window | dW_window (+)= G^T H_block
+    // dH of a row block is final after its last window, dW of a window after the last row block; both
+    // accumulate in a fixed order.
+    __bf16* G = reinterpret_cast<__bf16*>(ws);
+    float* dh_sums = reinterpret_cast<float*>(ws + p.blk_acc);
+    auto launch_dh_reduce_tiles = [&](int n_st, int rows, int64_t r0) {
+      Scope sc(st, MST_K_BWD_DH_REDUCE);
+      const int waves = n_st * p.n_jt * kTA16 * Tile16::kWaves;       // a multiple of the 4 of a workgroup
+      hipLaunchKernelGGL(k_bwd_dh_reduce_tiles, dim3(waves / 4), dim3(256), 0, st, dh_sums, p.blk_split, n_st, p.n_jt, rows,
+                         (int)p.d, nv, grad_loss, dHb + r0 * p.d);
+    };
+    for (int rb = 0; rb < p.blk_n_rb; ++rb) {
+      const int64_t r0 = (int64_t)rb * p.blk_rows;
+      const int rows = (int)((p.S - r0) < p.blk_rows ? (p.S - r0) : p.blk_rows);
+      const int n_st = (rows + kTile - 1) / kTile;
+      for (int w = 0; w < p.blk_n_win; ++w) {
+        const int t0 = w * p.blk_win_tiles;
+        const int tiles_w = t0 + p.blk_win_tiles <= p.n_vt ? p.blk_win_tiles : p.n_vt - t0;
+        const int64_t v_base = (int64_t)t0 * kTile;
+        const int Vw = (int)((p.V - v_base) < (int64_t)tiles_w * kTile ? (p.V - v_base) : (int64_t)tiles_w * kTile);
+        {
+          Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
+          const bool even = use_even_map(tiles_w, n_st);
+          hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, tiles_w, n_st)), dim3(kThreads), kLdsBytes, st,
+                             Hb + r0 * p.d, Wb + v_base * p.d, grad_of(r0), rows, (int)p.d, Vw, (int)v_base, n_st, tiles_w, G, p.blk_ldg);
+        }
+        after_dlogits(r0, rows, v_base, Vw, G, p.blk_ldg);
+        const bool last_win = w == p.blk_n_win - 1;
+        const int mode = p.blk_split > 1 ? (w == 0 ? kDhFirst : kDhAdd)
+                                         : (w == 0 ? (last_win ? kDhOnly : kDhFirst) : (last_win ? kDhLast : kDhAdd));
+        const int dw_last = rb == p.blk_n_rb - 1 ? 1 : 0;
+        if (p.blk_fused) {
+          Scope sc(st, MST_K_BWD_GEMM_DH_DW);
+          auto dh_share = [&](bool even) {
+            return even ? xcd_share(p.blk_split * p.n_jt, n_st, true) : p.blk_split * xcd_share(n_st, p.n_jt, false);
+          };
+          auto share = [&](bool even) { return dh_share(even) + xcd_share(tiles_w, p.n_jt, even); };
+          const bool both = saves_a_round(share(false), share(true));
+          const bool dh_even = both || uneven_over_xcds(n_st) || saves_a_round(dh_share(false), dh_share(true));
+          const bool dw_even = both || use_even_map(tiles_w, p.n_jt);
+          const bool general = p.blk_split > 1 || dh_even || dw_even;
+          const int dh_grid = dh_grid_2d(dh_even, p.blk_split, n_st, p.n_jt);
+          hipLaunchKernelGGL(general ? (rb > 0 ? k_bwd_gemm_dh_dw<false, true> : k_bwd_gemm_dh_dw<true, true>)
+                                     : (rb > 0 ? k_bwd_gemm_dh_dw<false, false> : k_bwd_gemm_dh_dw<true, false>),
+                             dim3(dh_grid + launch_grid(dw_even, tiles_w, p.n_jt)), dim3(kThreads), kLdsBytes, st,
+                             G, p.blk_ldg, Wb + v_base * p.d, Hb + r0 * p.d, rows, (int)p.d, Vw, n_st, tiles_w, p.n_jt,
+                             dh_grid, mode, dw_last, nv, grad_loss, dh_sums, p.blk_rows, dHb + r0 * p.d,
+                             dW + v_base * p.d, p.blk_split, dh_even ? 1 : 0, dw_even ? 1 : 0);
+          if (last_win && p.blk_split > 1) launch_dh_reduce_tiles(n_st, rows, r0);
+        } else {
+          {
+            Scope sc(st, MST_K_BWD_GEMM_DH);
+            const bool even = use_even_map(n_st, p.n_jt);
+            hipLaunchKernelGGL(even ? k_bwd_gemm_dh<true> : k_bwd_gemm_dh<false>, dim3(dh_grid_2d(even, 1, n_st, p.n_jt)), dim3(kThreads), kLdsBytes, st,
+                               G, p.blk_ldg, Wb + v_base * p.d, rows, (int)p.d, Vw, n_st, p.n_jt, 1, (Vw + kBK - 1) / kBK, mode,
+                               nv, grad_loss, dh_sums, p.blk_rows, dHb + r0 * p.d);
+          }
+          {
+            Scope sc(st, MST_K_BWD_GEMM_DW);
+            const bool even = use_even_map(tiles_w, p.n_jt);
+            hipLaunchKernelGGL(dw_kernel(rb == 0, even), dim3(launch_grid(even, tiles_w, p.n_jt)),
+                               dim3(kThreads), kLdsBytes, st,
+                               G, p.blk_ldg, Hb + r0 * p.d, rows, (int)p.d, Vw, tiles_w, p.n_jt,
+                               dw_last, nv, grad_loss, dW + v_base * p.d);
+          }
+        }
+      }
+    }
+    return check_launch();
+  }
+
+  // Algorithm 4's loop over mini-sequences, two at a time: the chunk pair (A, B) shares one dW pass.
+  //   dlogits(A) -> slot 0 | dH(A), partials in slot 1 | dlogits(B) -> slot 1 | dW += [G_A; G_B]^T [H_A; H_B]
+  //   | dH(B), partials in slot 0
+  if (p.joint == MST_PAIR_SPLIT) {
+    const int rows = (int)p.S, split = p.small_dh_split;
+    const int n_vh = (int)((p.V + Tile64::EB - 1) / Tile64::EB), n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA);
+    const int n_sh = (rows + Tile64::EB - 1) / Tile64::EB, dh_grid = even_grid(n_jh * split, n_sh);
+    dlogits(0, rows, slot[0]);
+    {
+      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
+      hipLaunchKernelGGL(k_bwd_gemm_dh_split_dw_small<Tile64>, dim3(dh_grid + even_grid(n_vh, n_jh)), dim3(Tile64::kThreads),
+                         Tile64::kLds, st, slot[0], p.ldg, Wb, Hb, rows, (int)p.d, (int)p.V, n_sh, n_jh, split, p.small_dh_ksteps,
+                         dh_grid, n_vh, nv, grad_loss, reinterpret_cast<float*>(slot[1]), dHb, dW);
+    }
+    if (split > 1) dh_reduce(0, rows, slot[1], split);
+    return check_launch();
+  }
+  if (p.joint == MST_PAIR_DH128) {
+    const bool even = use_even_map(p.n_vt, p.n_jt);
+    for (int ia = 0; ia < p.n_chunks; ia += 2) {          // the two slots are contiguous: the pair's dlogits are one matrix
+      const int64_t r0 = (int64_t)ia * p.C;
+      const int rows = (int)std::min(2 * (int64_t)p.C, p.S - r0);
+      const int n_sq = (rows + Tile16Quarter::EB - 1) / Tile16Quarter::EB, n_jq = (int)((p.d + Tile16Quarter::EA - 1) / Tile16Quarter::EA);
+      dlogits(ia, rows, slot[0]);
+      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
+      const auto kernel = even ? (ia > 0 ? k_bwd_gemm_dh128_dw<false, true> : k_bwd_gemm_dh128_dw<true, true>)
+                               : (ia > 0 ? k_bwd_gemm_dh128_dw<false, false> : k_bwd_gemm_dh128_dw<true, false>);
+      const int dh_grid = even_grid(n_jq, n_sq);
+      hipLaunchKernelGGL(kernel, dim3(dh_grid + launch_grid(even, p.n_vt, p.n_jt)), dim3(kThreads), kLdsBytes, st, slot[0], p.ldg, Wb,
+                         Hb + r0 * p.d, rows, (int)p.d, (int)p.V, n_sq, n_jq, dh_grid, p.n_vt, p.n_jt, ia + 2 >= p.n_chunks ? 1 : 0,
+                         nv, grad_loss, dHb + r0 * p.d, dW);
+    }
+    return check_launch();
+  }
+  if (p.joint) {
+    // the two slots are contiguous: the pair's dlogits are one matrix
+    for (int ia = 0; ia < p.n_chunks; ia += 2) {
+      const int64_t r0 = (int64_t)ia * p.C;
+      const int rows = (int)std::min(2 * (int64_t)p.C, p.S - r0);
+      dlogits(ia, rows, slot[0]);
+      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
+      const auto launch = p.joint == MST_PAIR_KSPLIT_32X16 ? launch_ksplit<TileKSplit32x16>
+                        : p.joint == MST_PAIR_KSPLIT_64X16 ? launch_ksplit<TileKSplit64x16> : launch_ksplit<TileKSplit64x32>;
+      launch(st, p, slot[0], Wb, Hb + r0 * p.d, rows, ia > 0 ? 1 : 0, ia + 2 >= p.n_chunks ? 1 : 0, nv, grad_loss, dHb + r0 * p.d, dW);
+    }
+    return check_launch();
+  }
+  for (int ia = 0; ia < p.n_chunks; ia += 2) {
+    const int ib = ia + 1;
+    dlogits(ia, rows_of(ia), slot[0]);
+    grad_h(ia, slot[0], slot[1]);
+    if (ib < p.n_chunks) {
+      dlogits(ib, rows_of(ib), slot[1]);
+      grad_w(ia, ib, p.C + rows_of(ib));
+      grad_h(ib, slot[1], slot[0]);
+    } else {
+      grad_w(ia, ia, rows_of(ia));
+    }
+  }
+  return check_launch();
 }
 
 mst_status check_forward_alignment(const void* H, const void* W, const int32_t* labels, const float* loss,
@@ -902,7 +1129,6 @@ mst_status mst_lmhead_ce_bwd(const void* H, const void* W, const int32_t* labels
     if (s != MST_OK) return s;
     lse = lse_tmp;
   }
-  __bf16* slot[2] = {reinterpret_cast<__bf16*>(ws), reinterpret_cast<__bf16*>(ws + p.b_slot)};
   __bf16* dHb = static_cast<__bf16*>(dH);
   if (p.streamed) {
     float* const partial = reinterpret_cast<float*>(ws);
@@ -919,205 +1145,8 @@ mst_status mst_lmhead_ce_bwd(const void* H, const void* W, const int32_t* labels
     }
     return check_launch();
   }
-
-  auto rows_of = [&](int i) { const int64_t r0 = (int64_t)i * p.C; return (int)((p.S - r0) < p.C ? (p.S - r0) : p.C); };
-  auto dlogits = [&](int i, int rows, __bf16* G) {        // of `rows` rows from chunk i on
-    const int64_t r0 = (int64_t)i * p.C;
-    const int n_st = (rows + kTile - 1) / kTile;
-    Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
-    if (p.joint == MST_PAIR_DH128 ? small_pair_dlogits(p, rows) : p.small_dlogits) {
-      const int n_vh = (int)((p.V + Tile64::EA - 1) / Tile64::EA), n_sh = (rows + Tile64::EB - 1) / Tile64::EB;
-      const bool lone = lone_small((double)n_vh * n_sh);
-      hipLaunchKernelGGL(lone ? k_bwd_gemm_dlogits_small<Tile64Lone> : k_bwd_gemm_dlogits_small<Tile64>,
-                         dim3(even_grid(n_vh, n_sh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
-                         Hb + r0 * p.d, Wb, labels + r0, lse + r0, rows, (int)p.d, (int)p.V, ignore_index, n_sh, n_vh, G, p.ldg);
-      return;
-    }
-    const bool even = use_even_map(p.n_vt, n_st);
-    hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, p.n_vt, n_st)), dim3(kThreads), kLdsBytes, st,
-                       Hb + r0 * p.d, Wb, labels + r0, lse + r0, rows, (int)p.d, (int)p.V, 0, (int)p.V, ignore_index,
-                       n_st, p.n_vt, G, p.ldg);
-  };
-  auto dh_reduce = [&](int i, int rows, const void* partial, int split) {
-    Scope sc(st, MST_K_BWD_DH_REDUCE);
-    const size_t n = (size_t)rows * p.d;
-    hipLaunchKernelGGL(k_bwd_dh_reduce, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st,
-                       static_cast<const float*>(partial), split, (size_t)p.C * p.d, n, nv, grad_loss, dHb + (int64_t)i * p.C * p.d);
-  };
-  auto grad_h = [&](int i, const __bf16* G, void* partial_space) {
-    const int64_t r0 = (int64_t)i * p.C;
-    const int rows = rows_of(i), n_st = (rows + kTile - 1) / kTile;
-    float* partial = static_cast<float*>(partial_space);
-    const int split = p.small_dh ? p.small_dh_split : p.dh_split;
-    {
-      Scope sc(st, MST_K_BWD_GEMM_DH);
-      if (p.small_dh) {
-        const int n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA), n_sh = (rows + Tile64::EB - 1) / Tile64::EB;
-        const bool lone = lone_small((double)n_jh * n_sh * split);
-        hipLaunchKernelGGL(lone ? k_bwd_gemm_dh_small<Tile64Lone> : k_bwd_gemm_dh_small<Tile64>,
-                           dim3(even_grid(n_jh * split, n_sh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
-                           G, p.ldg, Wb, rows, (int)p.d, (int)p.V, n_sh, n_jh, split, p.small_dh_ksteps, nv, grad_loss,
-                           partial, p.C, dHb + r0 * p.d);
-      } else {
-        hipLaunchKernelGGL(k_bwd_gemm_dh<false>, dim3(xcd_grid(n_st * p.n_jt * p.dh_split)), dim3(kThreads), kLdsBytes, st,
-                           G, p.ldg, Wb, rows, (int)p.d, (int)p.V, n_st, p.n_jt, p.dh_split, p.dh_ksteps, kDhSplit,
-                           nv, grad_loss, partial, p.C, dHb + r0 * p.d);
-      }
-    }
-    if (split > 1) dh_reduce(i, rows, partial, split);
-  };
-  auto grad_w = [&](int i_first, int i_last, int rows) {
-    const int64_t r0 = (int64_t)i_first * p.C;
-    Scope sc(st, MST_K_BWD_GEMM_DW);
-    if (p.small_dw) {
-      const int n_vh = (int)((p.V + Tile64::EB - 1) / Tile64::EB), n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA);
-      const bool lone = lone_small((double)n_vh * n_jh);
-      hipLaunchKernelGGL(lone ? k_bwd_gemm_dw_small<Tile64Lone> : k_bwd_gemm_dw_small<Tile64>,
-                         dim3(even_grid(n_vh, n_jh)), dim3(Tile64::kThreads), lone ? Tile64Lone::kLds : Tile64::kLds, st,
-                         slot[0], p.ldg, Hb + r0 * p.d, rows, (int)p.d, (int)p.V, n_vh, n_jh, i_first > 0 ? 1 : 0,
-                         i_last == p.n_chunks - 1 ? 1 : 0, nv, grad_loss, dW);
-      return;
-    }
-    const bool even = use_even_map(p.n_vt, p.n_jt);
-    hipLaunchKernelGGL(dw_kernel(i_first == 0, even), dim3(launch_grid(even, p.n_vt, p.n_jt)),
-                       dim3(kThreads), kLdsBytes, st,
-                       slot[0], p.ldg, Hb + r0 * p.d, rows, (int)p.d, (int)p.V, p.n_vt, p.n_jt,
-                       i_last == p.n_chunks - 1 ? 1 : 0, nv, grad_loss, dW);
-  };
-
-  if (p.blk_use) {
-    // Block schedule: for each block of rows, walk the vocabulary windows.  Per (row block, window):
-    //   dlogits of the block -> workspace | dH sums of the row block (+)= G W_window | dW_window (+)= G^T H_block
-    // dH of a row block is final after its last window, dW of a window after the last row block; both
-    // accumulate in a fixed order.
-    __bf16* G = reinterpret_cast<__bf16*>(ws);
-    float* dh_sums = reinterpret_cast<float*>(ws + p.blk_acc);
-    auto launch_dh_reduce_tiles = [&](int n_st, int rows, int64_t r0) {
-      Scope sc(st, MST_K_BWD_DH_REDUCE);
-      const int waves = n_st * p.n_jt * kTA16 * Tile16::kWaves;       // a multiple of the 4 of a workgroup
-      hipLaunchKernelGGL(k_bwd_dh_reduce_tiles, dim3(waves / 4), dim3(256), 0, st, dh_sums, p.blk_split, n_st, p.n_jt, rows,
-                         (int)p.d, nv, grad_loss, dHb + r0 * p.d);
-    };
-    for (int rb = 0; rb < p.blk_n_rb; ++rb) {
-      const int64_t r0 = (int64_t)rb * p.blk_rows;
-      const int rows = (int)((p.S - r0) < p.blk_rows ? (p.S - r0) : p.blk_rows);
-      const int n_st = (rows + kTile - 1) / kTile;
-      for (int w = 0; w < p.blk_n_win; ++w) {
-        const int t0 = w * p.blk_win_tiles;
-        const int tiles_w = t0 + p.blk_win_tiles <= p.n_vt ? p.blk_win_tiles : p.n_vt - t0;
-        const int64_t v_base = (int64_t)t0 * kTile;
-        const int Vw = (int)((p.V - v_base) < (int64_t)tiles_w * kTile ? (p.V - v_base) : (int64_t)tiles_w * kTile);
-        {
-          Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
-          const bool even = use_even_map(tiles_w, n_st);
-          hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, tiles_w, n_st)), dim3(kThreads), kLdsBytes, st,
-                             Hb + r0 * p.d, Wb + v_base * p.d, labels + r0, lse + r0, rows, (int)p.d, Vw, (int)v_base,
-                             (int)p.V, ignore_index, n_st, tiles_w, G, p.blk_ldg);
-        }
-        const bool last_win = w == p.blk_n_win - 1;
-        const int mode = p.blk_split > 1 ? (w == 0 ? kDhFirst : kDhAdd)
-                                         : (w == 0 ? (last_win ? kDhOnly : kDhFirst) : (last_win ? kDhLast : kDhAdd));
-        const int dw_last = rb == p.blk_n_rb - 1 ? 1 : 0;
-        if (p.blk_fused) {
-          Scope sc(st, MST_K_BWD_GEMM_DH_DW);
-          auto dh_share = [&](bool even) {
-            return even ? xcd_share(p.blk_split * p.n_jt, n_st, true) : p.blk_split * xcd_share(n_st, p.n_jt, false);
-          };
-          auto share = [&](bool even) { return dh_share(even) + xcd_share(tiles_w, p.n_jt, even); };
-          const bool both = saves_a_round(share(false), share(true));
-          const bool dh_even = both || uneven_over_xcds(n_st) || saves_a_round(dh_share(false), dh_share(true));
-          const bool dw_even = both || use_even_map(tiles_w, p.n_jt);
-          const bool general = p.blk_split > 1 || dh_even || dw_even;
-          const int dh_grid = dh_grid_2d(dh_even, p.blk_split, n_st, p.n_jt);
-          hipLaunchKernelGGL(general ? (rb > 0 ? k_bwd_gemm_dh_dw<false, true> : k_bwd_gemm_dh_dw<true, true>)
-                                     : (rb > 0 ? k_bwd_gemm_dh_dw<false, false> : k_bwd_gemm_dh_dw<true, false>),
-                             dim3(dh_grid + launch_grid(dw_even, tiles_w, p.n_jt)), dim3(kThreads), kLdsBytes, st,
-                             G, p.blk_ldg, Wb + v_base * p.d, Hb + r0 * p.d, rows, (int)p.d, Vw, n_st, tiles_w, p.n_jt,
-                             dh_grid, mode, dw_last, nv, grad_loss, dh_sums, p.blk_rows, dHb + r0 * p.d,
-                             dW + v_base * p.d, p.blk_split, dh_even ? 1 : 0, dw_even ? 1 : 0);
-          if (last_win && p.blk_split > 1) launch_dh_reduce_tiles(n_st, rows, r0);
-        } else {
-          {
-            Scope sc(st, MST_K_BWD_GEMM_DH);
-            const bool even = use_even_map(n_st, p.n_jt);
-            hipLaunchKernelGGL(even ? k_bwd_gemm_dh<true> : k_bwd_gemm_dh<false>, dim3(dh_grid_2d(even, 1, n_st, p.n_jt)), dim3(kThreads), kLdsBytes, st,
-                               G, p.blk_ldg, Wb + v_base * p.d, rows, (int)p.d, Vw, n_st, p.n_jt, 1, (Vw + kBK - 1) / kBK, mode,
-                               nv, grad_loss, dh_sums, p.blk_rows, dHb + r0 * p.d);
-          }
-          {
-            Scope sc(st, MST_K_BWD_GEMM_DW);
-            const bool even = use_even_map(tiles_w, p.n_jt);
-            hipLaunchKernelGGL(dw_kernel(rb == 0, even), dim3(launch_grid(even, tiles_w, p.n_jt)),
-                               dim3(kThreads), kLdsBytes, st,
-                               G, p.blk_ldg, Hb + r0 * p.d, rows, (int)p.d, Vw, tiles_w, p.n_jt,
-                               dw_last, nv, grad_loss, dW + v_base * p.d);
-          }
-        }
-      }
-    }
-    return check_launch();
-  }
-
-  // Algorithm 4's loop over mini-sequences, two at a time: the chunk pair (A, B) shares one dW pass.
-  //   dlogits(A) -> slot 0 | dH(A), partials in slot 1 | dlogits(B) -> slot 1 | dW += [G_A; G_B]^T [H_A; H_B]
-  //   | dH(B), partials in slot 0
-  if (p.joint == MST_PAIR_SPLIT) {
-    const int rows = (int)p.S, split = p.small_dh_split;
-    const int n_vh = (int)((p.V + Tile64::EB - 1) / Tile64::EB), n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA);
-    const int n_sh = (rows + Tile64::EB - 1) / Tile64::EB, dh_grid = even_grid(n_jh * split, n_sh);
-    dlogits(0, rows, slot[0]);
-    {
-      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
-      hipLaunchKernelGGL(k_bwd_gemm_dh_split_dw_small<Tile64>, dim3(dh_grid + even_grid(n_vh, n_jh)), dim3(Tile64::kThreads),
-                         Tile64::kLds, st, slot[0], p.ldg, Wb, Hb, rows, (int)p.d, (int)p.V, n_sh, n_jh, split, p.small_dh_ksteps,
-                         dh_grid, n_vh, nv, grad_loss, reinterpret_cast<float*>(slot[1]), dHb, dW);
-    }
-    if (split > 1) dh_reduce(0, rows, slot[1], split);
-    return check_launch();
-  }
-  if (p.joint == MST_PAIR_DH128) {
-    const bool even = use_even_map(p.n_vt, p.n_jt);
-    for (int ia = 0; ia < p.n_chunks; ia += 2) {          // the two slots are contiguous: the pair's dlogits are one matrix
-      const int64_t r0 = (int64_t)ia * p.C;
-      const int rows = (int)std::min(2 * (int64_t)p.C, p.S - r0);
-      const int n_sq = (rows + Tile16Quarter::EB - 1) / Tile16Quarter::EB, n_jq = (int)((p.d + Tile16Quarter::EA - 1) / Tile16Quarter::EA);
-      dlogits(ia, rows, slot[0]);
-      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
-      const auto kernel = even ? (ia > 0 ? k_bwd_gemm_dh128_dw<false, true> : k_bwd_gemm_dh128_dw<true, true>)
-                               : (ia > 0 ? k_bwd_gemm_dh128_dw<false, false> : k_bwd_gemm_dh128_dw<true, false>);
-      const int dh_grid = even_grid(n_jq, n_sq);
-      hipLaunchKernelGGL(kernel, dim3(dh_grid + launch_grid(even, p.n_vt, p.n_jt)), dim3(kThreads), kLdsBytes, st, slot[0], p.ldg, Wb,
-                         Hb + r0 * p.d, rows, (int)p.d, (int)p.V, n_sq, n_jq, dh_grid, p.n_vt, p.n_jt, ia + 2 >= p.n_chunks ? 1 : 0,
-                         nv, grad_loss, dHb + r0 * p.d, dW);
-    }
-    return check_launch();
-  }
-  if (p.joint) {
-    // the two slots are contiguous: the pair's dlogits are one matrix
-    for (int ia = 0; ia < p.n_chunks; ia += 2) {
-      const int64_t r0 = (int64_t)ia * p.C;
-      const int rows = (int)std::min(2 * (int64_t)p.C, p.S - r0);
-      dlogits(ia, rows, slot[0]);
-      Scope sc(st, MST_K_BWD_GEMM_DH_DW);
-      const auto launch = p.joint == MST_PAIR_KSPLIT_32X16 ? launch_ksplit<TileKSplit32x16>
-                        : p.joint == MST_PAIR_KSPLIT_64X16 ? launch_ksplit<TileKSplit64x16> : launch_ksplit<TileKSplit64x32>;
-      launch(st, p, slot[0], Wb, Hb + r0 * p.d, rows, ia > 0 ? 1 : 0, ia + 2 >= p.n_chunks ? 1 : 0, nv, grad_loss, dHb + r0 * p.d, dW);
-    }
-    return check_launch();
-  }
-  for (int ia = 0; ia < p.n_chunks; ia += 2) {
-    const int ib = ia + 1;
-    dlogits(ia, rows_of(ia), slot[0]);
-    grad_h(ia, slot[0], slot[1]);
-    if (ib < p.n_chunks) {
-      dlogits(ib, rows_of(ib), slot[1]);
-      grad_w(ia, ib, p.C + rows_of(ib));
-      grad_h(ib, slot[1], slot[0]);
-    } else {
-      grad_w(ia, ia, rows_of(ia));
-    }
-  }
-  return check_launch();
+  return run_backward_orders(p, Hb, Wb, nv, grad_loss, ws, dHb, dW, st, [&](int64_t r0) { return CeGrad{labels + r0, lse + r0, (int)V, ignore_index}; },
+                             [](int64_t, int, int64_t, int, __bf16*, int) {});
 }
 
 mst_status mst_set_bwd_schedule(int32_t schedule) {
@@ -1239,3 +1268,5 @@ const char* mst_profile_kind_name(int kind) {
 }
 
 }  // extern "C"
+
+#include "mst_objective_api.hpp"      // shares the plans and the launches above

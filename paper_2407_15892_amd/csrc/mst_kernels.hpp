@@ -416,17 +416,27 @@ __device__ __forceinline__ void lse_epilogue(f32x4 (&acc)[kTA16][TB], const int*
   }
 }
 
+struct LseEpilogue {
+  const int* labels_c;
+  float2* part;
+  size_t part_stride;
+  float* tgt;
+  template <int TB>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+    lse_epilogue<TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
+  }
+};
+
 // ---------------------------------------------------------------------------
-// forward: logits tile + running log-sum-exp partials + target logit
+// forward: logits tile + running log-sum-exp partials + target logit (E: LseEpilogue, or that of another objective)
 //   A side = vocabulary (W rows), B side = chunk rows (H rows): a lane owns one
 //   row s and 32 consecutive vocabulary entries, so the row reduction is in-lane
 //   plus exchanges with the other three lane quarters and the other wave row.
 // ---------------------------------------------------------------------------
-template <bool kEven>
+template <bool kEven, class E>
 __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse(
-    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, const int* __restrict__ labels_c,
-    int rows, int d, int V, int n_st, int n_vt, float2* __restrict__ part, size_t part_stride,
-    float* __restrict__ tgt, int* __restrict__ queue, int queue_base) {
+    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, int rows, int d, int V, int n_st, int n_vt, E epilogue,
+    int* __restrict__ queue, int queue_base) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave >> 2, wb = wave & 3;
@@ -451,15 +461,15 @@ __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse(
   pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
   gemm_mainloop_pp<Tile16>(acc, pa, pb, smem, 0, d, wa, [&]() { if (queue) feed.resolve(); });
 
-  lse_epilogue<kTB16>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
+  epilogue.template operator()<kTB16>(acc, rows, V, vt, s0, wa, wb, lane, smem);
   }
 }
 
 // The same with tiles of 128 rows, one workgroup per tile, for problems whose 256-row tiles would leave half of the chip
 // idle or more.
+template <class E>
 __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse_rows128(
-    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, const int* __restrict__ labels_c,
-    int rows, int d, int V, int n_st, int n_vt, float2* __restrict__ part, size_t part_stride, float* __restrict__ tgt) {
+    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, int rows, int d, int V, int n_st, int n_vt, E epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef Tile16Rows128 T;
   static_assert(T::EA == kTile && T::TA == kTA16, "one pair per row and 256 vocabulary entries");
@@ -476,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse_rows128(
   pa.init(W + (size_t)v0 * d, d, V - v0, d, wave, lane, wa);
   pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
   gemm_mainloop_pp<T>(acc, pa, pb, smem, 0, d, wa);
-  lse_epilogue<T::TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
+  epilogue.template operator()<T::TB>(acc, rows, V, vt, s0, wa, wb, lane, smem);
 }
 
 // per row: combine the vocab-tile partials into lse and nll.  A workgroup owns 16 rows; its 16 groups of threads each fold
@@ -634,10 +644,34 @@ __global__ __launch_bounds__(1024) void k_finalize_loss(
 // vocabulary entries from there on, G column 0 is the window's first entry; v_base is that entry's absolute
 // index and V_all the whole vocabulary (both only for the labels).  The row-chunk schedule passes the whole
 // vocabulary (v_base = 0, V = V_all).
-template <bool kEven>
+//
+// What an entry is, the objective's gradient E says:
+//   load(s)                 what it needs of a row;  settle(row): the same, ready for use (behind all loads)
+//   with(row, f)            calls f with a function of a logit that gives the entry, the label's own term left out
+//   label(row)              the row's label, -1 for none;  label_term(row, z): what its entry is less by
+struct CeGrad {
+  const int* labels_c;
+  const float* lse_c;
+  int V_all, ignore_index;
+  struct Row { int y; float lse; };
+  __device__ __forceinline__ Row load(int s) const { return {labels_c[s], lse_c[s]}; }
+  // An ignored row takes lse = +infinity: every p is then exp2(-infinity) = 0 without a select per element, and
+  // its label is -1 so that nothing is subtracted.
+  __device__ __forceinline__ Row settle(Row r) const {
+    const bool valid = (r.y != ignore_index) && ((unsigned)r.y < (unsigned)V_all);
+    return {valid ? r.y : -1, valid ? r.lse : __builtin_inff()};
+  }
+  // z - lse is formed first and scaled afterwards: where a class dominates (z close to lse) the difference is exact,
+  // so p - 1 at a confidently predicted label keeps full precision, and a one-class vocabulary gives exactly 0.
+  __device__ __forceinline__ static float entry(const Row& r, float z) { return fast_exp2((z - r.lse) * kLog2e); }
+  template <class F>
+  __device__ __forceinline__ void with(const Row& r, F f) const { f([&r](float z) { return entry(r, z); }); }
+  __device__ __forceinline__ int label(const Row& r) const { return r.y; }
+  __device__ __forceinline__ float label_term(const Row&, float) const { return 1.0f; }
+};
+template <bool kEven, class E>
 __global__ __launch_bounds__(kThreads) void k_bwd_gemm_dlogits(
-    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, const int* __restrict__ labels_c,
-    const float* __restrict__ lse_c, int rows, int d, int V, int v_base, int V_all, int ignore_index, int n_st, int n_vt,
+    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, E grad, int rows, int d, int V, int v_base, int n_st, int n_vt,
     __bf16* __restrict__ G, int ldg) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   int vt, st;                                        // an XCD's resident workgroups: 4 vocabulary x 8 row tiles
@@ -672,38 +706,31 @@ __global__ __launch_bounds__(kThreads) void k_bwd_gemm_dlogits(
           for (int u = 0; u < kTB16; ++u) acc[t][u][r] = kMasked;
         }
   }
-  // Labels and log-sum-exps of all four rows first: read row by row, behind branches, they were eight loads that each
-  // waited for the one before.
-  int y_u[kTB16];
-  float lse_u[kTB16];
+  // What all four rows need first: read row by row, behind branches, they were eight loads that each waited for the one before.
+  typename E::Row row_u[kTB16];
 #pragma unroll
   for (int u = 0; u < kTB16; ++u) {
     const int s_local = s0 + wb * 64 + 16 * u + (lane & 15), s_in = s_local < rows ? s_local : rows - 1;
-    y_u[u] = labels_c[s_in];
-    lse_u[u] = lse_c[s_in];
+    row_u[u] = grad.load(s_in);
   }
 #pragma unroll
   for (int u = 0; u < kTB16; ++u) {
     const int row = wb * 64 + 16 * u + (lane & 15);
     const int s_local = s0 + row;
     if (s_local >= rows) continue;
-    const int y_abs = y_u[u];
-    const bool valid = (y_abs != ignore_index) && ((unsigned)y_abs < (unsigned)V_all);
-    // z - lse is formed first and scaled afterwards: where a class dominates (z close to lse) the difference is exact,
-    // so p - 1 at a confidently predicted label keeps full precision, and a one-class vocabulary gives exactly 0.
-    // An ignored row takes lse = +infinity: every p is then exp2(-infinity) = 0 without a select per element, and
-    // its label index is moved out of range so that nothing is subtracted.
-    const float lse_s = valid ? lse_u[u] : __builtin_inff();
-    const int y_lane = valid ? y_abs - v_base - va : -1;   // the label's position among this lane's 32 entries, if it is there
+    const typename E::Row of = grad.settle(row_u[u]);
+    const int y_abs = grad.label(of);
+    const int y_lane = y_abs >= 0 ? y_abs - v_base - va : -1;   // the label's position among this lane's 32 entries, if it is there
     char* srow = smem + row * kStageRow + (wa * 128 + 32 * (lane >> 4)) * 2;
+    grad.with(of, [&](auto entry) {
 #pragma unroll
-    for (int p = 0; p < kTA16 / 2; ++p) {            // tiles 2p and 2p + 1: entries va + 8p .. + 7
-      bf16x8 o;
+      for (int p = 0; p < kTA16 / 2; ++p) {            // tiles 2p and 2p + 1: entries va + 8p .. + 7
+        bf16x8 o;
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        o[e] = (__bf16)fast_exp2((acc[2 * p + (e >> 2)][u][e & 3] - lse_s) * kLog2e);
-      *reinterpret_cast<bf16x8*>(srow + 16 * p) = o;
-    }
+        for (int e = 0; e < 8; ++e) o[e] = (__bf16)entry(acc[2 * p + (e >> 2)][u][e & 3]);
+        *reinterpret_cast<bf16x8*>(srow + 16 * p) = o;
+      }
+    });
     // The label's entry, p - 1, is patched in afterwards by the one lane that holds it (a lane holds 32 of the V
     // entries of its row, so for most waves nobody does and the branch is skipped): a compare and a select per
     // element of every row would cost a third of this epilogue's instructions.
@@ -714,7 +741,7 @@ __global__ __launch_bounds__(kThreads) void k_bwd_gemm_dlogits(
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (4 * t + r == y_lane) z_y = acc[t][u][r];
-      *reinterpret_cast<__bf16*>(srow + 2 * y_lane) = (__bf16)(fast_exp2((z_y - lse_s) * kLog2e) - 1.0f);
+      grad.with(of, [&](auto entry) { *reinterpret_cast<__bf16*>(srow + 2 * y_lane) = (__bf16)(entry(z_y) - grad.label_term(of, z_y)); });
     }
   }
   __syncthreads();

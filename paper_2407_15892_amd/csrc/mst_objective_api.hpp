@@ -1,0 +1,289 @@
+// Host side of the LM head's other objectives (mst_objective.h): validation, workspace carving, launches.  Part of mst_api.hip,
+// whose plans, forward groups and backward orders these calls run with their own kernels for the logits.
+#include "../../include/mst_objective.h"
+
+#include <cmath>
+
+namespace {
+
+struct ObjPlan {
+  Plan p;
+  int K;
+  // forward workspace: the plain forward's (its nll: the rows' losses), then
+  size_t f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
+  size_t s_rows, s_rows2, s_index, s_at, s_total;      // of `saved`
+};
+
+// Byte ranges of a call's arguments: no output may overlap anything else.
+struct Ranges {
+  struct R { uintptr_t at; size_t bytes; bool out; };
+  R r[20];
+  int n = 0;
+  void add(const void* p, size_t bytes, bool out) {
+    if (p) r[n++] = {reinterpret_cast<uintptr_t>(p), bytes, out};
+  }
+  bool apart() const {
+    for (int i = 0; i < n; ++i)
+      for (int j = 0; j < i; ++j)
+        if ((r[i].out || r[j].out) && r[i].at < r[j].at + r[j].bytes && r[j].at < r[i].at + r[i].bytes) return false;
+    return true;
+  }
+};
+
+mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO, bool schedule = false) {
+  const mst_status s = make_plan(S, d, V, M, &o->p, forced, 0, schedule);
+  if (s != MST_OK) return s;
+  if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
+  o->p.streamed = 0;      // that order stores no dlogits to put the entries into
+  o->K = K;
+  const size_t rows = (size_t)o->p.fwd_group_rows, k = (size_t)K;
+  size_t off = o->p.f_total;
+  auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
+  o->f_count = take((size_t)S * 4);
+  o->f_part_label = K ? take((size_t)o->p.n_vt * rows * 4) : 0;
+  o->f_starts = K ? take((size_t)(o->p.n_vt + 1) * rows * 2) : 0;
+  o->f_index = K ? take(rows * k * 4) : 0;
+  o->f_logit = K ? take(rows * k * 4) : 0;
+  o->f_entry_y = K ? take(rows * k * 4) : 0;
+  o->f_info = K ? take(rows * 4) : 0;
+  o->f_total = off;
+  off = align_up(sizeof(ObjHeader), 256);
+  o->s_rows = take((size_t)S * sizeof(ObjRow));
+  o->s_rows2 = K ? take((size_t)S * sizeof(ObjRow2)) : 0;
+  o->s_index = K ? take((size_t)S * k * 4) : 0;
+  o->s_at = K ? take((size_t)S * k * 4) : 0;
+  o->s_total = off;
+  return MST_OK;
+}
+
+struct ObjCall {       // a forward call's arguments, of either objective
+  const void *H, *W;
+  const int32_t* labels;
+  const float* weights;
+  const int32_t* index;
+  const void* logits;
+  int32_t logits_bf16;
+  const float* teacher_lse;
+  int32_t ignore_index;
+  float softcap, label_coef, teacher_coef, temperature, z_coef;
+  int64_t divisor;
+  void* workspace;
+  size_t workspace_bytes;
+  void* saved;
+  size_t saved_bytes;
+  float *loss, *nll, *kd, *lse;
+  int64_t* n_valid;
+  void* stream;
+};
+
+mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
+  const Plan& p = o.p;
+  const size_t rows = (size_t)p.S, k = (size_t)o.K;
+  if (!c.H || !c.W || !c.loss || (o.K ? !c.index || !c.logits : !c.labels)) return MST_ERR_NULL_POINTER;
+  const bool good_cap = c.softcap == 0.f || (c.softcap >= 1e-3f && c.softcap <= 1e6f);
+  if (!good_cap || !std::isfinite(c.label_coef) || !std::isfinite(c.teacher_coef) || !std::isfinite(c.z_coef) ||
+      !(c.temperature >= 0.01f && c.temperature <= 100.f) || c.divisor < 0 || (!c.labels && (c.label_coef != 0.f || c.nll)))
+    return MST_ERR_BAD_ARGUMENT;
+  if (!c.workspace || c.workspace_bytes < o.f_total || (c.saved && c.saved_bytes < o.s_total)) return MST_ERR_WORKSPACE;
+  if (misaligned(c.H, 16) || misaligned(c.W, 16) || misaligned(c.workspace, 256) || misaligned(c.saved, 256) || misaligned(c.labels, 4) ||
+      misaligned(c.weights, 4) || misaligned(c.index, 4) || misaligned(c.logits, c.logits_bf16 ? 2 : 4) || misaligned(c.teacher_lse, 4) ||
+      misaligned(c.loss, 4) || misaligned(c.nll, 4) || misaligned(c.kd, 4) || misaligned(c.lse, 4) || misaligned(c.n_valid, 8))
+    return MST_ERR_ALIGNMENT;
+  Ranges ranges;
+  ranges.add(c.H, rows * p.d * 2, false);
+  ranges.add(c.W, (size_t)p.V * p.d * 2, false);
+  ranges.add(c.labels, rows * 4, false);
+  ranges.add(c.weights, rows * 4, false);
+  ranges.add(c.index, rows * k * 4, false);
+  ranges.add(c.logits, rows * k * (c.logits_bf16 ? 2 : 4), false);
+  ranges.add(c.teacher_lse, rows * 4, false);
+  ranges.add(c.workspace, o.f_total, true);
+  ranges.add(c.saved, o.s_total, true);
+  ranges.add(c.loss, 4, true);
+  ranges.add(c.nll, rows * 4, true);
+  ranges.add(c.kd, rows * 4, true);
+  ranges.add(c.lse, rows * 4, true);
+  ranges.add(c.n_valid, 8, true);
+  if (!ranges.apart()) return MST_ERR_BAD_ARGUMENT;
+  mst_status s = prepare_device();
+  if (s != MST_OK) return s;
+
+  hipStream_t st = reinterpret_cast<hipStream_t>(c.stream);
+  char* const ws = static_cast<char*>(c.workspace);
+  char* const saved = static_cast<char*>(c.saved);
+  const size_t stride = (size_t)p.fwd_group_rows;
+  // both log-sum-exps, at 1 / T for the teacher and at 1 for the labels, only where they differ
+  const bool two = o.K && c.labels && c.temperature != 1.f;
+  const float exponent = (float)(1.4426950408889634 / (double)c.temperature);
+  ObjEpilogue e = {};
+  e.part = reinterpret_cast<float2*>(ws + p.f_part);
+  e.part_label = two ? reinterpret_cast<float*>(ws + o.f_part_label) : nullptr;
+  e.part_stride = stride;
+  e.tgt = reinterpret_cast<float*>(ws + p.f_tgt);
+  e.K = o.K;
+  e.cap = c.softcap;
+  e.exponent = exponent;
+  e.exponent_label = kLog2e;
+  int* const index = reinterpret_cast<int*>(ws + o.f_index);
+  float* const logit = reinterpret_cast<float*>(ws + o.f_logit);
+  int* const info = reinterpret_cast<int*>(ws + o.f_info);
+  unsigned short* const starts = reinterpret_cast<unsigned short*>(ws + o.f_starts);
+  if (o.K) {
+    e.starts = starts;
+    e.index = index;
+    e.entry_y = reinterpret_cast<float*>(ws + o.f_entry_y);
+  }
+  ObjFinal f = {};
+  f.part = e.part; f.part_label = e.part_label; f.part_stride = stride;
+  f.n_vt = p.n_vt; f.V = (int)p.V; f.K = o.K;
+  f.tgt = e.tgt; f.ignore_index = c.ignore_index;
+  f.index = index; f.logit = logit; f.entry_y = e.entry_y; f.info = info;
+  f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t = (float)(1.0 / (double)c.temperature);
+  f.label_coef = c.label_coef; f.teacher_coef = c.teacher_coef; f.z_coef = c.z_coef; f.temperature = c.temperature;
+  float* const row_loss = reinterpret_cast<float*>(ws + p.f_nll);
+  int* const count = reinterpret_cast<int*>(ws + o.f_count);
+
+  s = run_forward_groups(
+      p, static_cast<const __bf16*>(c.H), static_cast<const __bf16*>(c.W), st, reinterpret_cast<Control*>(ws),
+      [&](int64_t g0) {
+        ObjEpilogue of = e;
+        of.labels_c = c.labels ? c.labels + g0 : nullptr;
+        return of;
+      },
+      [&](int64_t g0, int g_rows) {
+        if (!o.K) return;
+        const size_t from = (size_t)g0 * k;
+        const void* const logits = static_cast<const char*>(c.logits) + from * (c.logits_bf16 ? 2 : 4);
+        Scope sc(st, MST_K_LABEL_SCAN);
+        hipLaunchKernelGGL(k_entries, dim3((unsigned)((g_rows + kEntryRows - 1) / kEntryRows)), dim3(64 * kEntryRows), 0, st,
+                           c.index + from, logits, c.logits_bf16, g_rows, o.K, (int)p.V, p.n_vt, index, logit, info, starts, stride);
+      },
+      [&](int64_t g0, int g_rows) {
+        ObjFinal of = f;
+        of.rows = g_rows;
+        of.labels_c = c.labels ? c.labels + g0 : nullptr;
+        of.weights_c = c.weights ? c.weights + g0 : nullptr;
+        of.teacher_lse_c = c.teacher_lse ? c.teacher_lse + g0 : nullptr;
+        of.nll_c = c.nll ? c.nll + g0 : nullptr;
+        of.kd_c = c.kd ? c.kd + g0 : nullptr;
+        of.lse_c = c.lse ? c.lse + g0 : nullptr;
+        of.row_loss_c = row_loss + g0;
+        of.count_c = count + g0;
+        if (saved) {
+          of.rows_c = reinterpret_cast<ObjRow*>(saved + o.s_rows) + g0;
+          if (o.K) {
+            of.rows2_c = reinterpret_cast<ObjRow2*>(saved + o.s_rows2) + g0;
+            of.saved_index_c = reinterpret_cast<int*>(saved + o.s_index) + (size_t)g0 * k;
+            of.saved_at_c = reinterpret_cast<float*>(saved + o.s_at) + (size_t)g0 * k;
+          }
+        }
+        Scope sc(st, MST_K_LSE_FINALIZE);
+        hipLaunchKernelGGL(k_obj_finalize, dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of);
+      });
+  if (s != MST_OK) return s;
+  ObjHeader head = {};
+  head.cap = c.softcap;
+  head.exponent = exponent;
+  head.exponent_label = kLog2e;
+  head.two = two;
+  Scope sc(st, MST_K_LOSS_REDUCE);
+  hipLaunchKernelGGL(k_obj_loss, dim3(1), dim3(1024), 0, st, row_loss, count, (long long)p.S, (long long)c.divisor, head,
+                     reinterpret_cast<ObjHeader*>(saved), c.loss, reinterpret_cast<long long*>(c.n_valid));
+  return check_launch();
+}
+
+mst_status obj_backward(const ObjPlan& o, const void* H, const void* W, float grad_loss, const void* saved_in, size_t saved_bytes,
+                        void* workspace, size_t workspace_bytes, void* dH, float* dW, void* stream) {
+  const Plan& p = o.p;
+  if (!H || !W || !saved_in || !dH || !dW) return MST_ERR_NULL_POINTER;
+  if (!workspace || workspace_bytes < p.b_total || saved_bytes < o.s_total) return MST_ERR_WORKSPACE;
+  if (misaligned(H, 16) || misaligned(W, 16) || misaligned(dH, 16) || misaligned(dW, 16) || misaligned(workspace, 256) || misaligned(saved_in, 256))
+    return MST_ERR_ALIGNMENT;
+  Ranges ranges;
+  ranges.add(H, (size_t)p.S * p.d * 2, false);
+  ranges.add(W, (size_t)p.V * p.d * 2, false);
+  ranges.add(saved_in, o.s_total, false);
+  ranges.add(workspace, p.b_total, true);
+  ranges.add(dH, (size_t)p.S * p.d * 2, true);
+  ranges.add(dW, (size_t)p.V * p.d * 4, true);
+  if (!ranges.apart()) return MST_ERR_BAD_ARGUMENT;
+  mst_status s = prepare_device();
+  if (s != MST_OK) return s;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const char* const saved = static_cast<const char*>(saved_in);
+  const ObjHeader* const head = reinterpret_cast<const ObjHeader*>(saved);
+  const ObjRow* const rows = reinterpret_cast<const ObjRow*>(saved + o.s_rows);
+  const ObjRow2* const rows2 = o.K ? reinterpret_cast<const ObjRow2*>(saved + o.s_rows2) : nullptr;
+  return run_backward_orders(
+      p, static_cast<const __bf16*>(H), static_cast<const __bf16*>(W), &head->n_divisor, grad_loss, static_cast<char*>(workspace),
+      static_cast<__bf16*>(dH), dW, st,
+      [&](int64_t r0) { return ObjGrad{head, rows + r0, rows2 ? rows2 + r0 : nullptr}; },
+      [&](int64_t r0, int n_rows, int64_t v_base, int Vw, __bf16* G, int ldg) {
+        if (!o.K) return;
+        const size_t from = (size_t)r0 * o.K;
+        const long long n = (long long)n_rows * o.K;
+        Scope sc(st, MST_K_BWD_DH_REDUCE);
+        hipLaunchKernelGGL(k_obj_entries, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, reinterpret_cast<const int*>(saved + o.s_index) + from,
+                           reinterpret_cast<const float*>(saved + o.s_at) + from, n, o.K, (int)v_base, Vw, G, ldg);
+      });
+}
+
+}  // namespace
+
+extern "C" {
+
+mst_status mst_objective_bytes(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, size_t* fwd_bytes, size_t* bwd_bytes, size_t* saved_bytes) {
+  ObjPlan o;
+  const mst_status s = make_obj_plan(S, d, V, M, K, &o);
+  if (s != MST_OK) return s;
+  if (fwd_bytes) *fwd_bytes = o.f_total;
+  if (bwd_bytes) *bwd_bytes = o.p.b_total;
+  if (saved_bytes) *saved_bytes = o.s_total;
+  return MST_OK;
+}
+
+mst_status mst_lmhead_wce_fwd(const void* H, const void* W, const int32_t* labels, const float* weights, int64_t S, int64_t d, int64_t V,
+                              int32_t ignore_index, int32_t M, float softcap, float z_coef, int64_t divisor, void* workspace,
+                              size_t workspace_bytes, void* saved, size_t saved_bytes, float* loss, float* nll, float* lse, int64_t* n_valid,
+                              void* stream) {
+  ObjPlan o;
+  const mst_status s = make_obj_plan(S, d, V, M, 0, &o);
+  if (s != MST_OK) return s;
+  return obj_forward(o, {H, W, labels, weights, nullptr, nullptr, 0, nullptr, ignore_index, softcap, 1.f, 0.f, 1.f, z_coef, divisor, workspace,
+                         workspace_bytes, saved, saved_bytes, loss, nll, nullptr, lse, n_valid, stream});
+}
+
+mst_status mst_lmhead_wce_bwd(const void* H, const void* W, int64_t S, int64_t d, int64_t V, int32_t M, float grad_loss, const void* saved,
+                              size_t saved_bytes, void* workspace, size_t workspace_bytes, void* dH, float* dW, void* stream) {
+  ObjPlan o;
+  const mst_status s = make_obj_plan(S, d, V, M, 0, &o, t_bwd_schedule, true);
+  if (s != MST_OK) return s;
+  return obj_backward(o, H, W, grad_loss, saved, saved_bytes, workspace, workspace_bytes, dH, dW, stream);
+}
+
+mst_status mst_lmhead_distill_fwd(const void* H, const void* W, const int32_t* labels, const float* weights, const int32_t* teacher_index,
+                                  const void* teacher_logits, int32_t teacher_type, const float* teacher_lse, int64_t S, int64_t d, int64_t V,
+                                  int32_t K, int32_t ignore_index, int32_t M, float softcap, float label_coef, float teacher_coef,
+                                  float temperature, int64_t divisor, void* workspace, size_t workspace_bytes, void* saved, size_t saved_bytes,
+                                  float* loss, float* nll, float* kd, int64_t* n_valid, void* stream) {
+  if (K < 1) return MST_ERR_BAD_SHAPE;
+  ObjPlan o;
+  const mst_status s = make_obj_plan(S, d, V, M, K, &o);
+  if (s != MST_OK) return s;
+  if (teacher_type != 0 && teacher_type != 1) return MST_ERR_BAD_ARGUMENT;
+  return obj_forward(o, {H, W, labels, weights, teacher_index, teacher_logits, teacher_type == 0, teacher_lse, ignore_index, softcap, label_coef,
+                         teacher_coef, temperature, 0.f, divisor, workspace, workspace_bytes, saved, saved_bytes, loss, nll, kd, nullptr, n_valid,
+                         stream});
+}
+
+mst_status mst_lmhead_distill_bwd(const void* H, const void* W, int64_t S, int64_t d, int64_t V, int32_t K, int32_t M, float grad_loss,
+                                  const void* saved, size_t saved_bytes, void* workspace, size_t workspace_bytes, void* dH, float* dW,
+                                  void* stream) {
+  if (K < 1) return MST_ERR_BAD_SHAPE;
+  ObjPlan o;
+  const mst_status s = make_obj_plan(S, d, V, M, K, &o, t_bwd_schedule, true);
+  if (s != MST_OK) return s;
+  return obj_backward(o, H, W, grad_loss, saved, saved_bytes, workspace, workspace_bytes, dH, dW, stream);
+}
+
+}  // extern "C"

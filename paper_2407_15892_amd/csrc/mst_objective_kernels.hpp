@@ -1,0 +1,603 @@
+// Device code of the LM head's other objectives (mst_objective.h): cross-entropy of capped logits with token weights, and
+// distillation from a teacher's largest logits.  The contractions, their tiles and their launches are those of the plain
+// cross-entropy; what differs is what is taken from a tile of logits and what the logits' gradient is.
+//
+// Notation of a row: z logits, y = c tanh(z / c) (y = z without a cap), T the temperature, "entries" the vocabulary entries that
+// the teacher gives, "others" the rest.
+//
+//   forward   k_entries        the teacher's entries of every row in ascending order, and where each vocabulary tile's begin
+//             (logits)         ObjEpilogue: the label's y and the entries' y out of the accumulators; partial log-sum-exps of the
+//                              others alone, at 1 / T and, where a row needs both, at 1
+//             k_obj_finalize   log-sum-exps, losses, what the backward needs of each row and at each entry
+//             k_obj_loss       the loss, in a fixed order
+//   backward  (logits again)   ObjGrad: every entry of a row as two coefficients times exponentials
+//             k_obj_entries    the teacher's entries put into the block of dlogits
+//
+// The others' log-sum-exp is formed without the entries, not as a difference: where the student gives nearly everything to the
+// entries a difference of float32 numbers would leave nothing of the share of the others.
+#pragma once
+#include "mst_small_kernels.hpp"
+
+namespace mst {
+
+constexpr int kMaxEntries = 256;            // of a row of the teacher
+constexpr int kNoEntry = 0x7fffffff;        // sorts behind every entry
+
+// What the backward call needs, at the front of the caller's `saved`.
+struct ObjHeader {
+  long long n_valid;                        // rows that count; -1: an index out of range
+  long long n_divisor;                      // what the sums are divided by (-1 again, 0 where no row counts)
+  float cap, exponent, exponent_label;      // log2(e) / T of the (first) exponential, log2(e) of the second
+  int two;                                  // rows have two exponentials
+};
+
+// Of one row, for the backward: the gradient of y_v is
+//   at * exp((y_v - base) / T) + row2.at * exp(y_v - row2.base) - [v == label] label_term
+// at every entry that is not the teacher's; the second exponential only where there are two (ObjRow2).
+struct ObjRow { float base, at, label_term; int label; };
+struct ObjRow2 { float base, at; };
+
+// y = c tanh(z / c) and dy/dz = 1 - tanh^2, by u = 1 / (1 + exp(2 |z| / c)), which is at most 1/2: tanh = sign(z) (1 - 2 u) and
+// 1 - tanh^2 = 4 u (1 - u), without cancellation in the second at any z.
+__device__ __forceinline__ float cap_u(float z, float scale /* 2 log2(e) / c */) {
+  return __builtin_amdgcn_rcpf(1.f + fast_exp2(__builtin_fabsf(z) * scale));
+}
+__device__ __forceinline__ float capped(float z, float cap, float scale) {
+  return __builtin_copysignf(cap - 2.f * cap * cap_u(z, scale), z);
+}
+
+// merge_lse for sums of exp2(exponent (y - m)), and a second sum beside the first at another exponent
+__device__ __forceinline__ void merge_sums(float& m, float& l, float& k, float m2, float l2, float k2, float exponent, float exponent_label, bool two) {
+  const float mm = fmaxf(m, m2), a = m - mm, b = m2 - mm;
+  l = __builtin_fmaf(l, fast_exp2(a * exponent), l2 * fast_exp2(b * exponent));
+  if (two) k = __builtin_fmaf(k, fast_exp2(a * exponent_label), k2 * fast_exp2(b * exponent_label));
+  m = mm;
+}
+
+// ---------------------------------------------------------------------------
+// forward epilogue
+// ---------------------------------------------------------------------------
+struct ObjEpilogue {
+  const int* labels_c;                 // null: none
+  float2* part;                        // [n_vt][part_stride] (maximum, sum) of the others
+  float* part_label;                   // the sum at the second exponent; null: rows have one
+  size_t part_stride;
+  float* tgt;                          // y of the label
+  const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile; null: no teacher
+  const int* index;                    // [rows][K] ascending
+  float* entry_y;                      // [rows][K] y of the entries
+  int K;
+  float cap, exponent, exponent_label;
+
+  template <int TB>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+    const int v0 = vt * kTile;
+    const int g = lane >> 4, c = lane & 15;
+    const int va = v0 + wa * 128 + 32 * g;             // a lane's 32 consecutive entries of each of its TB rows
+    int y_u[TB], from[TB], to[TB];                     // on their way meanwhile
+#pragma unroll
+    for (int u = 0; u < TB; ++u) {
+      const int s_local = s0 + wb * (16 * TB) + 16 * u + c, s_in = s_local < rows ? s_local : rows - 1;
+      y_u[u] = labels_c ? labels_c[s_in] : -1;
+      from[u] = starts ? starts[(size_t)vt * part_stride + s_in] : 0;
+      to[u] = starts ? starts[(size_t)(vt + 1) * part_stride + s_in] : 0;
+    }
+    if (cap > 0.f) {
+      const float scale = 2.f * kLog2e / cap;
+#pragma unroll
+      for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+        for (int u = 0; u < TB; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[t][u][r] = capped(acc[t][u][r], cap, scale);
+    }
+#pragma unroll
+    for (int u = 0; u < TB; ++u) {
+      const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+      const int y = s_local < rows ? y_u[u] : -1;
+      const int rel = y - (v0 + wa * 128);
+      if (rel >= 0 && rel < 128 && y < V && (rel >> 5) == g) {
+        const int t_sel = (rel & 31) >> 2, r_sel = rel & 3;
+        float val = 0.f;
+#pragma unroll
+        for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t == t_sel && r == r_sel) val = acc[t][u][r];
+        tgt[s_local] = val;
+      }
+    }
+    if (starts) {
+#pragma unroll
+      for (int u = 0; u < TB; ++u) {
+        const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+        const int end = s_local < rows ? to[u] : 0;
+        unsigned mine = 0;                             // bit i: entry va + i is the teacher's
+        int first = 0;                                 // place of the lowest of them in the row's list
+        for (int e = from[u]; e < end; ++e) {
+          const int rel = index[(size_t)s_local * K + e] - va;
+          if ((unsigned)rel < 32u) {
+            if (!mine) first = e;
+            mine |= 1u << rel;
+          }
+        }
+        if (!__any(mine != 0)) continue;
+#pragma unroll
+        for (int t = 0; t < kTA16; ++t) {
+          if (!__any((mine >> (4 * t)) & 15u)) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((mine >> (4 * t + r)) & 1u) {
+              entry_y[(size_t)s_local * K + first + __builtin_popcount(mine & ((1u << (4 * t + r)) - 1u))] = acc[t][u][r];
+              acc[t][u][r] = kMasked;
+            }
+        }
+      }
+    }
+    if (v0 + kTile > V) {
+#pragma unroll
+      for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (va + 4 * t + r >= V) {
+#pragma unroll
+            for (int u = 0; u < TB; ++u) acc[t][u][r] = kMasked;
+          }
+    }
+    const bool two = part_label != nullptr;
+    float m_u[TB], l_u[TB], k_u[TB];
+#pragma unroll
+    for (int u = 0; u < TB; ++u) {
+      float m = kMasked, l = 0.f, k = 0.f;
+#pragma unroll
+      for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][u][r]);
+#pragma unroll
+      for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
+      if (two) {
+#pragma unroll
+        for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
+      }
+#pragma unroll
+      for (int o = 16; o <= 32; o <<= 1)
+        merge_sums(m, l, k, __shfl_xor(m, o), __shfl_xor(l, o), two ? __shfl_xor(k, o) : 0.f, exponent, exponent_label, two);
+      m_u[u] = m; l_u[u] = l; k_u[u] = k;
+    }
+    // the main loop ended with a barrier, LDS is free
+    float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves
+    if (wa == 1 && lane < 16) {
+#pragma unroll
+      for (int u = 0; u < TB; ++u) {
+        float* at = xch + ((wb * TB + u) * 16 + lane) * 3;
+        at[0] = m_u[u]; at[1] = l_u[u]; at[2] = k_u[u];
+      }
+    }
+    __syncthreads();
+    if (wa == 0 && lane < 16) {
+#pragma unroll
+      for (int u = 0; u < TB; ++u) {
+        const float* at = xch + ((wb * TB + u) * 16 + lane) * 3;
+        merge_sums(m_u[u], l_u[u], k_u[u], at[0], at[1], at[2], exponent, exponent_label, two);
+        const int s_local = s0 + wb * (16 * TB) + 16 * u + lane;
+        if (s_local >= rows) continue;
+        part[(size_t)vt * part_stride + s_local] = make_float2(m_u[u], l_u[u]);
+        if (two) part_label[(size_t)vt * part_stride + s_local] = k_u[u];
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// The teacher's entries of a group of rows in ascending order.  A wave takes a row: every lane counts, for its (up to four)
+// entries, those that come before them.  An index below 0 is no entry; one that comes twice counts once, with the logit it has
+// first; one at or behind V makes the row bad.
+//   index, logit [rows][K] (float32), the rest of a row kNoEntry; info[row] = entries, or -1
+//   starts [n_vt + 1][stride]
+// ---------------------------------------------------------------------------
+constexpr int kEntryRows = 16;              // of a workgroup, one wave each: 32-byte pieces of starts
+__global__ __launch_bounds__(64 * kEntryRows) void k_entries(
+    const int* __restrict__ index_in, const void* __restrict__ logit_in, int logit_bf16, int rows, int K, int V, int n_vt,
+    int* __restrict__ index, float* __restrict__ logit, int* __restrict__ info, unsigned short* __restrict__ starts, size_t stride) {
+  __shared__ __attribute__((aligned(16))) int key_sh[kEntryRows][kMaxEntries];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int s = blockIdx.x * kEntryRows + w, s_in = s < rows ? s : rows - 1;
+  constexpr int kPer = kMaxEntries / 64;
+  int* const key = key_sh[w];
+  const int per = (K + 63) / 64;
+  int mine[kPer], rank[kPer];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = lane + 64 * i;
+    int v = kNoEntry;
+    if (e < K) {
+      v = index_in[(size_t)s_in * K + e];
+      if (v >= V) bad = true;
+      if ((unsigned)v >= (unsigned)V) v = kNoEntry;
+    }
+    mine[i] = v;
+    key[e] = v;
+  }
+  bad = __any(bad);
+  __syncthreads();
+  const int K4 = (K + 3) / 4;
+  // one that came before: not an entry any more
+  for (int j = 0; j < K4; ++j) {
+    const int4 q = *reinterpret_cast<const int4*>(key + 4 * j);
+    const int of[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i < per) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          if (of[b] == mine[i] && 4 * j + b < lane + 64 * i) mine[i] = kNoEntry;
+      }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) { key[lane + 64 * i] = mine[i]; rank[i] = 0; }
+  __syncthreads();
+  for (int j = 0; j < K4; ++j) {
+    const int4 q = *reinterpret_cast<const int4*>(key + 4 * j);
+    const int of[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i < per) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) rank[i] += of[b] < mine[i] || (of[b] == mine[i] && 4 * j + b < lane + 64 * i);
+      }
+  }
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = lane + 64 * i;
+    n += __builtin_popcountll(__ballot(e < K && mine[i] != kNoEntry));
+    key[e] = kNoEntry;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = lane + 64 * i;
+    if (e >= K) continue;
+    key[rank[i]] = mine[i];
+    if (s >= rows) continue;
+    const size_t to = (size_t)s * K + rank[i];
+    index[to] = mine[i];
+    const size_t at = (size_t)s * K + e;
+    logit[to] = logit_bf16 ? (float)static_cast<const __bf16*>(logit_in)[at] : static_cast<const float*>(logit_in)[at];
+  }
+  if (lane == 0 && s < rows) info[s] = bad ? -1 : n;
+  __syncthreads();
+  // entries before vocabulary entry 256 vt, by bisection
+  const int r = threadIdx.x % kEntryRows, row = blockIdx.x * kEntryRows + r;
+  if (row >= rows) return;
+  for (int vt = threadIdx.x / kEntryRows; vt <= n_vt; vt += 64) {
+    const int v = vt < n_vt ? vt * kTile : kNoEntry;
+    int lo = 0, hi = K;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (key_sh[r][mid] < v) lo = mid + 1; else hi = mid;
+    }
+    starts[(size_t)vt * stride + row] = (unsigned short)lo;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Per row: log-sum-exps, losses, and what the backward needs.  A workgroup owns 16 rows; first its 16 groups of threads each
+// fold every 16th vocabulary tile of each row (as k_lse_finalize), then 16 neighbouring lanes have a row each.  All sums in a
+// fixed order.
+// ---------------------------------------------------------------------------
+struct ObjFinal {
+  const float2* part;
+  const float* part_label;
+  size_t part_stride;
+  int n_vt, rows, V, K;
+  const float* tgt;
+  const int* labels_c;
+  const float* weights_c;
+  int ignore_index;
+  const int* index;                   // [rows][K] and their logits and y, ascending
+  const float* logit;
+  const float* entry_y;
+  const int* info;
+  const float* teacher_lse_c;
+  float cap, exponent, exponent_label, inv_t;
+  float label_coef, teacher_coef, z_coef, temperature;
+  float *nll_c, *kd_c, *lse_c;        // outputs, each may be null
+  float* row_loss_c;
+  int* count_c;                       // 1: the row counts, -1: an index out of range
+  ObjRow* rows_c;                     // null: no backward follows
+  ObjRow2* rows2_c;
+  int* saved_index_c;
+  float* saved_at_c;
+};
+constexpr int kObjRows = 16, kObjGroups = 16;
+
+__device__ __forceinline__ float max16(float x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+template <class X> __device__ __forceinline__ X sum16(X x) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+__global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal a) {
+  __shared__ float sh[kObjRows][kObjGroups][3];
+  const bool two = a.part_label != nullptr;
+  {
+    const int r = threadIdx.x & (kObjRows - 1), g = threadIdx.x / kObjRows;
+    const int s = blockIdx.x * kObjRows + r;
+    float m = kMasked, l = 0.f, k = 0.f;
+    if (s < a.rows) {
+      constexpr int kBatch = 16;
+      for (int v0 = g; v0 < a.n_vt; v0 += kBatch * kObjGroups) {
+        float2 p[kBatch];
+        float q[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int vt = v0 + i * kObjGroups;
+          p[i] = vt < a.n_vt ? a.part[(size_t)vt * a.part_stride + s] : make_float2(kMasked, 0.f);
+          q[i] = two && vt < a.n_vt ? a.part_label[(size_t)vt * a.part_stride + s] : 0.f;
+        }
+        float mm = m;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) mm = fmaxf(mm, p[i].x);
+        l *= fast_exp2((m - mm) * a.exponent);
+        k *= fast_exp2((m - mm) * a.exponent_label);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) l = __builtin_fmaf(p[i].y, fast_exp2((p[i].x - mm) * a.exponent), l);
+        if (two) {
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) k = __builtin_fmaf(q[i], fast_exp2((p[i].x - mm) * a.exponent_label), k);
+        }
+        m = mm;
+      }
+    }
+    sh[r][g][0] = m; sh[r][g][1] = l; sh[r][g][2] = k;
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  const int s = blockIdx.x * kObjRows + r;
+  const bool in = s < a.rows;
+  const int s_in = in ? s : a.rows - 1;
+  // the others
+  const float m_lane = sh[r][lane][0];
+  const float m = max16(m_lane);
+  const float l = sum16(sh[r][lane][1] * fast_exp2((m_lane - m) * a.exponent));
+  const float k = two ? sum16(sh[r][lane][2] * fast_exp2((m_lane - m) * a.exponent_label)) : 0.f;
+  const bool others = m > 0.5f * kMasked;                        // there are some
+
+  // the entries
+  const int n = a.K ? max(a.info[s_in], 0) : 0;
+  const bool bad_entry = a.K && a.info[s_in] < 0;
+  const size_t at0 = (size_t)s_in * a.K;
+  float my = kMasked, mt = kMasked;
+  for (int e = lane; e < n; e += 16) {
+    my = fmaxf(my, a.entry_y[at0 + e]);
+    mt = fmaxf(mt, a.logit[at0 + e]);
+  }
+  my = max16(my);
+  mt = max16(mt);
+  float ly = 0.f, ky = 0.f, lt = 0.f;
+  for (int e = lane; e < n; e += 16) {
+    const float y = a.entry_y[at0 + e] - my;
+    ly += fast_exp2(y * a.exponent);
+    if (two) ky += fast_exp2(y * a.exponent_label);
+    lt += expf((a.logit[at0 + e] - mt) * a.inv_t);
+  }
+  ly = sum16(ly);
+  ky = sum16(ky);
+  lt = sum16(lt);
+
+  // log-sum-exps, as maximum and logarithm of the sum: at 1 / T (m_all / T + log_all), and at 1 (m_all + log_label)
+  const float m_all = fmaxf(m, my);
+  const float l_all = l * fast_exp2((m - m_all) * a.exponent) + ly * fast_exp2((my - m_all) * a.exponent);
+  const float k_all = two ? k * fast_exp2((m - m_all) * a.exponent_label) + ky * fast_exp2((my - m_all) * a.exponent_label) : l_all;
+  const float log_all = logf(l_all), log_label = two ? logf(k_all) : log_all;
+  const float lse = m_all + log_label;
+  const float lse_t = m_all * a.inv_t + log_all;
+  const float base = m + a.temperature * logf(l);                // T times the others' log-sum-exp at 1 / T
+  // log of the others' share, with the two logarithms of sums and not with those of the log-sum-exps
+  const float log_share = (m - m_all) * a.inv_t + (logf(l) - log_all);
+
+  const float weight = a.weights_c ? a.weights_c[s_in] : 1.f;
+  const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
+  const bool labelled = a.labels_c && y != a.ignore_index;
+  const bool valid = labelled && (unsigned)y < (unsigned)a.V;
+  const float nll = valid ? (m_all - a.tgt[s_in]) + log_label : 0.f;
+
+  // the teacher's shares; `rest`: what it leaves to the others
+  const bool given = a.teacher_lse_c != nullptr;
+  const bool taught = n > 0 && (given || !(mt <= 0.5f * kMasked));          // true for NaN
+  const float lse_teacher = given ? a.teacher_lse_c[s_in] : mt * a.inv_t + logf(lt);
+  double sum_q = 0.0;
+  float kd = 0.f;
+  for (int e = lane; e < n; e += 16) {
+    // relative to the largest logits, so that equal distributions leave nothing
+    const float log_q = given ? a.logit[at0 + e] * a.inv_t - lse_teacher : (a.logit[at0 + e] - mt) * a.inv_t - logf(lt);
+    const float log_p = (a.entry_y[at0 + e] - m_all) * a.inv_t - log_all;
+    const float q = expf(log_q);
+    sum_q += (double)q;
+    if (!(q == 0.f)) kd += q * (log_q - log_p);
+  }
+  sum_q = sum16(sum_q);
+  kd = sum16(kd);
+  const float total_q = (float)sum_q;
+  const double rest_64 = given && others ? 1.0 - sum_q : 0.0;
+  const float rest = rest_64 > 0.0 || rest_64 != rest_64 ? (float)rest_64 : 0.f;
+  if (!(rest == 0.f)) kd += rest * (logf(rest) - log_share);
+  if (!taught) kd = 0.f;
+  const float on_kd = taught && weight != 0.f ? weight * a.teacher_coef * a.temperature : 0.f;
+  const float on_label = valid && weight != 0.f ? weight * a.label_coef : 0.f;
+  const float on_p = on_label + (valid && weight != 0.f ? 2.f * weight * a.z_coef * lse : 0.f);
+  if (in && lane == 0) {
+    if (a.nll_c) a.nll_c[s] = nll;
+    if (a.kd_c) a.kd_c[s] = kd;
+    if (a.lse_c) a.lse_c[s] = lse;
+    float loss = 0.f;
+    if (weight != 0.f) {
+      if (valid) loss += weight * (a.label_coef * nll + a.z_coef * lse * lse);
+      if (taught) loss += weight * a.teacher_coef * a.temperature * a.temperature * kd;
+    }
+    a.row_loss_c[s] = loss;
+    a.count_c[s] = bad_entry || (labelled && !valid) ? -1 : valid || taught ? 1 : 0;
+  }
+  if (!a.rows_c || !in) return;
+  const float share = expf(log_share);                           // of the others at 1 / T
+  const float kd_others = on_kd != 0.f ? on_kd * ((total_q + rest) * share - rest) : 0.f;
+  if (lane == 0) {
+    ObjRow row;
+    ObjRow2 row2 = {__builtin_inff(), 0.f};
+    row.label = valid && weight != 0.f ? y : -1;
+    row.label_term = on_label;
+    if (two) {
+      row.base = base;
+      row.at = kd_others;
+      row2.base = lse;
+      row2.at = on_p;
+      if (on_p == 0.f) row2.base = __builtin_inff();
+    } else if (a.K) {
+      row.base = base;
+      row.at = kd_others + on_p * share;
+    } else {
+      row.base = lse;
+      row.at = on_p;
+    }
+    if (!others || row.at == 0.f) row.base = __builtin_inff(), row.at = 0.f;     // exp2 of -infinity: zeros whatever the logits
+    a.rows_c[s] = row;
+    if (a.rows2_c) a.rows2_c[s] = row2;
+  }
+  if (!a.K) return;
+  for (int e = lane; e < a.K; e += 16) {
+    const int v = a.index[at0 + e];
+    float x = 0.f;
+    if (e < n) {
+      const float ye = a.entry_y[at0 + e];
+      const float log_q = given ? a.logit[at0 + e] * a.inv_t - lse_teacher : (a.logit[at0 + e] - mt) * a.inv_t - logf(lt);
+      if (on_kd != 0.f) x = on_kd * (expf((ye - m_all) * a.inv_t - log_all) * (total_q + rest) - expf(log_q));
+      if (on_p != 0.f) x += on_p * expf((ye - m_all) - log_label);
+      if (valid && v == y) x -= on_label;
+      if (a.cap > 0.f) {
+        const float h = ye / a.cap;
+        x *= (1.f - h) * (1.f + h);
+      }
+    }
+    a.saved_index_c[at0 + e] = v;
+    a.saved_at_c[at0 + e] = x;
+  }
+}
+
+// loss = sum of the rows' / divisor, in a fixed order in 64 bits, and the header of `saved`.  One workgroup.
+__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S,
+                                                   long long divisor, ObjHeader head, ObjHeader* __restrict__ saved,
+                                                   float* __restrict__ loss, long long* __restrict__ n_valid_out) {
+  __shared__ double sh[16];
+  __shared__ long long sh_n[16];
+  __shared__ int sh_bad[16];
+  double a = 0.0;
+  long long n = 0;
+  int bad = 0;
+  for (long long i0 = threadIdx.x; i0 < S; i0 += 8 * 1024) {
+    float x[8];
+    int c[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const long long i = i0 + k * 1024;
+      x[k] = i < S ? row_loss[i] : 0.f;
+      c[k] = i < S ? count[i] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      a += (double)x[k];
+      n += c[k] > 0;
+      bad |= c[k] < 0;
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    a += __shfl_xor(a, o);
+    n += __shfl_xor(n, o);
+    bad |= __shfl_xor(bad, o);
+  }
+  const int w = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) { sh[w] = a; sh_n[w] = n; sh_bad[w] = bad; }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  a = 0.0; n = 0; bad = 0;
+  for (int i = 0; i < 16; ++i) { a += sh[i]; n += sh_n[i]; bad |= sh_bad[i]; }
+  head.n_valid = bad ? -1 : n;
+  head.n_divisor = bad ? -1 : n == 0 ? 0 : divisor > 0 ? divisor : n;
+  *loss = bad ? __builtin_nanf("") : n == 0 ? 0.f : (float)(a / (double)head.n_divisor);
+  if (n_valid_out) *n_valid_out = head.n_valid;
+  if (saved) *saved = head;
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+struct ObjGrad {
+  const ObjHeader* head;
+  const ObjRow* rows;
+  const ObjRow2* rows2;              // read where head->two
+  struct Row { ObjRow a; ObjRow2 b; };
+  __device__ __forceinline__ Row load(int s) const {
+    Row r;
+    r.a = rows[s];
+    r.b = head->two ? rows2[s] : ObjRow2{0.f, 0.f};
+    return r;
+  }
+  __device__ __forceinline__ Row settle(const Row& r) const { return r; }
+  __device__ __forceinline__ int label(const Row& r) const { return r.a.label; }
+  __device__ __forceinline__ float label_term(const Row& r, float z) const {
+    if (!(head->cap > 0.f)) return r.a.label_term;
+    const float u = cap_u(z, 2.f * kLog2e / head->cap);
+    return r.a.label_term * (4.f * u * (1.f - u));
+  }
+  template <class F>
+  __device__ __forceinline__ void with(const Row& r, F f) const {
+    const float c1 = head->exponent, c2 = head->exponent_label, cap = head->cap;
+    if (cap > 0.f) {
+      const float scale = 2.f * kLog2e / cap;
+      auto split = [=](float z, float& y) {
+        const float u = cap_u(z, scale);
+        y = __builtin_copysignf(cap - 2.f * cap * u, z);
+        return 4.f * u * (1.f - u);
+      };
+      if (head->two)
+        f([&](float z) {
+          float y;
+          const float slope = split(z, y);
+          return slope * (r.a.at * fast_exp2((y - r.a.base) * c1) + r.b.at * fast_exp2((y - r.b.base) * c2));
+        });
+      else
+        f([&](float z) {
+          float y;
+          const float slope = split(z, y);
+          return slope * (r.a.at * fast_exp2((y - r.a.base) * c1));
+        });
+    } else if (head->two) {
+      f([&](float z) { return r.a.at * fast_exp2((z - r.a.base) * c1) + r.b.at * fast_exp2((z - r.b.base) * c2); });
+    } else {
+      f([&](float z) { return r.a.at * fast_exp2((z - r.a.base) * c1); });
+    }
+  }
+};
+
+// The teacher's entries of `rows` rows that lie in a window of the vocabulary, into its dlogits.
+__global__ __launch_bounds__(256) void k_obj_entries(const int* __restrict__ index, const float* __restrict__ at, long long n, int K,
+                                                     int v_base, int V, __bf16* __restrict__ G, int ldg) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int v = index[i] - v_base;
+  if ((unsigned)v < (unsigned)V) G[(size_t)(i / K) * ldg + v] = (__bf16)at[i];
+}
+
+}  // namespace mst

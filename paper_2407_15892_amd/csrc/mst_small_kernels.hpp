@@ -37,10 +37,9 @@ inline double small_launch_us(double tiles, double ksteps) {
 // holds one (max, sum-exp) pair per row and 256 entries; every pair is formed in the same order as by k_fwd_gemm_lse, so
 // lse and loss keep their bits.
 // ---------------------------------------------------------------------------
-template <class C>
+template <class C, class E>
 __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_lse_small(
-    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, const int* __restrict__ labels_c,
-    int rows, int d, int V, int n_st, int n_vt, float2* __restrict__ part, size_t part_stride, float* __restrict__ tgt) {
+    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, int rows, int d, int V, int n_st, int n_vt, E epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   static_assert(C::EA == kTile && C::TA == kTA16, "one pair per row and 256 vocabulary entries");
   int vt, st;
@@ -59,16 +58,15 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_ls
     pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
     gemm_mainloop_small<C>(acc, pa, pb, smem, 0, d);
   }
-  lse_epilogue<C::TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
+  epilogue.template operator()<C::TB>(acc, rows, V, vt, s0, wa, wb, lane, smem);
 }
 
 // ---------------------------------------------------------------------------
 // backward 1: recomputed logits -> softmax - onehot, as k_bwd_gemm_dlogits (whole vocabulary)
 // ---------------------------------------------------------------------------
-template <class C>
+template <class C, class E>
 __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dlogits_small(
-    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, const int* __restrict__ labels_c,
-    const float* __restrict__ lse_c, int rows, int d, int V, int ignore_index, int n_st, int n_vt,
+    const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, E grad, int rows, int d, int V, int n_st, int n_vt,
     __bf16* __restrict__ G, int ldg) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   int vt, st;
@@ -92,37 +90,36 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dl
   // now; rows padded by 16 bytes) as whole rows
   constexpr int kPer = 4 * C::TA, kStageRow = C::EA * 2 + 16;
   const int va_tile = wa * (16 * C::TA) + kPer * (lane >> 4), va = v0 + va_tile;
-  int y_u[C::TB];                       // all loads before the first is waited for
-  float lse_u[C::TB];
+  typename E::Row row_u[C::TB];         // all loads before the first is waited for
 #pragma unroll
   for (int u = 0; u < C::TB; ++u) {
     const int s_local = s0 + wb * (16 * C::TB) + 16 * u + (lane & 15), s_in = s_local < rows ? s_local : rows - 1;
-    y_u[u] = labels_c[s_in];
-    lse_u[u] = lse_c[s_in];
+    row_u[u] = grad.load(s_in);
   }
 #pragma unroll
   for (int u = 0; u < C::TB; ++u) {
     const int row = wb * (16 * C::TB) + 16 * u + (lane & 15);
     const int s_local = s0 + row;
     if (s_local >= rows) continue;
-    const int y_abs = y_u[u];
-    const bool valid = (y_abs != ignore_index) && ((unsigned)y_abs < (unsigned)V);
-    const float lse_s = valid ? lse_u[u] : __builtin_inff();           // an ignored row: every p is exp2(-infinity)
-    const int y_lane = valid ? y_abs - va : -1;
+    const typename E::Row of = grad.settle(row_u[u]);
+    const int y_abs = grad.label(of);
+    const int y_lane = y_abs >= 0 ? y_abs - va : -1;
     char* srow = smem + row * kStageRow + va_tile * 2;
+    grad.with(of, [&](auto entry) {
 #pragma unroll
-    for (int p = 0; p < C::TA / 2; ++p) {
-      bf16x8 o;
+      for (int p = 0; p < C::TA / 2; ++p) {
+        bf16x8 o;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float z = acc[2 * p + (e >> 2)][u][e & 3];
-        float x = fast_exp2((z - lse_s) * kLog2e);
-        if (va + 8 * p + e >= V) x = 0.f;
-        if (8 * p + e == y_lane) x -= 1.0f;
-        o[e] = (__bf16)x;
+        for (int e = 0; e < 8; ++e) {
+          const float z = acc[2 * p + (e >> 2)][u][e & 3];
+          float x = entry(z);
+          if (va + 8 * p + e >= V) x = 0.f;
+          if (8 * p + e == y_lane) x -= grad.label_term(of, z);
+          o[e] = (__bf16)x;
+        }
+        *reinterpret_cast<bf16x8*>(srow + 16 * p) = o;
       }
-      *reinterpret_cast<bf16x8*>(srow + 16 * p) = o;
-    }
+    });
   }
   __syncthreads();
   constexpr int kLanesPerRow = C::EA / 8, kRowsPerPass = C::kThreads / kLanesPerRow;

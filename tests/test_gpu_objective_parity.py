@@ -1,0 +1,85 @@
+"""The LM head's weighted cross-entropy and distillation on the GPU against their definition in 64 bits, element by element."""
+import numpy as np
+import pytest
+
+from tests.objective_gpu_harness import Problem, Run, check
+
+pytestmark = pytest.mark.gpu
+
+WCE = [
+    # S, d, V, options
+    (1, 8, 1, dict()),                                              # one class: everything is 0
+    (1, 64, 300, dict(softcap=30.0)),
+    (3, 16, 2, dict(softcap=5.0, weights=True)),
+    (37, 72, 256, dict(z_coef=1e-2, weights=True)),
+    (64, 128, 257, dict(softcap=2.0, z_coef=1e-3)),                 # the cap bends most logits
+    (130, 136, 1000, dict(weights=True, M=3)),
+    (255, 264, 511, dict(softcap=30.0, weights=True, M=2, divisor=1000)),
+    (300, 520, 2048, dict(softcap=50.0, z_coef=1e-4, M=4)),
+    (600, 64, 5003, dict(weights=True, softcap=1.0, sigma=0.5, M=2)),
+    (257, 256, 8200, dict(z_coef=1e-4, sigma=6.0)),                 # sharp
+    (40, 64, 300, dict(ignore=1.0, weights=True)),                  # no label at all
+]
+DISTILL = [
+    (1, 8, 1, dict(K=1)),
+    (1, 8, 1, dict(K=1, tail=True)),
+    (1, 64, 300, dict(K=32, tail=True)),
+    (5, 16, 7, dict(K=7, tail=True, label_coef=0.5)),               # the entries are the whole vocabulary
+    (9, 16, 7, dict(K=5, tail=True, temperature=4.0, label_coef=0.5, weights=True)),
+    (37, 72, 256, dict(K=256, temperature=2.0)),
+    (64, 128, 257, dict(K=255, tail=True, softcap=5.0)),            # two others in most rows, in another tile or not
+    (130, 136, 1000, dict(K=64, tail=True, label_coef=0.3, teacher_coef=0.7, weights=True, M=3, teacher="bf16")),
+    (130, 136, 1000, dict(K=64, label_coef=0.3, teacher_coef=0.7, temperature=2.0, weights=True, M=3, teacher="bf16")),
+    (255, 264, 511, dict(K=20, tail=True, label_coef=0.5, temperature=0.5, softcap=30.0, M=2, divisor=77)),
+    (300, 520, 2048, dict(K=1, label_coef=0.5, M=4)),
+    (257, 256, 8200, dict(K=128, tail=True, labels=False, sigma=6.0)),
+    (600, 64, 5003, dict(K=200, tail=True, temperature=3.0, label_coef=0.1, M=2)),
+    (70, 64, 300, dict(K=16, empty=1.0, label_coef=0.5)),           # no teacher at all
+    (70, 64, 300, dict(K=16, ignore=1.0, empty=0.5, label_coef=0.5, temperature=2.0)),
+]
+
+
+def _ids(cases):
+    return ["%dx%dx%d-%s" % (*c[:3], "-".join("%s=%s" % kv for kv in c[3].items())) for c in cases]
+
+
+@pytest.mark.parametrize("S,d,V,o", WCE + DISTILL, ids=_ids(WCE + DISTILL))
+def test_outputs_and_gradients(S, d, V, o):
+    p = Problem(S, d, V, **o)
+    run = Run(p)
+    run.forward()
+    run.backward(grad_loss=1.5)
+    print(check(p, run.outputs(), p.oracle(1.5), 1.5))
+
+
+@pytest.mark.parametrize("schedule", [1, 2, 3])
+@pytest.mark.parametrize("o", [dict(K=40, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=20.0, weights=True, z_coef=1e-3)])
+def test_orders_of_the_backward_pass(schedule, o):
+    import paper_2407_15892_amd as mst
+    p = Problem(700, 264, 3001, M=3, **o)
+    run = Run(p)
+    run.forward()
+    mst.mst_set_bwd_schedule(schedule)
+    try:
+        run.backward()
+        run.torch.cuda.synchronize()
+    finally:
+        mst.mst_set_bwd_schedule(mst.BWD_SCHEDULE_AUTO)
+    print(check(p, run.outputs(), p.oracle()))
+
+
+@pytest.mark.parametrize("rows", [20, 100, 400, 1500])
+def test_tiles_of_the_forward_pass(rows):
+    """Every height of the forward's tiles, with entries at the borders of tiles and lanes."""
+    import paper_2407_15892_amd as mst
+    V = 12800
+    p = Problem(rows, 64, V, K=48, tail=True, label_coef=0.5, temperature=2.0, softcap=10.0)
+    edges = np.array([0, 1, 31, 32, 127, 128, 255, 256, 257, 511, 512, V - 1, V - 2, V - 256, V - 257], dtype=np.int32)
+    for s in range(0, rows, 3):
+        p.index[s, :] = -1
+        p.index[s, 3:3 + len(edges)] = edges[::-1]
+    print(mst.mst_forward_tile_rows(rows, 64, V, 1), mst.mst_forward_launch(rows, 64, V, 1))
+    run = Run(p)
+    run.forward()
+    run.backward()
+    print(check(p, run.outputs(), p.oracle()))
