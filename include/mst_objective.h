@@ -40,6 +40,8 @@
  *   - `saved` carries what the backward call needs from the forward call (mst_objective_bytes): per row 16 bytes, distill 24 and
  *     8 for each of K entries.  The backward call takes softcap, temperature, coefficients, weights, labels and the teacher from
  *     it; H, W, S, d, V and K have to be those of the forward call, M need not be.  NULL where no backward call follows;
+ *   - M is the largest number of mini-sequences: the calls make fewer, longer ones as long as the fp32 logits of one are at most
+ *     512 MiB, and their workspace is that of these;
  *   - arithmetic: that of mst_lmhead.h; the loss and the rows' outputs float32 (sums over rows in 64 bits), the gradient of the
  *     logits without the factor grad_loss / n rounded to bf16 before the two products; everything in a fixed order, without
  *     atomics: repeated calls give the same bits.
@@ -58,7 +60,7 @@ extern "C" {
 
 /*
  * Bytes of the forward's and the backward's workspace and of `saved` (host, pure; each pointer may be NULL).  K: 0 for wce.
- * The backward's workspace is that of mst_lmhead_ce_bwd, one mini-sequence of fp32 logits; the forward's that of
+ * The backward's workspace is that of mst_lmhead_ce_bwd, one mini-sequence (see M above) of fp32 logits; the forward's that of
  * mst_lmhead_ce_fwd and 8 bytes a row, for distill also 6 bytes for each pair that is kept there and 12 K + 4 bytes for each row of
  * a group of mini-sequences.
  */

@@ -9,10 +9,15 @@ namespace {
 struct ObjPlan {
   Plan p;
   int K;
+  int few;               // row tiles of 16 of the forward of a few rows (k_obj_few); 0: the plain forward's tiles
+  int n_vt;              // vocabulary tiles of the forward
   // forward workspace: the plain forward's (its nll: the rows' losses), then
-  size_t f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
+  size_t f_part_few, f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
   size_t s_rows, s_rows2, s_index, s_at, s_total;      // of `saved`
 };
+
+// Calls of a few rows have a forward of their own.
+int few_rows(const Plan& p) { return p.S > p.fwd_group_rows ? 0 : p.S <= 16 ? 1 : p.S <= 32 ? 2 : 0; }
 
 // Byte ranges of a call's arguments: no output may overlap anything else.
 struct Ranges {
@@ -30,18 +35,33 @@ struct Ranges {
   }
 };
 
+// Mini-sequences that the calls make of a call's M: no more than leave each kObjRoom of fp32 logits.  M bounds the memory, and
+// below some hundred MB the backward pays for the bound and the chip has no use for it: its launches get too small to fill the
+// compute units.  Backward of the plain cross-entropy, us, by mini-sequences: 5003 rows, d = 1544, V = 32003: 2340 with 19 (32 MB), 1757
+// with 10, 1452 with 4, 1380 with 3, 1407 with 2, 1552 with 1 (610 MB); 8192, 4096, 128256: 19616 with 31 (129 MB), 19324 with 16, 18694
+// with 8, 18593 with 4 (1 GB); 20000, 520, 30000: 3927 with 57 (40 MB), 2300 with 16, 2245 with 4; 3000, 1024, 8000: 340 with 8, 152 with 1.
+constexpr int64_t kObjRoom = int64_t(512) << 20;
+int32_t fewer_mini_sequences(int64_t S, int64_t V, int32_t M) {
+  if (S < 1 || V < 1 || V >= (int64_t(1) << 31) || M < 1 || M > S) return M;      // refused by make_plan
+  const int64_t rows = std::max<int64_t>(1, kObjRoom / (4 * ((V + 7) / 8 * 8)));
+  return (int32_t)std::min<int64_t>(M, (S + rows - 1) / rows);
+}
+
 mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO, bool schedule = false) {
-  const mst_status s = make_plan(S, d, V, M, &o->p, forced, 0, schedule);
+  const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, V, M), &o->p, forced, 0, schedule);
   if (s != MST_OK) return s;
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
   o->p.streamed = 0;      // that order stores no dlogits to put the entries into
   o->K = K;
+  o->few = few_rows(o->p);
+  o->n_vt = o->few ? (int)((V + kFewV - 1) / kFewV) : o->p.n_vt;
   const size_t rows = (size_t)o->p.fwd_group_rows, k = (size_t)K;
   size_t off = o->p.f_total;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
+  o->f_part_few = o->few ? take((size_t)o->n_vt * rows * 8) : 0;
   o->f_count = take((size_t)S * 4);
-  o->f_part_label = K ? take((size_t)o->p.n_vt * rows * 4) : 0;
-  o->f_starts = K ? take((size_t)(o->p.n_vt + 1) * rows * 2) : 0;
+  o->f_part_label = K ? take((size_t)o->n_vt * rows * 4) : 0;
+  o->f_starts = K ? take((size_t)(o->n_vt + 1) * rows * 2) : 0;
   o->f_index = K ? take(rows * k * 4) : 0;
   o->f_logit = K ? take(rows * k * 4) : 0;
   o->f_entry_y = K ? take(rows * k * 4) : 0;
@@ -116,7 +136,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   const bool two = o.K && c.labels && c.temperature != 1.f;
   const float exponent = (float)(1.4426950408889634 / (double)c.temperature);
   ObjEpilogue e = {};
-  e.part = reinterpret_cast<float2*>(ws + p.f_part);
+  e.part = reinterpret_cast<float2*>(ws + (o.few ? o.f_part_few : p.f_part));
   e.part_label = two ? reinterpret_cast<float*>(ws + o.f_part_label) : nullptr;
   e.part_stride = stride;
   e.tgt = reinterpret_cast<float*>(ws + p.f_tgt);
@@ -135,7 +155,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   }
   ObjFinal f = {};
   f.part = e.part; f.part_label = e.part_label; f.part_stride = stride;
-  f.n_vt = p.n_vt; f.V = (int)p.V; f.K = o.K;
+  f.n_vt = o.n_vt; f.V = (int)p.V; f.K = o.K;
   f.tgt = e.tgt; f.ignore_index = c.ignore_index;
   f.index = index; f.logit = logit; f.entry_y = e.entry_y; f.info = info;
   f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t = (float)(1.0 / (double)c.temperature);
@@ -143,52 +163,71 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   float* const row_loss = reinterpret_cast<float*>(ws + p.f_nll);
   int* const count = reinterpret_cast<int*>(ws + o.f_count);
 
-  s = run_forward_groups(
-      p, static_cast<const __bf16*>(c.H), static_cast<const __bf16*>(c.W), st, reinterpret_cast<Control*>(ws),
-      [&](int64_t g0) {
-        ObjEpilogue of = e;
-        of.labels_c = c.labels ? c.labels + g0 : nullptr;
-        return of;
-      },
-      [&](int64_t g0, int g_rows) {
-        if (!o.K) return;
-        const size_t from = (size_t)g0 * k;
-        const void* const logits = static_cast<const char*>(c.logits) + from * (c.logits_bf16 ? 2 : 4);
-        Scope sc(st, MST_K_LABEL_SCAN);
-        hipLaunchKernelGGL(k_entries, dim3((unsigned)((g_rows + kEntryRows - 1) / kEntryRows)), dim3(64 * kEntryRows), 0, st,
-                           c.index + from, logits, c.logits_bf16, g_rows, o.K, (int)p.V, p.n_vt, index, logit, info, starts, stride);
-      },
-      [&](int64_t g0, int g_rows) {
-        ObjFinal of = f;
-        of.rows = g_rows;
-        of.labels_c = c.labels ? c.labels + g0 : nullptr;
-        of.weights_c = c.weights ? c.weights + g0 : nullptr;
-        of.teacher_lse_c = c.teacher_lse ? c.teacher_lse + g0 : nullptr;
-        of.nll_c = c.nll ? c.nll + g0 : nullptr;
-        of.kd_c = c.kd ? c.kd + g0 : nullptr;
-        of.lse_c = c.lse ? c.lse + g0 : nullptr;
-        of.row_loss_c = row_loss + g0;
-        of.count_c = count + g0;
-        if (saved) {
-          of.rows_c = reinterpret_cast<ObjRow*>(saved + o.s_rows) + g0;
-          if (o.K) {
-            of.rows2_c = reinterpret_cast<ObjRow2*>(saved + o.s_rows2) + g0;
-            of.saved_index_c = reinterpret_cast<int*>(saved + o.s_index) + (size_t)g0 * k;
-            of.saved_at_c = reinterpret_cast<float*>(saved + o.s_at) + (size_t)g0 * k;
-          }
-        }
-        Scope sc(st, MST_K_LSE_FINALIZE);
-        hipLaunchKernelGGL(k_obj_finalize, dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of);
-      });
-  if (s != MST_OK) return s;
-  ObjHeader head = {};
-  head.cap = c.softcap;
-  head.exponent = exponent;
-  head.exponent_label = kLog2e;
-  head.two = two;
-  Scope sc(st, MST_K_LOSS_REDUCE);
-  hipLaunchKernelGGL(k_obj_loss, dim3(1), dim3(1024), 0, st, row_loss, count, (long long)p.S, (long long)c.divisor, head,
-                     reinterpret_cast<ObjHeader*>(saved), c.loss, reinterpret_cast<long long*>(c.n_valid));
+  ObjLoss l = {};
+  l.divisor = c.divisor;
+  l.head.cap = c.softcap;
+  l.head.exponent = exponent;
+  l.head.exponent_label = kLog2e;
+  l.head.two = two;
+  l.saved = reinterpret_cast<ObjHeader*>(saved);
+  l.loss = c.loss;
+  l.n_valid = reinterpret_cast<long long*>(c.n_valid);
+  const bool one = p.S <= kObjRows && p.S <= p.fwd_group_rows;                 // the rows of the call are one workgroup of k_obj_finalize
+  auto epilogue_of = [&](int64_t g0) {
+    ObjEpilogue of = e;
+    of.labels_c = c.labels ? c.labels + g0 : nullptr;
+    return of;
+  };
+  auto before = [&](int64_t g0, int g_rows) {
+    if (!o.K) return;
+    const size_t from = (size_t)g0 * k;
+    const void* const logits = static_cast<const char*>(c.logits) + from * (c.logits_bf16 ? 2 : 4);
+    Scope sc(st, MST_K_LABEL_SCAN);
+    const auto kernel = o.K <= 64 ? k_entries<1> : o.K <= 128 ? k_entries<2> : k_entries<4>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((g_rows + kEntryRows - 1) / kEntryRows)), dim3(64 * kEntryRows), 0, st,
+                       c.index + from, logits, c.logits_bf16, g_rows, o.K, (int)p.V, o.n_vt, o.few ? kFewV : kTile, index, logit, info, starts,
+                       stride);
+  };
+  auto after = [&](int64_t g0, int g_rows) {
+    ObjFinal of = f;
+    of.rows = g_rows;
+    of.labels_c = c.labels ? c.labels + g0 : nullptr;
+    of.weights_c = c.weights ? c.weights + g0 : nullptr;
+    of.teacher_lse_c = c.teacher_lse ? c.teacher_lse + g0 : nullptr;
+    of.nll_c = c.nll ? c.nll + g0 : nullptr;
+    of.kd_c = c.kd ? c.kd + g0 : nullptr;
+    of.lse_c = c.lse ? c.lse + g0 : nullptr;
+    of.row_loss_c = row_loss + g0;
+    of.count_c = count + g0;
+    if (saved) {
+      of.rows_c = reinterpret_cast<ObjRow*>(saved + o.s_rows) + g0;
+      if (o.K) {
+        of.rows2_c = reinterpret_cast<ObjRow2*>(saved + o.s_rows2) + g0;
+        of.saved_index_c = reinterpret_cast<int*>(saved + o.s_index) + (size_t)g0 * k;
+        of.saved_at_c = reinterpret_cast<float*>(saved + o.s_at) + (size_t)g0 * k;
+      }
+    }
+    Scope sc(st, MST_K_LSE_FINALIZE);
+    const auto kernel = one ? k_obj_finalize<true> : k_obj_finalize<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of, l);
+  };
+  const __bf16 *const H = static_cast<const __bf16*>(c.H), *const W = static_cast<const __bf16*>(c.W);
+  if (o.few) {
+    before(0, (int)p.S);
+    {
+      Scope sc(st, MST_K_FWD_GEMM_LSE);
+      hipLaunchKernelGGL(o.few == 1 ? k_obj_few<1> : k_obj_few<2>, dim3(o.n_vt), dim3(64 * kFewWaves), 0, st, H, W, (int)p.S, (int)p.d, (int)p.V,
+                         epilogue_of(0));
+    }
+    after(0, (int)p.S);
+  } else {
+    s = run_forward_groups(p, H, W, st, reinterpret_cast<Control*>(ws), epilogue_of, before, after);
+    if (s != MST_OK) return s;
+  }
+  if (!one) {
+    Scope sc(st, MST_K_LOSS_REDUCE);
+    hipLaunchKernelGGL(k_obj_loss, dim3(1), dim3(1024), 0, st, row_loss, count, (long long)p.S, l);
+  }
   return check_launch();
 }
 

@@ -62,7 +62,7 @@ struct ObjEpilogue {
   float2* part;                        // [n_vt][part_stride] (maximum, sum) of the others
   float* part_label;                   // the sum at the second exponent; null: rows have one
   size_t part_stride;
-  float* tgt;                          // y of the label
+  float* tgt;                          // y of the label, unless it is an entry
   const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile; null: no teacher
   const int* index;                    // [rows][K] ascending
   float* entry_y;                      // [rows][K] y of the entries
@@ -90,22 +90,6 @@ struct ObjEpilogue {
         for (int u = 0; u < TB; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[t][u][r] = capped(acc[t][u][r], cap, scale);
-    }
-#pragma unroll
-    for (int u = 0; u < TB; ++u) {
-      const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
-      const int y = s_local < rows ? y_u[u] : -1;
-      const int rel = y - (v0 + wa * 128);
-      if (rel >= 0 && rel < 128 && y < V && (rel >> 5) == g) {
-        const int t_sel = (rel & 31) >> 2, r_sel = rel & 3;
-        float val = 0.f;
-#pragma unroll
-        for (int t = 0; t < kTA16; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (t == t_sel && r == r_sel) val = acc[t][u][r];
-        tgt[s_local] = val;
-      }
     }
     if (starts) {
 #pragma unroll
@@ -167,6 +151,19 @@ struct ObjEpilogue {
       for (int o = 16; o <= 32; o <<= 1)
         merge_sums(m, l, k, __shfl_xor(m, o), __shfl_xor(l, o), two ? __shfl_xor(k, o) : 0.f, exponent, exponent_label, two);
       m_u[u] = m; l_u[u] = l; k_u[u] = k;
+      const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+      const int y = s_local < rows ? y_u[u] : -1;
+      const int rel = y - (v0 + wa * 128);
+      if (rel >= 0 && rel < 128 && y < V && (rel >> 5) == g) {
+        const int t_sel = (rel & 31) >> 2, r_sel = rel & 3;
+        float val = 0.f;
+#pragma unroll
+        for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t == t_sel && r == r_sel) val = acc[t][u][r];
+        tgt[s_local] = val;
+      }
     }
     // the main loop ended with a barrier, LDS is free
     float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves
@@ -193,96 +190,217 @@ struct ObjEpilogue {
 };
 
 // ---------------------------------------------------------------------------
-// The teacher's entries of a group of rows in ascending order.  A wave takes a row: every lane counts, for its (up to four)
-// entries, those that come before them.  An index below 0 is no entry; one that comes twice counts once, with the logit it has
-// first; one at or behind V makes the row bad.
+// forward of a few rows: W is read once, which is all that takes time.  A workgroup owns kFewV vocabulary entries, a wave 16 of
+// them and up to 16 TB rows; both operands come from memory straight into registers as MFMA fragments.  The contraction's
+// order is free, so a lane quarter g takes the 16 consecutive k = 16 g .. 16 g + 15 of every 64: 32 contiguous bytes a lane, a
+// whole line of each of the 16 rows for the wave.  kDepth such steps are loaded while the kDepth before them are multiplied.
+// ---------------------------------------------------------------------------
+constexpr int kFewWaves = 8, kFewV = 16 * kFewWaves, kFewDepth = 4;
+template <int TB>
+__global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __restrict__ H, const __bf16* __restrict__ W, int rows, int d, int V,
+                                                            ObjEpilogue e) {
+  __shared__ float xch[kFewWaves][16 * TB][3];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int vt = blockIdx.x, v0 = vt * kFewV + 16 * wave;
+  const int v_in = v0 + c < V ? v0 + c : V - 1;
+  const __bf16* const a_row = W + (size_t)v_in * d + 16 * g;
+  const __bf16* b_row[TB];
+#pragma unroll
+  for (int u = 0; u < TB; ++u) b_row[u] = H + (size_t)(16 * u + c < rows ? 16 * u + c : rows - 1) * d + 16 * g;
+  f32x4 acc[TB];
+#pragma unroll
+  for (int u = 0; u < TB; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Step { bf16x8 a[2], b[TB][2]; };
+  auto load = [&](Step& x, int k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x.a[h] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(a_row + k + 8 * h));
+#pragma unroll
+      for (int u = 0; u < TB; ++u) x.b[u][h] = *reinterpret_cast<const bf16x8*>(b_row[u] + k + 8 * h);
+    }
+  };
+  auto multiply = [&](const Step& x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < TB; ++u) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.a[h], x.b[u][h], acc[u], 0, 0, 0);
+  };
+  const int n_block = d / (64 * kFewDepth);
+  if (n_block) {
+    Step now[kFewDepth], next[kFewDepth];
+#pragma unroll
+    for (int i = 0; i < kFewDepth; ++i) load(now[i], 64 * i);
+    for (int b = 1; b < n_block; ++b) {
+#pragma unroll
+      for (int i = 0; i < kFewDepth; ++i) load(next[i], 64 * (b * kFewDepth + i));
+#pragma unroll
+      for (int i = 0; i < kFewDepth; ++i) multiply(now[i]);
+#pragma unroll
+      for (int i = 0; i < kFewDepth; ++i) now[i] = next[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kFewDepth; ++i) multiply(now[i]);
+  }
+  for (int k = n_block * 64 * kFewDepth; k < d; k += 64) {             // the rest, eight k at a time inside or outside
+    Step x;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = k + 16 * g + 8 * h < d;
+      const bf16x8 zero = {};
+      x.a[h] = in ? *reinterpret_cast<const bf16x8*>(a_row + k + 8 * h) : zero;
+#pragma unroll
+      for (int u = 0; u < TB; ++u) x.b[u][h] = in ? *reinterpret_cast<const bf16x8*>(b_row[u] + k + 8 * h) : zero;
+    }
+    multiply(x);
+  }
+
+  // as ObjEpilogue: a lane has, of row 16 u + c, the four entries from va on
+  const int va = v0 + 4 * g;
+  const bool two = e.part_label != nullptr;
+#pragma unroll
+  for (int u = 0; u < TB; ++u) {
+    const int s = 16 * u + c;
+    const bool in = s < rows;
+    const int s_in = in ? s : rows - 1;
+    float y[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = e.cap > 0.f ? capped(acc[u][r], e.cap, 2.f * kLog2e / e.cap) : acc[u][r];
+    if (e.labels_c && in) {
+      const int at = e.labels_c[s] - va;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (at == r && va + r < V) e.tgt[s] = y[r];
+    }
+    if (e.starts) {
+      const int end = in ? e.starts[(size_t)(vt + 1) * e.part_stride + s_in] : 0;
+      for (int i = e.starts[(size_t)vt * e.part_stride + s_in]; i < end; ++i) {
+        const int at = e.index[(size_t)s * e.K + i] - va;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (at == r) {
+            e.entry_y[(size_t)s * e.K + i] = y[r];
+            y[r] = kMasked;
+          }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (va + r >= V) y[r] = kMasked;
+    float m = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), l = 0.f, k = 0.f;
+    m = fmaxf(m, kMasked);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      l += fast_exp2((y[r] - m) * e.exponent);
+      if (two) k += fast_exp2((y[r] - m) * e.exponent_label);
+    }
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1)
+      merge_sums(m, l, k, __shfl_xor(m, o), __shfl_xor(l, o), two ? __shfl_xor(k, o) : 0.f, e.exponent, e.exponent_label, two);
+    if (lane < 16) {
+      float* const at = xch[wave][16 * u + lane];
+      at[0] = m; at[1] = l; at[2] = k;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x >= 16 * TB || (int)threadIdx.x >= rows) return;
+  const int s = threadIdx.x;
+  float m = kMasked, l = 0.f, k = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) merge_sums(m, l, k, xch[w][s][0], xch[w][s][1], xch[w][s][2], e.exponent, e.exponent_label, two);
+  e.part[(size_t)vt * e.part_stride + s] = make_float2(m, l);
+  if (two) e.part_label[(size_t)vt * e.part_stride + s] = k;
+}
+
+// ---------------------------------------------------------------------------
+// The teacher's entries of a group of rows in ascending order.  A wave sorts a row, P entries a lane, with a bitonic network on
+// (index, place) in 64 bits: of entries with the same index the first comes first and the others are dropped.  An index below 0 is
+// no entry; one at or behind V makes the row bad.
 //   index, logit [rows][K] (float32), the rest of a row kNoEntry; info[row] = entries, or -1
-//   starts [n_vt + 1][stride]
+//   starts [n_vt + 1][stride]: entries before vocabulary entry `width` vt
+// 32768 rows of 256: 510 us with every entry compared to all others of its row, in LDS.
 // ---------------------------------------------------------------------------
 constexpr int kEntryRows = 16;              // of a workgroup, one wave each: 32-byte pieces of starts
+template <int P>
+__device__ __forceinline__ void sort_entries(unsigned long long (&x)[P], int lane) {
+  auto order = [](unsigned long long& a, unsigned long long& b, bool up) {
+    const bool swap = (b < a) == up;
+    const unsigned long long t = a;
+    a = swap ? b : a;
+    b = swap ? t : b;
+  };
+#pragma unroll
+  for (int k = 2; k <= 64 * P; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2) {
+      if (j >= P) {
+        const bool lower = (lane & (j / P)) == 0;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const unsigned long long other = __shfl_xor(x[i], j / P);
+          const bool up = ((lane * P + i) & k) == 0;
+          x[i] = (other < x[i]) == (up == lower) ? other : x[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+          if (!(i & j)) order(x[i], x[i | j], ((lane * P + i) & k) == 0);
+      }
+    }
+}
+template <int P>
 __global__ __launch_bounds__(64 * kEntryRows) void k_entries(
-    const int* __restrict__ index_in, const void* __restrict__ logit_in, int logit_bf16, int rows, int K, int V, int n_vt,
+    const int* __restrict__ index_in, const void* __restrict__ logit_in, int logit_bf16, int rows, int K, int V, int n_vt, int width,
     int* __restrict__ index, float* __restrict__ logit, int* __restrict__ info, unsigned short* __restrict__ starts, size_t stride) {
-  __shared__ __attribute__((aligned(16))) int key_sh[kEntryRows][kMaxEntries];
+  __shared__ int key_sh[kEntryRows][64 * P];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int s = blockIdx.x * kEntryRows + w, s_in = s < rows ? s : rows - 1;
-  constexpr int kPer = kMaxEntries / 64;
-  int* const key = key_sh[w];
-  const int per = (K + 63) / 64;
-  int mine[kPer], rank[kPer];
+  unsigned long long x[P];
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 64 * i;
-    int v = kNoEntry;
-    if (e < K) {
-      v = index_in[(size_t)s_in * K + e];
-      if (v >= V) bad = true;
-      if ((unsigned)v >= (unsigned)V) v = kNoEntry;
-    }
-    mine[i] = v;
-    key[e] = v;
+  for (int i = 0; i < P; ++i) {
+    const int e = lane * P + i;
+    int v = e < K ? index_in[(size_t)s_in * K + e] : -1;
+    bad |= v >= V;
+    if ((unsigned)v >= (unsigned)V) v = kNoEntry;
+    x[i] = ((unsigned long long)(unsigned)v << 8) | (unsigned)e;
   }
   bad = __any(bad);
-  __syncthreads();
-  const int K4 = (K + 3) / 4;
-  // one that came before: not an entry any more
-  for (int j = 0; j < K4; ++j) {
-    const int4 q = *reinterpret_cast<const int4*>(key + 4 * j);
-    const int of[4] = {q.x, q.y, q.z, q.w};
+  sort_entries<P>(x, lane);
+  int v[P];
+  bool keep[P];
+  int before = 0, n = 0;                      // entries that are kept: in lanes below, in all
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i < per) {
+  for (int i = 0; i < P; ++i) v[i] = (int)(x[i] >> 8);
+  const int last_below = __shfl_up(v[P - 1], 1);
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-          if (of[b] == mine[i] && 4 * j + b < lane + 64 * i) mine[i] = kNoEntry;
-      }
+  for (int i = 0; i < P; ++i) {
+    const bool again = i ? v[i] == v[i ? i - 1 : 0] : lane > 0 && v[0] == last_below;
+    keep[i] = v[i] != kNoEntry && !again;
+    const unsigned long long all = __ballot(keep[i]);
+    before += __builtin_popcountll(all & ((1ull << lane) - 1));
+    n += __builtin_popcountll(all);
   }
-  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) { key[lane + 64 * i] = mine[i]; rank[i] = 0; }
-  __syncthreads();
-  for (int j = 0; j < K4; ++j) {
-    const int4 q = *reinterpret_cast<const int4*>(key + 4 * j);
-    const int of[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i < per) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) rank[i] += of[b] < mine[i] || (of[b] == mine[i] && 4 * j + b < lane + 64 * i);
-      }
-  }
-  __syncthreads();
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 64 * i;
-    n += __builtin_popcountll(__ballot(e < K && mine[i] != kNoEntry));
-    key[e] = kNoEntry;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 64 * i;
-    if (e >= K) continue;
-    key[rank[i]] = mine[i];
-    if (s >= rows) continue;
-    const size_t to = (size_t)s * K + rank[i];
-    index[to] = mine[i];
-    const size_t at = (size_t)s * K + e;
-    logit[to] = logit_bf16 ? (float)static_cast<const __bf16*>(logit_in)[at] : static_cast<const float*>(logit_in)[at];
+  for (int i = 0; i < P; ++i) {
+    const int place = keep[i] ? before : n + lane * P + i - before;      // what is dropped goes behind the rest
+    before += keep[i];
+    key_sh[w][place] = keep[i] ? v[i] : kNoEntry;
+    if (place >= K || s >= rows) continue;
+    const size_t to = (size_t)s * K + place, at = (size_t)s * K + (int)(x[i] & 255);
+    index[to] = keep[i] ? v[i] : kNoEntry;
+    if (keep[i]) logit[to] = logit_bf16 ? (float)static_cast<const __bf16*>(logit_in)[at] : static_cast<const float*>(logit_in)[at];
   }
   if (lane == 0 && s < rows) info[s] = bad ? -1 : n;
   __syncthreads();
-  // entries before vocabulary entry 256 vt, by bisection
+  // by bisection
   const int r = threadIdx.x % kEntryRows, row = blockIdx.x * kEntryRows + r;
   if (row >= rows) return;
   for (int vt = threadIdx.x / kEntryRows; vt <= n_vt; vt += 64) {
-    const int v = vt < n_vt ? vt * kTile : kNoEntry;
+    const int v0 = vt < n_vt ? vt * width : kNoEntry;
     int lo = 0, hi = K;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (key_sh[r][mid] < v) lo = mid + 1; else hi = mid;
+      if (key_sh[r][mid] < v0) lo = mid + 1; else hi = mid;
     }
     starts[(size_t)vt * stride + row] = (unsigned short)lo;
   }
@@ -317,6 +435,26 @@ struct ObjFinal {
   int* saved_index_c;
   float* saved_at_c;
 };
+// What the loss needs besides the rows'.
+struct ObjLoss {
+  long long divisor;
+  ObjHeader head;
+  ObjHeader* saved;                   // null: no backward follows
+  float* loss;
+  long long* n_valid;
+};
+__device__ __forceinline__ void write_loss(const ObjLoss& o, double sum, long long n, int bad) {
+  const long long divisor = bad ? -1 : n == 0 ? 0 : o.divisor > 0 ? o.divisor : n;
+  *o.loss = bad ? __builtin_nanf("") : n == 0 ? 0.f : (float)(sum / (double)divisor);
+  if (o.n_valid) *o.n_valid = bad ? -1 : n;
+  if (!o.saved) return;
+  o.saved->n_valid = bad ? -1 : n;
+  o.saved->n_divisor = divisor;
+  o.saved->cap = o.head.cap;
+  o.saved->exponent = o.head.exponent;
+  o.saved->exponent_label = o.head.exponent_label;
+  o.saved->two = o.head.two;
+}
 constexpr int kObjRows = 16, kObjGroups = 16;
 
 __device__ __forceinline__ float max16(float x) {
@@ -330,7 +468,9 @@ template <class X> __device__ __forceinline__ X sum16(X x) {
   return x;
 }
 
-__global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal a) {
+// kAll: the rows are all of the call's, whose loss is formed here too (one launch less).
+template <bool kAll>
+__global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal a, ObjLoss o) {
   __shared__ float sh[kObjRows][kObjGroups][3];
   const bool two = a.part_label != nullptr;
   {
@@ -397,6 +537,16 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   ly = sum16(ly);
   ky = sum16(ky);
   lt = sum16(lt);
+  const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
+  const bool labelled = a.labels_c && y != a.ignore_index;
+  const bool valid = labelled && (unsigned)y < (unsigned)a.V;
+  float y_entry = 0.f;                                           // the label's logit where it is an entry
+  int is_entry = 0;
+  if (valid)
+    for (int e = lane; e < n; e += 16)
+      if (a.index[at0 + e] == y) y_entry = a.entry_y[at0 + e], is_entry = 1;
+  y_entry = sum16(y_entry);
+  is_entry = sum16(is_entry);
 
   // log-sum-exps, as maximum and logarithm of the sum: at 1 / T (m_all / T + log_all), and at 1 (m_all + log_label)
   const float m_all = fmaxf(m, my);
@@ -410,10 +560,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const float log_share = (m - m_all) * a.inv_t + (logf(l) - log_all);
 
   const float weight = a.weights_c ? a.weights_c[s_in] : 1.f;
-  const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
-  const bool labelled = a.labels_c && y != a.ignore_index;
-  const bool valid = labelled && (unsigned)y < (unsigned)a.V;
-  const float nll = valid ? (m_all - a.tgt[s_in]) + log_label : 0.f;
+  const float nll = valid ? (m_all - (is_entry ? y_entry : a.tgt[s_in])) + log_label : 0.f;
 
   // the teacher's shares; `rest`: what it leaves to the others
   const bool given = a.teacher_lse_c != nullptr;
@@ -439,6 +586,8 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const float on_kd = taught && weight != 0.f ? weight * a.teacher_coef * a.temperature : 0.f;
   const float on_label = valid && weight != 0.f ? weight * a.label_coef : 0.f;
   const float on_p = on_label + (valid && weight != 0.f ? 2.f * weight * a.z_coef * lse : 0.f);
+  __shared__ float sh_loss[kObjRows];
+  __shared__ int sh_count[kObjRows];
   if (in && lane == 0) {
     if (a.nll_c) a.nll_c[s] = nll;
     if (a.kd_c) a.kd_c[s] = kd;
@@ -448,8 +597,27 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
       if (valid) loss += weight * (a.label_coef * nll + a.z_coef * lse * lse);
       if (taught) loss += weight * a.teacher_coef * a.temperature * a.temperature * kd;
     }
-    a.row_loss_c[s] = loss;
-    a.count_c[s] = bad_entry || (labelled && !valid) ? -1 : valid || taught ? 1 : 0;
+    const int count = bad_entry || (labelled && !valid) ? -1 : valid || taught ? 1 : 0;
+    if (kAll) {
+      sh_loss[r] = loss;
+      sh_count[r] = count;
+    } else {
+      a.row_loss_c[s] = loss;
+      a.count_c[s] = count;
+    }
+  }
+  if constexpr (kAll) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      double sum = 0.0;
+      int n_rows = 0, bad = 0;
+      for (int i = 0; i < a.rows; ++i) {
+        sum += (double)sh_loss[i];
+        n_rows += sh_count[i] > 0;
+        bad |= sh_count[i] < 0;
+      }
+      write_loss(o, sum, n_rows, bad);
+    }
   }
   if (!a.rows_c || !in) return;
   const float share = expf(log_share);                           // of the others at 1 / T
@@ -497,9 +665,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
 }
 
 // loss = sum of the rows' / divisor, in a fixed order in 64 bits, and the header of `saved`.  One workgroup.
-__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S,
-                                                   long long divisor, ObjHeader head, ObjHeader* __restrict__ saved,
-                                                   float* __restrict__ loss, long long* __restrict__ n_valid_out) {
+__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S, ObjLoss o) {
   __shared__ double sh[16];
   __shared__ long long sh_n[16];
   __shared__ int sh_bad[16];
@@ -522,10 +688,10 @@ __global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row
       bad |= c[k] < 0;
     }
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    a += __shfl_xor(a, o);
-    n += __shfl_xor(n, o);
-    bad |= __shfl_xor(bad, o);
+  for (int o2 = 32; o2 > 0; o2 >>= 1) {
+    a += __shfl_xor(a, o2);
+    n += __shfl_xor(n, o2);
+    bad |= __shfl_xor(bad, o2);
   }
   const int w = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) { sh[w] = a; sh_n[w] = n; sh_bad[w] = bad; }
@@ -533,11 +699,7 @@ __global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row
   if (threadIdx.x != 0) return;
   a = 0.0; n = 0; bad = 0;
   for (int i = 0; i < 16; ++i) { a += sh[i]; n += sh_n[i]; bad |= sh_bad[i]; }
-  head.n_valid = bad ? -1 : n;
-  head.n_divisor = bad ? -1 : n == 0 ? 0 : divisor > 0 ? divisor : n;
-  *loss = bad ? __builtin_nanf("") : n == 0 ? 0.f : (float)(a / (double)head.n_divisor);
-  if (n_valid_out) *n_valid_out = head.n_valid;
-  if (saved) *saved = head;
+  write_loss(o, a, n, bad);
 }
 
 // ---------------------------------------------------------------------------

@@ -83,3 +83,66 @@ def test_tiles_of_the_forward_pass(rows):
     run.forward()
     run.backward()
     print(check(p, run.outputs(), p.oracle()))
+
+
+@pytest.mark.parametrize("S", [1, 2, 15, 16, 17, 31, 32, 33])
+@pytest.mark.parametrize("d", [8, 72, 256, 776])
+def test_a_few_rows(S, d):
+    for o in (dict(K=33, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=4.0, z_coef=1e-3)):
+        p = Problem(S, d, 1003, seed=S, **o)
+        run = Run(p)
+        run.forward()
+        run.backward()
+        print(check(p, run.outputs(), p.oracle()))
+
+
+@pytest.mark.parametrize("o", [dict(K=30, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=20.0, weights=True, z_coef=1e-3)])
+def test_several_mini_sequences(o):
+    """2300 x 150000 logits are 1.3 GB in float32, three mini-sequences: every row's outputs and gradient are those of a call of its
+    own rows (one mini-sequence), and the weights' gradient is the sum of these calls'."""
+    import torch
+    import paper_2407_15892_amd as mst
+    S, d, V = 2300, 64, 150000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    H = torch.randn((S, d), generator=g, device="cuda").bfloat16()
+    W = (torch.randn((V, d), generator=g, device="cuda") / 4).bfloat16()
+    labels = torch.randint(0, V, (S,), generator=g, device="cuda", dtype=torch.int32)
+    labels[::7] = -100
+    weights = torch.rand(S, generator=g, device="cuda") if o.get("weights") else None
+    K = o.get("K", 0)
+    if K:
+        index = torch.randint(-1, V, (S, K), generator=g, device="cuda", dtype=torch.int32)
+        index[:, :4] = index[:, :4] % 300
+        logits = torch.randn((S, K), generator=g, device="cuda")
+        lse = torch.full((S,), 6.0, device="cuda")
+
+    def call(rows, M):
+        n = len(range(*rows.indices(S)))
+        f, b, sv = mst.mst_objective_bytes(n, d, V, M, K)
+        ws, saved = (torch.empty(x, dtype=torch.uint8, device="cuda") for x in (max(f, b), sv))
+        loss, cnt = torch.empty(1, device="cuda"), torch.empty(1, dtype=torch.int64, device="cuda")
+        nll, other = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        dH, dW = torch.empty((n, d), dtype=torch.bfloat16, device="cuda"), torch.empty((V, d), device="cuda")
+        kw = dict(saved=saved, weights=None if weights is None else weights[rows], divisor=1000, nll=nll, n_valid=cnt)
+        if K:
+            mst.mst_lmhead_distill_fwd(H[rows], W, index[rows], logits[rows], M, ws, loss, teacher_lse=lse[rows], labels=labels[rows],
+                                       label_coef=0.5, temperature=2.0, kd=other, **kw)
+            mst.mst_lmhead_distill_bwd(H[rows], W, K, M, 1.0, saved, ws, dH, dW)
+        else:
+            mst.mst_lmhead_wce_fwd(H[rows], W, labels[rows], -100, M, ws, loss, lse=other, softcap=20.0, z_coef=1e-3, **kw)
+            mst.mst_lmhead_wce_bwd(H[rows], W, M, 1.0, saved, ws, dH, dW)
+        return loss.double().item(), int(cnt), nll, other, dH, dW
+
+    assert mst.mst_objective_bytes(S, d, V, 5, K)[1] == -(-S // 3) * V * 4
+    whole = call(slice(0, S), 5)
+    parts = [call(slice(a, b), 1) for a, b in ((0, 300), (300, 1000), (1000, 1500), (1500, S))]
+    assert whole[1] == sum(p[1] for p in parts)
+    assert abs(whole[0] - sum(p[0] for p in parts)) <= 8 * 2.0 ** -24 * sum(p[0] for p in parts)
+    assert torch.equal(whole[2], torch.cat([p[2] for p in parts])) and torch.equal(whole[3], torch.cat([p[3] for p in parts]))
+    # dH: the same logits' gradient, another split of the contraction and a bf16 rounding each: two half steps and little more
+    dH = torch.cat([p[4] for p in parts]).double()
+    assert ((whole[4].double() - dH).abs() <= 2 * 2.0 ** -8 * dH.abs() + 2.0 ** -12 * dH.abs().amax(1, keepdim=True)).all()
+    # dW: float32 sums of the same terms in another order
+    dW = sum(p[5].double() for p in parts)
+    terms = sum(p[5].double().abs() for p in parts)
+    assert ((whole[5].double() - dW).abs() <= 2.0 ** -16 * terms + 2.0 ** -20 * dW.abs().amax(1, keepdim=True)).all()

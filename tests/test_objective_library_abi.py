@@ -34,6 +34,11 @@ def test_bytes(lib):
     assert bwd == plain[1] and plain[0] < fwd <= plain[0] + 4 * 8192 + 512 and saved <= 16 * 8192 + 512
     fwd, bwd, saved = mst.mst_objective_bytes(8192, 4096, 128256, 8, 64)
     assert bwd == plain[1] and fwd < bwd and saved <= (24 + 8 * 64) * 8192 + 2048
+    # M is the largest number of mini-sequences: fewer where one of them is less than 512 MiB of fp32 logits
+    assert mst.mst_objective_bytes(8192, 4096, 128256, 31, 64) == mst.mst_objective_bytes(8192, 4096, 128256, 8, 64)
+    for S_, V_, M_, most in ((5003, 32003, 19, 2), (100, 1000, 50, 1), (16384, 256000, 16, 16), (16384, 256000, 2000, 32), (1 << 17, 32768, 64, 32)):
+        c = -(-S_ // most)
+        assert mst.mst_objective_bytes(S_, 64, V_, M_)[1] == c * (-(-V_ // 8) * 8) * 4
     # the next group of mini-sequences takes the room of the one before
     assert mst.mst_objective_bytes(1 << 17, 4096, 128256, 128, 64)[0] < 3 * mst.mst_objective_bytes(1 << 15, 4096, 128256, 32, 64)[0]
     for args, status in (((0, 64, 10, 1, 0), SHAPE), ((8, 63, 10, 1, 0), SHAPE), ((8, 64, 10, 9, 0), BAD_M), ((8, 64, 10, 1, 257), SHAPE),
