@@ -573,13 +573,17 @@ mst_host::PerDeviceOnce g_attr_once, g_shape_once;
 // The tile maps and the schedule's cost model are written for the whole chip: kNumCu compute units in kNumXcd
 // XCDs.  A partitioned device is refused.
 bool device_is_whole_chip(int dev) { return mst_host::has_compute_units(dev, kNumCu); }
-template <class E, class D, class Set>       // the kernels that form logits, for one objective
-void set_logits_kernels(Set set) {
+template <class E, class Set>                // the kernels that form logits, for one objective
+void set_forward_kernels(Set set) {
+  typedef typename E::Small S;
   set((const void*)k_fwd_gemm_lse<false, E>);
   set((const void*)k_fwd_gemm_lse<true, E>);
-  set((const void*)k_fwd_gemm_lse_small<TileFwd64, E>);
-  set((const void*)k_fwd_gemm_lse_small<TileFwd32, E>);
-  set((const void*)k_fwd_gemm_lse_rows128<E>);
+  set((const void*)k_fwd_gemm_lse_small<TileFwd64, S>);
+  set((const void*)k_fwd_gemm_lse_small<TileFwd32, S>);
+  set((const void*)k_fwd_gemm_lse_rows128<S>);
+}
+template <class D, class Set>
+void set_dlogits_kernels(Set set) {
   set((const void*)k_bwd_gemm_dlogits_small<Tile64, D>);
   set((const void*)k_bwd_gemm_dlogits_small<Tile64Lone, D>);
   set((const void*)k_bwd_gemm_dlogits<false, D>);
@@ -590,8 +594,12 @@ bool set_kernel_attributes() {   // on the current device
   auto set = [&ok](const void* f) {
     if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes) != hipSuccess) ok = false;
   };
-  set_logits_kernels<LseEpilogue, CeGrad>(set);
-  set_logits_kernels<ObjEpilogue, ObjGrad>(set);
+  set_forward_kernels<LseEpilogue>(set);
+  set_dlogits_kernels<CeGrad>(set);
+  set_forward_kernels<ObjEpilogue<0>>(set);
+  set_forward_kernels<ObjEpilogue<kObjCap>>(set);
+  set_forward_kernels<ObjEpilogue<kObjAny>>(set);
+  set_dlogits_kernels<ObjGrad>(set);
   set((const void*)k_bwd_gemm_dh_small<Tile64>);
   set((const void*)k_bwd_gemm_dh_small<Tile64Lone>);
   set((const void*)k_bwd_gemm_dw_small<Tile64>);
@@ -680,6 +688,7 @@ template <class EpilogueOf, class Before, class After>
 mst_status run_forward_groups(const Plan& p, const __bf16* H, const __bf16* W, hipStream_t st, Control* ctl,
                               EpilogueOf epilogue_of, Before before, After after) {
   typedef decltype(epilogue_of(int64_t(0))) E;
+  typedef typename E::Small Small;
   const int tile_rows = forward_tile_rows(p);
   int* queue = ctl && persistent_forward(p) ? ctl->queue : nullptr;
   int queue_base = 0;
@@ -706,12 +715,12 @@ mst_status run_forward_groups(const Plan& p, const __bf16* H, const __bf16* W, h
       queue_base += tiles / kNumXcd + grid;
     } else {
       Scope sc(st, MST_K_FWD_GEMM_LSE);
-      const auto kernel = tile_rows == 128 ? k_fwd_gemm_lse_rows128<E>
-                        : tile_rows == 64 ? k_fwd_gemm_lse_small<TileFwd64, E> : k_fwd_gemm_lse_small<TileFwd32, E>;
+      const auto kernel = tile_rows == 128 ? k_fwd_gemm_lse_rows128<Small>
+                        : tile_rows == 64 ? k_fwd_gemm_lse_small<TileFwd64, Small> : k_fwd_gemm_lse_small<TileFwd32, Small>;
       const int threads = tile_rows == 128 ? kThreads : TileFwd64::kThreads;
       const int lds = tile_rows == 128 ? Tile16Rows128::kLds : tile_rows == 64 ? TileFwd64::kLds : TileFwd32::kLds;
       hipLaunchKernelGGL(kernel, dim3(even_grid(p.n_vt, n_st)), dim3(threads), lds, st,
-                         H + g0 * p.d, W, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt, epilogue);
+                         H + g0 * p.d, W, (int)g_rows, (int)p.d, (int)p.V, n_st, p.n_vt, Small(epilogue));
     }
     after(g0, (int)g_rows);
   }
@@ -747,7 +756,8 @@ void launch_ksplit(hipStream_t st, const Plan& p, const __bf16* G, const __bf16*
 }
 
 // Backward in the order that the plan has, of an objective whose gradient grad_of(r0) gives (rows from r0 on, see CeGrad).
-// after_dlogits(r0, rows, v_base, V, G, ldg): behind every launch that has formed the dlogits of those rows and vocabulary entries.
+// after_dlogits(r0, rows, v_base, V, G, ldg, small): behind every launch that has formed the dlogits of those rows and vocabulary
+// entries, in small tiles or in large ones.
 template <class GradOf, class After>
 mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb, const long long* nv, float grad_loss, char* ws, __bf16* dHb,
                                float* dW, hipStream_t st, GradOf grad_of, After after_dlogits) {
@@ -758,7 +768,8 @@ mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb
   auto dlogits = [&](int i, int rows, __bf16* G) {        // of `rows` rows from chunk i on
     const int64_t r0 = (int64_t)i * p.C;
     const int n_st = (rows + kTile - 1) / kTile;
-    if (p.joint == MST_PAIR_DH128 ? small_pair_dlogits(p, rows) : p.small_dlogits) {
+    const bool small = p.joint == MST_PAIR_DH128 ? small_pair_dlogits(p, rows) : p.small_dlogits;
+    if (small) {
       Scope sc(st, MST_K_BWD_GEMM_DLOGITS);
       const int n_vh = (int)((p.V + Tile64::EA - 1) / Tile64::EA), n_sh = (rows + Tile64::EB - 1) / Tile64::EB;
       const bool lone = lone_small((double)n_vh * n_sh);
@@ -771,7 +782,7 @@ mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb
       hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, p.n_vt, n_st)), dim3(kThreads), kLdsBytes, st,
                          Hb + r0 * p.d, Wb, grad_of(r0), rows, (int)p.d, (int)p.V, 0, n_st, p.n_vt, G, p.ldg);
     }
-    after_dlogits(r0, rows, 0, (int)p.V, G, p.ldg);
+    after_dlogits(r0, rows, 0, (int)p.V, G, p.ldg, small);
   };
   auto dh_reduce = [&](int i, int rows, const void* partial, int split) {
     Scope sc(st, MST_K_BWD_DH_REDUCE);
@@ -848,7 +859,7 @@ mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb
           hipLaunchKernelGGL(dlogits_kernel(even), dim3(launch_grid(even, tiles_w, n_st)), dim3(kThreads), kLdsBytes, st,
                              Hb + r0 * p.d, Wb + v_base * p.d, grad_of(r0), rows, (int)p.d, Vw, (int)v_base, n_st, tiles_w, G, p.blk_ldg);
         }
-        after_dlogits(r0, rows, v_base, Vw, G, p.blk_ldg);
+        after_dlogits(r0, rows, v_base, Vw, G, p.blk_ldg, false);
         const bool last_win = w == p.blk_n_win - 1;
         const int mode = p.blk_split > 1 ? (w == 0 ? kDhFirst : kDhAdd)
                                          : (w == 0 ? (last_win ? kDhOnly : kDhFirst) : (last_win ? kDhLast : kDhAdd));
@@ -1146,7 +1157,7 @@ mst_status mst_lmhead_ce_bwd(const void* H, const void* W, const int32_t* labels
     return check_launch();
   }
   return run_backward_orders(p, Hb, Wb, nv, grad_loss, ws, dHb, dW, st, [&](int64_t r0) { return CeGrad{labels + r0, lse + r0, (int)V, ignore_index}; },
-                             [](int64_t, int, int64_t, int, __bf16*, int) {});
+                             [](int64_t, int, int64_t, int, __bf16*, int, bool) {});
 }
 
 mst_status mst_set_bwd_schedule(int32_t schedule) {

@@ -417,13 +417,14 @@ __device__ __forceinline__ void lse_epilogue(f32x4 (&acc)[kTA16][TB], const int*
 }
 
 struct LseEpilogue {
+  typedef LseEpilogue Small;           // that of the smaller tiles
   const int* labels_c;
   float2* part;
   size_t part_stride;
   float* tgt;
-  template <int TB>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
-    lse_epilogue<TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
+  template <class C>                   // the tile
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+    lse_epilogue<C::TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
   }
 };
 
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse(
   pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
   gemm_mainloop_pp<Tile16>(acc, pa, pb, smem, 0, d, wa, [&]() { if (queue) feed.resolve(); });
 
-  epilogue.template operator()<kTB16>(acc, rows, V, vt, s0, wa, wb, lane, smem);
+  epilogue.template operator()<Tile16>(acc, rows, V, vt, s0, wa, wb, lane, smem);
   }
 }
 
@@ -486,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void k_fwd_gemm_lse_rows128(
   pa.init(W + (size_t)v0 * d, d, V - v0, d, wave, lane, wa);
   pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
   gemm_mainloop_pp<T>(acc, pa, pb, smem, 0, d, wa);
-  epilogue.template operator()<T::TB>(acc, rows, V, vt, s0, wa, wb, lane, smem);
+  epilogue.template operator()<T>(acc, rows, V, vt, s0, wa, wb, lane, smem);
 }
 
 // per row: combine the vocab-tile partials into lse and nll.  A workgroup owns 16 rows; its 16 groups of threads each fold
@@ -649,7 +650,9 @@ __global__ __launch_bounds__(1024) void k_finalize_loss(
 //   load(s)                 what it needs of a row;  settle(row): the same, ready for use (behind all loads)
 //   with(row, f)            calls f with a function of a logit that gives the entry, the label's own term left out
 //   label(row)              the row's label, -1 for none;  label_term(row, z): what its entry is less by
+//   kPatch, patch(...)      whether entries are put into a small tile behind all others (mst_objective_kernels.hpp)
 struct CeGrad {
+  static constexpr bool kPatch = false;
   const int* labels_c;
   const float* lse_c;
   int V_all, ignore_index;

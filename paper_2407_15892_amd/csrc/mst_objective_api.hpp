@@ -3,6 +3,7 @@
 #include "../../include/mst_objective.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
@@ -15,6 +16,10 @@ struct ObjPlan {
   size_t f_part_few, f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
   size_t s_rows, s_rows2, s_index, s_at, s_total;      // of `saved`
 };
+
+// Up to so many entries a row, tiles of 64 x 64 dlogits put them in themselves: a launch less, 3 us, for which a tile looks through
+// the entries of its rows.
+constexpr int kPatchEntries = 64;
 
 // Calls of a few rows have a forward of their own.
 int few_rows(const Plan& p) { return p.S > p.fwd_group_rows ? 0 : p.S <= 16 ? 1 : p.S <= 32 ? 2 : 0; }
@@ -61,7 +66,7 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   o->f_part_few = o->few ? take((size_t)o->n_vt * rows * 8) : 0;
   o->f_count = take((size_t)S * 4);
   o->f_part_label = K ? take((size_t)o->n_vt * rows * 4) : 0;
-  o->f_starts = K ? take((size_t)(o->n_vt + 1) * rows * 2) : 0;
+  o->f_starts = K && !o->few ? take((size_t)(o->n_vt + 1) * rows * 2) : 0;
   o->f_index = K ? take(rows * k * 4) : 0;
   o->f_logit = K ? take(rows * k * 4) : 0;
   o->f_entry_y = K ? take(rows * k * 4) : 0;
@@ -95,6 +100,13 @@ struct ObjCall {       // a forward call's arguments, of either objective
   int64_t* n_valid;
   void* stream;
 };
+
+template <bool kAll>
+auto finalize_kernel_of(int K) {
+  return K == 0 ? k_obj_finalize<kAll, 0> : K <= 16 ? k_obj_finalize<kAll, 1> : K <= 32 ? k_obj_finalize<kAll, 2>
+       : K <= 64 ? k_obj_finalize<kAll, 4> : K <= 128 ? k_obj_finalize<kAll, 8> : k_obj_finalize<kAll, 16>;
+}
+auto finalize_kernel(bool all, int K) { return all ? finalize_kernel_of<true>(K) : finalize_kernel_of<false>(K); }
 
 mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   const Plan& p = o.p;
@@ -135,7 +147,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   // both log-sum-exps, at 1 / T for the teacher and at 1 for the labels, only where they differ
   const bool two = o.K && c.labels && c.temperature != 1.f;
   const float exponent = (float)(1.4426950408889634 / (double)c.temperature);
-  ObjEpilogue e = {};
+  ObjTile e = {};
   e.part = reinterpret_cast<float2*>(ws + (o.few ? o.f_part_few : p.f_part));
   e.part_label = two ? reinterpret_cast<float*>(ws + o.f_part_label) : nullptr;
   e.part_stride = stride;
@@ -144,14 +156,19 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   e.cap = c.softcap;
   e.exponent = exponent;
   e.exponent_label = kLog2e;
+  e.power = c.temperature == 2.f ? 2 : c.temperature == 4.f ? 4 : 0;
   int* const index = reinterpret_cast<int*>(ws + o.f_index);
   float* const logit = reinterpret_cast<float*>(ws + o.f_logit);
   int* const info = reinterpret_cast<int*>(ws + o.f_info);
   unsigned short* const starts = reinterpret_cast<unsigned short*>(ws + o.f_starts);
+  const bool sorted = o.K && !o.few && forward_tile_rows(p) == kTile;
   if (o.K) {
-    e.starts = starts;
+    e.starts = sorted ? starts : nullptr;
     e.index = index;
     e.entry_y = reinterpret_cast<float*>(ws + o.f_entry_y);
+    e.logit_bf16 = c.logits_bf16;
+    e.logit = logit;
+    e.info = info;
   }
   ObjFinal f = {};
   f.part = e.part; f.part_label = e.part_label; f.part_stride = stride;
@@ -172,21 +189,21 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   l.saved = reinterpret_cast<ObjHeader*>(saved);
   l.loss = c.loss;
   l.n_valid = reinterpret_cast<long long*>(c.n_valid);
-  const bool one = p.S <= kObjRows && p.S <= p.fwd_group_rows;                 // the rows of the call are one workgroup of k_obj_finalize
-  auto epilogue_of = [&](int64_t g0) {
-    ObjEpilogue of = e;
+  const bool one_group = p.S <= kObjRows && p.S <= p.fwd_group_rows;       // the call's rows are one workgroup of k_obj_finalize
+  const bool one = one_group || (!o.K && !o.few && finalize_in_one(p));    // the loss is formed with the rows' losses
+  auto logits_from = [&](int64_t g0) -> const void* { return static_cast<const char*>(c.logits) + (size_t)g0 * k * (c.logits_bf16 ? 2 : 4); };
+  auto tile_of = [&](int64_t g0) {
+    ObjTile of = e;
     of.labels_c = c.labels ? c.labels + g0 : nullptr;
+    if (o.K) of.index_in_c = c.index + (size_t)g0 * k, of.logit_in_c = logits_from(g0);
     return of;
   };
   auto before = [&](int64_t g0, int g_rows) {
-    if (!o.K) return;
-    const size_t from = (size_t)g0 * k;
-    const void* const logits = static_cast<const char*>(c.logits) + from * (c.logits_bf16 ? 2 : 4);
+    if (!sorted) return;
     Scope sc(st, MST_K_LABEL_SCAN);
     const auto kernel = o.K <= 64 ? k_entries<1> : o.K <= 128 ? k_entries<2> : k_entries<4>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((g_rows + kEntryRows - 1) / kEntryRows)), dim3(64 * kEntryRows), 0, st,
-                       c.index + from, logits, c.logits_bf16, g_rows, o.K, (int)p.V, o.n_vt, o.few ? kFewV : kTile, index, logit, info, starts,
-                       stride);
+                       c.index + (size_t)g0 * k, logits_from(g0), c.logits_bf16, g_rows, o.K, (int)p.V, p.n_vt, index, logit, info, starts, stride);
   };
   auto after = [&](int64_t g0, int g_rows) {
     ObjFinal of = f;
@@ -208,20 +225,27 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
       }
     }
     Scope sc(st, MST_K_LSE_FINALIZE);
-    const auto kernel = one ? k_obj_finalize<true> : k_obj_finalize<false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of, l);
+    if (one && !one_group) {
+      hipLaunchKernelGGL(k_obj_finalize_one, dim3(1), dim3(1024), 0, st, of, l);
+      return;
+    }
+    hipLaunchKernelGGL(finalize_kernel(one, o.K), dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of, l);
   };
   const __bf16 *const H = static_cast<const __bf16*>(c.H), *const W = static_cast<const __bf16*>(c.W);
   if (o.few) {
-    before(0, (int)p.S);
     {
       Scope sc(st, MST_K_FWD_GEMM_LSE);
       hipLaunchKernelGGL(o.few == 1 ? k_obj_few<1> : k_obj_few<2>, dim3(o.n_vt), dim3(64 * kFewWaves), 0, st, H, W, (int)p.S, (int)p.d, (int)p.V,
-                         epilogue_of(0));
+                         tile_of(0));
     }
     after(0, (int)p.S);
   } else {
-    s = run_forward_groups(p, H, W, st, reinterpret_cast<Control*>(ws), epilogue_of, before, after);
+    auto run = [&](auto what) {
+      return run_forward_groups(p, H, W, st, reinterpret_cast<Control*>(ws),
+                                [&](int64_t g0) { return ObjEpilogue<decltype(what)::value>(tile_of(g0)); }, before, after);
+    };
+    s = o.K ? run(std::integral_constant<int, kObjAny>())
+            : c.softcap > 0.f ? run(std::integral_constant<int, kObjCap>()) : run(std::integral_constant<int, 0>());
     if (s != MST_OK) return s;
   }
   if (!one) {
@@ -253,17 +277,22 @@ mst_status obj_backward(const ObjPlan& o, const void* H, const void* W, float gr
   const ObjHeader* const head = reinterpret_cast<const ObjHeader*>(saved);
   const ObjRow* const rows = reinterpret_cast<const ObjRow*>(saved + o.s_rows);
   const ObjRow2* const rows2 = o.K ? reinterpret_cast<const ObjRow2*>(saved + o.s_rows2) : nullptr;
+  const int* const index = reinterpret_cast<const int*>(saved + o.s_index);
+  const float* const at = reinterpret_cast<const float*>(saved + o.s_at);
   return run_backward_orders(
       p, static_cast<const __bf16*>(H), static_cast<const __bf16*>(W), &head->n_divisor, grad_loss, static_cast<char*>(workspace),
       static_cast<__bf16*>(dH), dW, st,
-      [&](int64_t r0) { return ObjGrad{head, rows + r0, rows2 ? rows2 + r0 : nullptr}; },
-      [&](int64_t r0, int n_rows, int64_t v_base, int Vw, __bf16* G, int ldg) {
-        if (!o.K) return;
+      [&](int64_t r0) {
+        const bool patch = o.K && o.K <= kPatchEntries;
+        return ObjGrad{head, rows + r0, rows2 ? rows2 + r0 : nullptr, index + (size_t)r0 * o.K, at + (size_t)r0 * o.K, patch ? o.K : 0};
+      },
+      [&](int64_t r0, int n_rows, int64_t v_base, int Vw, __bf16* G, int ldg, bool small) {
+        if (!o.K || (small && o.K <= kPatchEntries)) return;
         const size_t from = (size_t)r0 * o.K;
         const long long n = (long long)n_rows * o.K;
         Scope sc(st, MST_K_BWD_DH_REDUCE);
-        hipLaunchKernelGGL(k_obj_entries, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, reinterpret_cast<const int*>(saved + o.s_index) + from,
-                           reinterpret_cast<const float*>(saved + o.s_at) + from, n, o.K, (int)v_base, Vw, G, ldg);
+        hipLaunchKernelGGL(k_obj_entries, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, index + from, at + from, n, o.K, (int)v_base, Vw, G,
+                           ldg);
       });
 }
 

@@ -5,7 +5,8 @@
 // Notation of a row: z logits, y = c tanh(z / c) (y = z without a cap), T the temperature, "entries" the vocabulary entries that
 // the teacher gives, "others" the rest.
 //
-//   forward   k_entries        the teacher's entries of every row in ascending order, and where each vocabulary tile's begin
+//   forward   k_entries        the teacher's entries of every row in ascending order, and where each vocabulary tile's begin (for
+//                              256-row tiles; calls with smaller tiles find them as they need them: TileEntries)
 //             (logits)         ObjEpilogue: the label's y and the entries' y out of the accumulators; partial log-sum-exps of the
 //                              others alone, at 1 / T and, where a row needs both, at 1
 //             k_obj_finalize   log-sum-exps, losses, what the backward needs of each row and at each entry
@@ -57,20 +58,103 @@ __device__ __forceinline__ void merge_sums(float& m, float& l, float& k, float m
 // ---------------------------------------------------------------------------
 // forward epilogue
 // ---------------------------------------------------------------------------
-struct ObjEpilogue {
+struct ObjTile {
   const int* labels_c;                 // null: none
   float2* part;                        // [n_vt][part_stride] (maximum, sum) of the others
   float* part_label;                   // the sum at the second exponent; null: rows have one
   size_t part_stride;
   float* tgt;                          // y of the label, unless it is an entry
-  const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile; null: no teacher
-  const int* index;                    // [rows][K] ascending
-  float* entry_y;                      // [rows][K] y of the entries
-  int K;
+  int K;                               // 0: no teacher
+  int* index;                          // [rows][K] the entries, kNoEntry where there is none
+  float* entry_y;                      // [rows][K] their y
+  const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile, with `index` ascending; null where the tile
+                                       // finds its entries among the caller's and writes `index`, `logit` and `info` (TileEntries)
+  const int* index_in_c;
+  const void* logit_in_c;
+  int logit_bf16;
+  float* logit;
+  int* info;
   float cap, exponent, exponent_label;
+  int power;                           // T where it is 2 or 4: the second exponential is a power of the first; else 0
+};
 
-  template <int TB>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+// A tile's entries without a launch before it, for tiles that are all in one round of workgroups: its threads look through the
+// entries of its rows and note in LDS which of the tile's kWidth vocabulary entries are the teacher's (a bit each) and at which place
+// of the row's list (the first, where an index comes twice).  The tile that has an entry writes what the following kernel reads of
+// it, the first tile also what is no entry.  512 x 256 x 4096 with 20 entries: 8.6 us of a launch of sorting, 1 us here.
+template <int kThreadsOfTile, class F>
+__device__ __forceinline__ void each_entry(const int* __restrict__ index, int rows, int K, F f) {     // f(row, place in its list, index)
+  constexpr int kAtOnce = 8;
+  const int n = rows * K;
+  const float by_k = 1.f / (float)K;
+  for (int i0 = threadIdx.x; i0 < n; i0 += kAtOnce * kThreadsOfTile) {
+    int v[kAtOnce];
+#pragma unroll
+    for (int b = 0; b < kAtOnce; ++b) v[b] = index[i0 + b * kThreadsOfTile < n ? i0 + b * kThreadsOfTile : n - 1];
+#pragma unroll
+    for (int b = 0; b < kAtOnce; ++b) {
+      const int i = i0 + b * kThreadsOfTile;
+      const int r = (int)(((float)i + 0.5f) * by_k);       // i / K: i < 2^15, K <= 2^8, half of 1 / K is more than the product is off by
+      if (i < n) f(r, i - r * K, v[b]);
+    }
+  }
+}
+template <int kRows, int kWidth, int kThreadsOfTile>
+struct TileEntries {
+  static constexpr int kWords = kWidth / 32;
+  static constexpr int kBytes = kRows * (kWords + kWidth) * 4;
+  static_assert(kRows * kMaxEntries <= 1 << 15 && kBytes % 16 == 0, "each_entry");
+  unsigned* bits;                      // [kRows][kWords]
+  int* place;                          // [kRows][kWidth], where there is a bit
+  TileEntries() = default;
+  // smem: kBytes, 16-byte aligned, that nobody uses; all threads of the workgroup
+  __device__ __forceinline__ TileEntries(char* smem, const ObjTile& e, int s0, int rows, int v0, int V, bool first_tile) {
+    bits = reinterpret_cast<unsigned*>(smem);
+    place = reinterpret_cast<int*>(bits + kRows * kWords);
+    for (int i = threadIdx.x; i < kRows * kWords; i += kThreadsOfTile) bits[i] = 0;
+    for (int i = threadIdx.x; i < kRows * kWidth / 4; i += kThreadsOfTile) reinterpret_cast<int4*>(place)[i] = make_int4(kNoEntry, kNoEntry, kNoEntry, kNoEntry);
+    const int here = rows - s0 < kRows ? rows - s0 : kRows;
+    const size_t from = (size_t)s0 * e.K;
+    const int* const index_in = e.index_in_c + from;
+    auto in_tile = [&](int v) { return (unsigned)(v - v0) < (unsigned)kWidth && v < V; };
+    if (first_tile)
+      for (int r = threadIdx.x; r < here; r += kThreadsOfTile) e.info[s0 + r] = e.K;
+    __syncthreads();
+    each_entry<kThreadsOfTile>(index_in, here, e.K, [&](int r, int k, int v) {
+      if (!in_tile(v)) return;
+      atomicMin(place + r * kWidth + v - v0, k);
+      atomicOr(bits + r * kWords + (v - v0) / 32, 1u << ((v - v0) & 31));
+    });
+    __syncthreads();
+    each_entry<kThreadsOfTile>(index_in, here, e.K, [&](int r, int k, int v) {
+      const size_t at = from + (size_t)r * e.K + k;
+      if (in_tile(v)) {
+        const bool kept = place[r * kWidth + v - v0] == k;
+        e.index[at] = kept ? v : kNoEntry;
+        if (kept) e.logit[at] = e.logit_bf16 ? (float)static_cast<const __bf16*>(e.logit_in_c)[at] : static_cast<const float*>(e.logit_in_c)[at];
+      } else if (first_tile && (unsigned)v >= (unsigned)V) {
+        e.index[at] = kNoEntry;
+        if (v >= V) e.info[s0 + r] = -1;             // behind e.K, with a barrier in between
+      }
+    });
+  }
+};
+
+// kWhat: what is known when compiled, 0 or kObjCap for calls without a teacher; kObjAny asks the arguments.
+// Known against asked, us: 16384 x 3584 x 256000 with a cap 20780, 20980; with a teacher the same.
+constexpr int kObjCap = 1, kObjAny = 2;
+template <int kWhat>
+struct ObjEpilogue : ObjTile {
+  typedef ObjEpilogue<kObjAny> Small;          // of the smaller tiles
+  ObjEpilogue() = default;
+  explicit ObjEpilogue(const ObjTile& t) : ObjTile(t) {}
+
+  template <class C>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+    constexpr int TB = C::TB;
+    constexpr bool kSorted = C::EB == kTile;           // entries from k_entries
+    typedef TileEntries<C::EB, kTile, C::kThreads> Found;
+    const bool teacher = kWhat == kObjAny && K > 0, two = kWhat == kObjAny && part_label != nullptr;
     const int v0 = vt * kTile;
     const int g = lane >> 4, c = lane & 15;
     const int va = v0 + wa * 128 + 32 * g;             // a lane's 32 consecutive entries of each of its TB rows
@@ -79,10 +163,10 @@ struct ObjEpilogue {
     for (int u = 0; u < TB; ++u) {
       const int s_local = s0 + wb * (16 * TB) + 16 * u + c, s_in = s_local < rows ? s_local : rows - 1;
       y_u[u] = labels_c ? labels_c[s_in] : -1;
-      from[u] = starts ? starts[(size_t)vt * part_stride + s_in] : 0;
-      to[u] = starts ? starts[(size_t)(vt + 1) * part_stride + s_in] : 0;
+      from[u] = teacher && kSorted ? starts[(size_t)vt * part_stride + s_in] : 0;
+      to[u] = teacher && kSorted ? starts[(size_t)(vt + 1) * part_stride + s_in] : 0;
     }
-    if (cap > 0.f) {
+    if (kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap) {
       const float scale = 2.f * kLog2e / cap;
 #pragma unroll
       for (int t = 0; t < kTA16; ++t)
@@ -91,30 +175,62 @@ struct ObjEpilogue {
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[t][u][r] = capped(acc[t][u][r], cap, scale);
     }
-    if (starts) {
+    float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
+    // The entries' y out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's;
+    // place_of(i): its place in the row's list.
+    auto take = [&](int u, unsigned mine, auto place_of) {
+      const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+      if (!__any(mine != 0)) return;
 #pragma unroll
-      for (int u = 0; u < TB; ++u) {
-        const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
-        const int end = s_local < rows ? to[u] : 0;
-        unsigned mine = 0;                             // bit i: entry va + i is the teacher's
-        int first = 0;                                 // place of the lowest of them in the row's list
-        for (int e = from[u]; e < end; ++e) {
-          const int rel = index[(size_t)s_local * K + e] - va;
-          if ((unsigned)rel < 32u) {
-            if (!mine) first = e;
-            mine |= 1u << rel;
+      for (int t = 0; t < kTA16; ++t) {
+        if (!__any((mine >> (4 * t)) & 15u)) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((mine >> (4 * t + r)) & 1u) {
+            entry_y[(size_t)s_local * K + place_of(4 * t + r)] = acc[t][u][r];
+            acc[t][u][r] = kMasked;
           }
+      }
+    };
+    if (teacher) {
+      if constexpr (kSorted) {
+        // The first entries of all rows at once: one after the other each would wait for the one before.
+        constexpr int kAtOnce = 4;
+        int entry[TB][kAtOnce];
+#pragma unroll
+        for (int u = 0; u < TB; ++u) {
+          const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+          if (s_local >= rows) to[u] = 0;
+          const int* const row = index + (size_t)(s_local < rows ? s_local : rows - 1) * K;
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) entry[u][i] = row[from[u] + i < K ? from[u] + i : K - 1];
         }
-        if (!__any(mine != 0)) continue;
 #pragma unroll
-        for (int t = 0; t < kTA16; ++t) {
-          if (!__any((mine >> (4 * t)) & 15u)) continue;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if ((mine >> (4 * t + r)) & 1u) {
-              entry_y[(size_t)s_local * K + first + __builtin_popcount(mine & ((1u << (4 * t + r)) - 1u))] = acc[t][u][r];
-              acc[t][u][r] = kMasked;
+        for (int u = 0; u < TB; ++u) {
+          const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+          unsigned mine = 0;
+          int first = 0;                               // place of the lowest of them
+          auto note = [&](int e, int v) {
+            const int rel = v - va;
+            if ((unsigned)rel < 32u && e < to[u]) {
+              if (!mine) first = e;
+              mine |= 1u << rel;
             }
+          };
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) note(from[u] + i, entry[u][i]);
+          for (int e = from[u] + kAtOnce; e < to[u]; ++e) note(e, index[(size_t)s_local * K + e]);
+          take(u, mine, [&](int i) { return first + __builtin_popcount(mine & ((1u << i) - 1u)); });
+        }
+      } else {
+        static_assert(Found::kBytes + 2 * C::EB * 12 <= C::kLds, "beside the triples");
+        const Found found(smem, *this, s0, rows, v0, V, vt == 0);
+        xch = reinterpret_cast<float*>(smem + Found::kBytes);
+#pragma unroll
+        for (int u = 0; u < TB; ++u) {
+          const int r = wb * (16 * TB) + 16 * u + c;   // past the last row: no bits
+          const int* const at = found.place + r * kTile + va - v0;
+          take(u, found.bits[r * Found::kWords + (va - v0) / 32], [&](int i) { return at[i]; });
         }
       }
     }
@@ -128,7 +244,6 @@ struct ObjEpilogue {
             for (int u = 0; u < TB; ++u) acc[t][u][r] = kMasked;
           }
     }
-    const bool two = part_label != nullptr;
     float m_u[TB], l_u[TB], k_u[TB];
 #pragma unroll
     for (int u = 0; u < TB; ++u) {
@@ -137,20 +252,33 @@ struct ObjEpilogue {
       for (int t = 0; t < kTA16; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][u][r]);
-#pragma unroll
-      for (int t = 0; t < kTA16; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
-      if (two) {
+      if (two && power) {
 #pragma unroll
         for (int t = 0; t < kTA16; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
+          for (int r = 0; r < 4; ++r) {
+            const float x = fast_exp2((acc[t][u][r] - m) * exponent), x2 = x * x;
+            l += x;
+            k = power == 2 ? k + x2 : __builtin_fmaf(x2, x2, k);
+          }
+      } else {
+#pragma unroll
+        for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
+        if (two) {
+#pragma unroll
+          for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
+        }
       }
 #pragma unroll
       for (int o = 16; o <= 32; o <<= 1)
         merge_sums(m, l, k, __shfl_xor(m, o), __shfl_xor(l, o), two ? __shfl_xor(k, o) : 0.f, exponent, exponent_label, two);
       m_u[u] = m; l_u[u] = l; k_u[u] = k;
+
+      // y of the label straight from the accumulator that holds it
       const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
       const int y = s_local < rows ? y_u[u] : -1;
       const int rel = y - (v0 + wa * 128);
@@ -165,8 +293,6 @@ struct ObjEpilogue {
         tgt[s_local] = val;
       }
     }
-    // the main loop ended with a barrier, LDS is free
-    float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves
     if (wa == 1 && lane < 16) {
 #pragma unroll
       for (int u = 0; u < TB; ++u) {
@@ -198,7 +324,7 @@ struct ObjEpilogue {
 constexpr int kFewWaves = 8, kFewV = 16 * kFewWaves, kFewDepth = 4;
 template <int TB>
 __global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __restrict__ H, const __bf16* __restrict__ W, int rows, int d, int V,
-                                                            ObjEpilogue e) {
+                                                            ObjTile e) {
   __shared__ float xch[kFewWaves][16 * TB][3];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int vt = blockIdx.x, v0 = vt * kFewV + 16 * wave;
@@ -254,6 +380,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __rest
     multiply(x);
   }
 
+  typedef TileEntries<16 * TB, kFewV, 64 * kFewWaves> Found;
+  __shared__ __attribute__((aligned(16))) char found_sh[Found::kBytes];
+  const Found found = e.K ? Found(found_sh, e, 0, rows, vt * kFewV, V, vt == 0) : Found();
+
   // as ObjEpilogue: a lane has, of row 16 u + c, the four entries from va on
   const int va = v0 + 4 * g;
   const bool two = e.part_label != nullptr;
@@ -271,17 +401,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __rest
       for (int r = 0; r < 4; ++r)
         if (at == r && va + r < V) e.tgt[s] = y[r];
     }
-    if (e.starts) {
-      const int end = in ? e.starts[(size_t)(vt + 1) * e.part_stride + s_in] : 0;
-      for (int i = e.starts[(size_t)vt * e.part_stride + s_in]; i < end; ++i) {
-        const int at = e.index[(size_t)s * e.K + i] - va;
+    if (e.K) {
+      const unsigned mine = found.bits[s * Found::kWords + (va - vt * kFewV) / 32] >> ((va - vt * kFewV) & 31);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (at == r) {
-            e.entry_y[(size_t)s * e.K + i] = y[r];
-            y[r] = kMasked;
-          }
-      }
+      for (int r = 0; r < 4; ++r)
+        if ((mine >> r) & 1u) {
+          e.entry_y[(size_t)s * e.K + found.place[s * kFewV + va - vt * kFewV + r]] = y[r];
+          y[r] = kMasked;
+        }
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -315,8 +442,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __rest
 // The teacher's entries of a group of rows in ascending order.  A wave sorts a row, P entries a lane, with a bitonic network on
 // (index, place) in 64 bits: of entries with the same index the first comes first and the others are dropped.  An index below 0 is
 // no entry; one at or behind V makes the row bad.
-//   index, logit [rows][K] (float32), the rest of a row kNoEntry; info[row] = entries, or -1
-//   starts [n_vt + 1][stride]: entries before vocabulary entry `width` vt
+//   index, logit [rows][K] (float32), the rest of a row kNoEntry; info[row] = entries, or -1 where the row is bad
+//   starts [n_vt + 1][stride]: entries before vocabulary entry 256 vt
 // 32768 rows of 256: 510 us with every entry compared to all others of its row, in LDS.
 // ---------------------------------------------------------------------------
 constexpr int kEntryRows = 16;              // of a workgroup, one wave each: 32-byte pieces of starts
@@ -349,7 +476,7 @@ __device__ __forceinline__ void sort_entries(unsigned long long (&x)[P], int lan
 }
 template <int P>
 __global__ __launch_bounds__(64 * kEntryRows) void k_entries(
-    const int* __restrict__ index_in, const void* __restrict__ logit_in, int logit_bf16, int rows, int K, int V, int n_vt, int width,
+    const int* __restrict__ index_in, const void* __restrict__ logit_in, int logit_bf16, int rows, int K, int V, int n_vt,
     int* __restrict__ index, float* __restrict__ logit, int* __restrict__ info, unsigned short* __restrict__ starts, size_t stride) {
   __shared__ int key_sh[kEntryRows][64 * P];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -396,7 +523,7 @@ __global__ __launch_bounds__(64 * kEntryRows) void k_entries(
   const int r = threadIdx.x % kEntryRows, row = blockIdx.x * kEntryRows + r;
   if (row >= rows) return;
   for (int vt = threadIdx.x / kEntryRows; vt <= n_vt; vt += 64) {
-    const int v0 = vt < n_vt ? vt * width : kNoEntry;
+    const int v0 = vt < n_vt ? vt * kTile : kNoEntry;
     int lo = 0, hi = K;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -420,7 +547,7 @@ struct ObjFinal {
   const int* labels_c;
   const float* weights_c;
   int ignore_index;
-  const int* index;                   // [rows][K] and their logits and y, ascending
+  const int* index;                   // [rows][K] (kNoEntry: none), and the entries' logits and y
   const float* logit;
   const float* entry_y;
   const int* info;
@@ -468,11 +595,33 @@ template <class X> __device__ __forceinline__ X sum16(X x) {
   return x;
 }
 
-// kAll: the rows are all of the call's, whose loss is formed here too (one launch less).
-template <bool kAll>
+// kAll: the rows are all of the call's, whose loss is formed here too (one launch less).  P: entries of a lane, all of which are
+// on their way with the first loads (read in a loop for each use, 512 rows of 20 entries took 8.6 us).
+template <bool kAll, int P>
 __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal a, ObjLoss o) {
   __shared__ float sh[kObjRows][kObjGroups][3];
   const bool two = a.part_label != nullptr;
+  const int r = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  const int s = blockIdx.x * kObjRows + r;
+  const bool in = s < a.rows;
+  const int s_in = in ? s : a.rows - 1;
+  const size_t at0 = (size_t)s_in * a.K;
+  int v_p[P ? P : 1];
+  float y_p[P ? P : 1], t_p[P ? P : 1];                          // of the row's entries lane, lane + 16, ...
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int e = lane + 16 * i, e_in = e < a.K ? e : a.K - 1;
+    const int v = a.index[at0 + e_in];
+    y_p[i] = a.entry_y[at0 + e_in];
+    t_p[i] = a.logit[at0 + e_in];
+    v_p[i] = e < a.K ? v : kNoEntry;
+  }
+  const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
+  const float weight = a.weights_c ? a.weights_c[s_in] : 1.f;
+  const bool bad_entry = P && a.info[s_in] < 0;
+  const bool given = P && a.teacher_lse_c != nullptr;
+  const float given_lse = given ? a.teacher_lse_c[s_in] : 0.f;
+  const float tgt = a.tgt[s_in];
   {
     const int r = threadIdx.x & (kObjRows - 1), g = threadIdx.x / kObjRows;
     const int s = blockIdx.x * kObjRows + r;
@@ -505,10 +654,6 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     sh[r][g][0] = m; sh[r][g][1] = l; sh[r][g][2] = k;
   }
   __syncthreads();
-  const int r = threadIdx.x >> 4, lane = threadIdx.x & 15;
-  const int s = blockIdx.x * kObjRows + r;
-  const bool in = s < a.rows;
-  const int s_in = in ? s : a.rows - 1;
   // the others
   const float m_lane = sh[r][lane][0];
   const float m = max16(m_lane);
@@ -517,34 +662,39 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const bool others = m > 0.5f * kMasked;                        // there are some
 
   // the entries
-  const int n = a.K ? max(a.info[s_in], 0) : 0;
-  const bool bad_entry = a.K && a.info[s_in] < 0;
-  const size_t at0 = (size_t)s_in * a.K;
+  auto entries = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (v_p[i] != kNoEntry) f(i);
+  };
   float my = kMasked, mt = kMasked;
-  for (int e = lane; e < n; e += 16) {
-    my = fmaxf(my, a.entry_y[at0 + e]);
-    mt = fmaxf(mt, a.logit[at0 + e]);
-  }
+  int some = 0;
+  entries([&](int i) {
+    my = fmaxf(my, y_p[i]);
+    mt = fmaxf(mt, t_p[i]);
+    some = 1;
+  });
   my = max16(my);
   mt = max16(mt);
+  some = sum16(some);
   float ly = 0.f, ky = 0.f, lt = 0.f;
-  for (int e = lane; e < n; e += 16) {
-    const float y = a.entry_y[at0 + e] - my;
+  entries([&](int i) {
+    const float y = y_p[i] - my;
     ly += fast_exp2(y * a.exponent);
     if (two) ky += fast_exp2(y * a.exponent_label);
-    lt += expf((a.logit[at0 + e] - mt) * a.inv_t);
-  }
+    lt += expf((t_p[i] - mt) * a.inv_t);
+  });
   ly = sum16(ly);
   ky = sum16(ky);
   lt = sum16(lt);
-  const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
   const bool labelled = a.labels_c && y != a.ignore_index;
   const bool valid = labelled && (unsigned)y < (unsigned)a.V;
   float y_entry = 0.f;                                           // the label's logit where it is an entry
   int is_entry = 0;
   if (valid)
-    for (int e = lane; e < n; e += 16)
-      if (a.index[at0 + e] == y) y_entry = a.entry_y[at0 + e], is_entry = 1;
+    entries([&](int i) {
+      if (v_p[i] == y) y_entry = y_p[i], is_entry = 1;
+    });
   y_entry = sum16(y_entry);
   is_entry = sum16(is_entry);
 
@@ -559,23 +709,21 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   // log of the others' share, with the two logarithms of sums and not with those of the log-sum-exps
   const float log_share = (m - m_all) * a.inv_t + (logf(l) - log_all);
 
-  const float weight = a.weights_c ? a.weights_c[s_in] : 1.f;
-  const float nll = valid ? (m_all - (is_entry ? y_entry : a.tgt[s_in])) + log_label : 0.f;
+  const float nll = valid ? (m_all - (is_entry ? y_entry : tgt)) + log_label : 0.f;
 
   // the teacher's shares; `rest`: what it leaves to the others
-  const bool given = a.teacher_lse_c != nullptr;
-  const bool taught = n > 0 && (given || !(mt <= 0.5f * kMasked));          // true for NaN
-  const float lse_teacher = given ? a.teacher_lse_c[s_in] : mt * a.inv_t + logf(lt);
+  const bool taught = some > 0 && (given || !(mt <= 0.5f * kMasked));          // true for NaN
+  const float lse_teacher = given ? given_lse : mt * a.inv_t + logf(lt);
   double sum_q = 0.0;
   float kd = 0.f;
-  for (int e = lane; e < n; e += 16) {
+  entries([&](int i) {
     // relative to the largest logits, so that equal distributions leave nothing
-    const float log_q = given ? a.logit[at0 + e] * a.inv_t - lse_teacher : (a.logit[at0 + e] - mt) * a.inv_t - logf(lt);
-    const float log_p = (a.entry_y[at0 + e] - m_all) * a.inv_t - log_all;
+    const float log_q = given ? t_p[i] * a.inv_t - lse_teacher : (t_p[i] - mt) * a.inv_t - logf(lt);
+    const float log_p = (y_p[i] - m_all) * a.inv_t - log_all;
     const float q = expf(log_q);
     sum_q += (double)q;
     if (!(q == 0.f)) kd += q * (log_q - log_p);
-  }
+  });
   sum_q = sum16(sum_q);
   kd = sum16(kd);
   const float total_q = (float)sum_q;
@@ -633,7 +781,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
       row2.base = lse;
       row2.at = on_p;
       if (on_p == 0.f) row2.base = __builtin_inff();
-    } else if (a.K) {
+    } else if (P) {
       row.base = base;
       row.at = kd_others + on_p * share;
     } else {
@@ -644,13 +792,14 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     a.rows_c[s] = row;
     if (a.rows2_c) a.rows2_c[s] = row2;
   }
-  if (!a.K) return;
-  for (int e = lane; e < a.K; e += 16) {
-    const int v = a.index[at0 + e];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int e = lane + 16 * i, v = v_p[i];
+    if (e >= a.K) continue;
     float x = 0.f;
-    if (e < n) {
-      const float ye = a.entry_y[at0 + e];
-      const float log_q = given ? a.logit[at0 + e] * a.inv_t - lse_teacher : (a.logit[at0 + e] - mt) * a.inv_t - logf(lt);
+    if (v != kNoEntry) {
+      const float ye = y_p[i];
+      const float log_q = given ? t_p[i] * a.inv_t - lse_teacher : (t_p[i] - mt) * a.inv_t - logf(lt);
       if (on_kd != 0.f) x = on_kd * (expf((ye - m_all) * a.inv_t - log_all) * (total_q + rest) - expf(log_q));
       if (on_p != 0.f) x += on_p * expf((ye - m_all) - log_label);
       if (valid && v == y) x -= on_label;
@@ -664,11 +813,26 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   }
 }
 
-// loss = sum of the rows' / divisor, in a fixed order in 64 bits, and the header of `saved`.  One workgroup.
-__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S, ObjLoss o) {
+// From every thread's sum, count and whether an index is out of range (1024 threads), in a fixed order.
+__device__ __forceinline__ void reduce_obj_loss(const ObjLoss& o, double a, long long n, int bad) {
   __shared__ double sh[16];
   __shared__ long long sh_n[16];
   __shared__ int sh_bad[16];
+  for (int k = 32; k > 0; k >>= 1) {
+    a += __shfl_xor(a, k);
+    n += __shfl_xor(n, k);
+    bad |= __shfl_xor(bad, k);
+  }
+  const int w = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) { sh[w] = a; sh_n[w] = n; sh_bad[w] = bad; }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  a = 0.0; n = 0; bad = 0;
+  for (int i = 0; i < 16; ++i) { a += sh[i]; n += sh_n[i]; bad |= sh_bad[i]; }
+  write_loss(o, a, n, bad);
+}
+// One workgroup, bound by the latency of its loads: eight rounds of them at a time.
+__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S, ObjLoss o) {
   double a = 0.0;
   long long n = 0;
   int bad = 0;
@@ -688,18 +852,41 @@ __global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row
       bad |= c[k] < 0;
     }
   }
-  for (int o2 = 32; o2 > 0; o2 >>= 1) {
-    a += __shfl_xor(a, o2);
-    n += __shfl_xor(n, o2);
-    bad |= __shfl_xor(bad, o2);
+  reduce_obj_loss(o, a, n, bad);
+}
+
+// k_obj_finalize and k_obj_loss of calls without a teacher that are few rows and vocabulary tiles (finalize_in_one), from one
+// workgroup: a thread has a row and all of its pairs in flight at once, as k_finalize_loss.
+__global__ __launch_bounds__(1024) void k_obj_finalize_one(ObjFinal a, ObjLoss o) {
+  const int s = threadIdx.x;
+  float loss = 0.f;
+  int count = 0;
+  if (s < a.rows) {
+    float2 p[kFinOneTiles];
+#pragma unroll
+    for (int vt = 0; vt < kFinOneTiles; ++vt) p[vt] = vt < a.n_vt ? a.part[(size_t)vt * a.part_stride + s] : make_float2(kMasked, 0.f);
+    const int y = a.labels_c[s];
+    const float z_y = a.tgt[s], weight = a.weights_c ? a.weights_c[s] : 1.f;
+    float m = kMasked, l = 0.f;
+    fold_lse(m, l, p);
+    const float log_l = logf(l), lse = m + log_l;
+    const bool valid = y != a.ignore_index && (unsigned)y < (unsigned)a.V;
+    const float nll = valid ? (m - z_y) + log_l : 0.f;
+    const bool on = valid && weight != 0.f;
+    if (on) loss = weight * (a.label_coef * nll + a.z_coef * lse * lse);
+    count = y == a.ignore_index ? 0 : valid ? 1 : -1;
+    if (a.nll_c) a.nll_c[s] = nll;
+    if (a.lse_c) a.lse_c[s] = lse;
+    if (a.rows_c) {
+      ObjRow row;
+      row.label = on ? y : -1;
+      row.label_term = on ? weight * a.label_coef : 0.f;
+      row.at = on ? row.label_term + 2.f * weight * a.z_coef * lse : 0.f;
+      row.base = row.at == 0.f ? __builtin_inff() : lse;
+      a.rows_c[s] = row;
+    }
   }
-  const int w = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) { sh[w] = a; sh_n[w] = n; sh_bad[w] = bad; }
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  a = 0.0; n = 0; bad = 0;
-  for (int i = 0; i < 16; ++i) { a += sh[i]; n += sh_n[i]; bad |= sh_bad[i]; }
-  write_loss(o, a, n, bad);
+  reduce_obj_loss(o, (double)loss, count > 0, count < 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -709,6 +896,21 @@ struct ObjGrad {
   const ObjHeader* head;
   const ObjRow* rows;
   const ObjRow2* rows2;              // read where head->two
+  const int* index;                  // [rows][K] the teacher's entries and the gradient there, for tiles that put them in themselves
+  const float* at;
+  int K;                             // 0: none, or k_obj_entries does it
+  static constexpr bool kPatch = true;
+  // `rows` rows of a tile from row s0 on, kWidth vocabulary entries from v0 on: into the tile at `staged`
+  template <int kThreadsOfTile>
+  __device__ __forceinline__ void patch(int s0, int n_rows, int v0, int width, int V, char* staged, int row_bytes) const {
+    if (!K) return;
+    __syncthreads();
+    const size_t from = (size_t)s0 * K;
+    each_entry<kThreadsOfTile>(index + from, n_rows, K, [&](int r, int k, int v) {
+      if ((unsigned)(v - v0) < (unsigned)width && v < V)
+        *reinterpret_cast<__bf16*>(staged + r * row_bytes + 2 * (v - v0)) = (__bf16)at[from + (size_t)r * K + k];
+    });
+  }
   struct Row { ObjRow a; ObjRow2 b; };
   __device__ __forceinline__ Row load(int s) const {
     Row r;

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_ls
     pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
     gemm_mainloop_small<C>(acc, pa, pb, smem, 0, d);
   }
-  epilogue.template operator()<C::TB>(acc, rows, V, vt, s0, wa, wb, lane, smem);
+  epilogue.template operator()<C>(acc, rows, V, vt, s0, wa, wb, lane, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -121,6 +121,7 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dl
       }
     });
   }
+  if constexpr (E::kPatch) grad.template patch<C::kThreads>(s0, rows - s0 < C::EB ? rows - s0 : C::EB, v0, C::EA, V, smem, kStageRow);
   __syncthreads();
   constexpr int kLanesPerRow = C::EA / 8, kRowsPerPass = C::kThreads / kLanesPerRow;
   const int col = (threadIdx.x % kLanesPerRow) * 8;
