@@ -599,6 +599,7 @@ bool set_kernel_attributes() {   // on the current device
   set_forward_kernels<ObjEpilogue<0>>(set);
   set_forward_kernels<ObjEpilogue<kObjCap>>(set);
   set_forward_kernels<ObjEpilogue<kObjAny>>(set);
+  set((const void*)k_fwd_gemm_lse_small<TileFew, ObjEpilogue<kObjAny>>);
   set_dlogits_kernels<ObjGrad>(set);
   set((const void*)k_bwd_gemm_dh_small<Tile64>);
   set((const void*)k_bwd_gemm_dh_small<Tile64Lone>);

@@ -418,6 +418,7 @@ __device__ __forceinline__ void lse_epilogue(f32x4 (&acc)[kTA16][TB], const int*
 
 struct LseEpilogue {
   typedef LseEpilogue Small;           // that of the smaller tiles
+  static constexpr bool kWhole = true; // tiles are 256 vocabulary entries wide
   const int* labels_c;
   float2* part;
   size_t part_stride;

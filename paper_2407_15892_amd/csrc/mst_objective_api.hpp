@@ -10,7 +10,7 @@ namespace {
 struct ObjPlan {
   Plan p;
   int K;
-  int few;               // row tiles of 16 of the forward of a few rows (k_obj_few); 0: the plain forward's tiles
+  bool few;              // the forward's tiles are TileFew, not the plain forward's
   int n_vt;              // vocabulary tiles of the forward
   // forward workspace: the plain forward's (its nll: the rows' losses), then
   size_t f_part_few, f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
@@ -21,8 +21,8 @@ struct ObjPlan {
 // the entries of its rows.
 constexpr int kPatchEntries = 64;
 
-// Calls of a few rows have a forward of their own.
-int few_rows(const Plan& p) { return p.S > p.fwd_group_rows ? 0 : p.S <= 16 ? 1 : p.S <= 32 ? 2 : 0; }
+// See TileFew.
+bool use_tile_few(const Plan& p) { return p.S <= TileFew::EB && p.S <= p.fwd_group_rows && 2 * p.n_vt <= kNumCu; }
 
 // Byte ranges of a call's arguments: no output may overlap anything else.
 struct Ranges {
@@ -58,8 +58,8 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
   o->p.streamed = 0;      // that order stores no dlogits to put the entries into
   o->K = K;
-  o->few = few_rows(o->p);
-  o->n_vt = o->few ? (int)((V + kFewV - 1) / kFewV) : o->p.n_vt;
+  o->few = use_tile_few(o->p);
+  o->n_vt = o->few ? (int)((V + TileFew::EA - 1) / TileFew::EA) : o->p.n_vt;
   const size_t rows = (size_t)o->p.fwd_group_rows, k = (size_t)K;
   size_t off = o->p.f_total;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
@@ -235,8 +235,8 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   if (o.few) {
     {
       Scope sc(st, MST_K_FWD_GEMM_LSE);
-      hipLaunchKernelGGL(o.few == 1 ? k_obj_few<1> : k_obj_few<2>, dim3(o.n_vt), dim3(64 * kFewWaves), 0, st, H, W, (int)p.S, (int)p.d, (int)p.V,
-                         tile_of(0));
+      hipLaunchKernelGGL((k_fwd_gemm_lse_small<TileFew, ObjEpilogue<kObjAny>>), dim3(even_grid(o.n_vt, 1)), dim3(TileFew::kThreads), TileFew::kLds,
+                         st, H, W, (int)p.S, (int)p.d, (int)p.V, 1, o.n_vt, ObjEpilogue<kObjAny>(tile_of(0)));
     }
     after(0, (int)p.S);
   } else {

@@ -146,18 +146,19 @@ constexpr int kObjCap = 1, kObjAny = 2;
 template <int kWhat>
 struct ObjEpilogue : ObjTile {
   typedef ObjEpilogue<kObjAny> Small;          // of the smaller tiles
+  static constexpr bool kWhole = false;
   ObjEpilogue() = default;
   explicit ObjEpilogue(const ObjTile& t) : ObjTile(t) {}
 
   template <class C>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
-    constexpr int TB = C::TB;
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[C::TA][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+    constexpr int TA = C::TA, TB = C::TB, kPer = 4 * TA, kWaveV = 16 * TA;    // vocabulary entries of a lane, of a wave
     constexpr bool kSorted = C::EB == kTile;           // entries from k_entries
-    typedef TileEntries<C::EB, kTile, C::kThreads> Found;
+    typedef TileEntries<C::EB, C::EA, C::kThreads> Found;
     const bool teacher = kWhat == kObjAny && K > 0, two = kWhat == kObjAny && part_label != nullptr;
-    const int v0 = vt * kTile;
+    const int v0 = vt * C::EA;
     const int g = lane >> 4, c = lane & 15;
-    const int va = v0 + wa * 128 + 32 * g;             // a lane's 32 consecutive entries of each of its TB rows
+    const int va = v0 + wa * kWaveV + kPer * g;        // a lane's consecutive entries of each of its TB rows
     int y_u[TB], from[TB], to[TB];                     // on their way meanwhile
 #pragma unroll
     for (int u = 0; u < TB; ++u) {
@@ -169,7 +170,7 @@ struct ObjEpilogue : ObjTile {
     if (kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap) {
       const float scale = 2.f * kLog2e / cap;
 #pragma unroll
-      for (int t = 0; t < kTA16; ++t)
+      for (int t = 0; t < TA; ++t)
 #pragma unroll
         for (int u = 0; u < TB; ++u)
 #pragma unroll
@@ -182,7 +183,7 @@ struct ObjEpilogue : ObjTile {
       const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
       if (!__any(mine != 0)) return;
 #pragma unroll
-      for (int t = 0; t < kTA16; ++t) {
+      for (int t = 0; t < TA; ++t) {
         if (!__any((mine >> (4 * t)) & 15u)) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -212,7 +213,7 @@ struct ObjEpilogue : ObjTile {
           int first = 0;                               // place of the lowest of them
           auto note = [&](int e, int v) {
             const int rel = v - va;
-            if ((unsigned)rel < 32u && e < to[u]) {
+            if ((unsigned)rel < (unsigned)kPer && e < to[u]) {
               if (!mine) first = e;
               mine |= 1u << rel;
             }
@@ -229,14 +230,15 @@ struct ObjEpilogue : ObjTile {
 #pragma unroll
         for (int u = 0; u < TB; ++u) {
           const int r = wb * (16 * TB) + 16 * u + c;   // past the last row: no bits
-          const int* const at = found.place + r * kTile + va - v0;
-          take(u, found.bits[r * Found::kWords + (va - v0) / 32], [&](int i) { return at[i]; });
+          const int* const at = found.place + r * C::EA + va - v0;
+          const unsigned word = found.bits[r * Found::kWords + (va - v0) / 32];
+          take(u, (word >> ((va - v0) & 31)) & (0xffffffffu >> (32 - kPer)), [&](int i) { return at[i]; });
         }
       }
     }
-    if (v0 + kTile > V) {
+    if (v0 + C::EA > V) {
 #pragma unroll
-      for (int t = 0; t < kTA16; ++t)
+      for (int t = 0; t < TA; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (va + 4 * t + r >= V) {
@@ -249,12 +251,12 @@ struct ObjEpilogue : ObjTile {
     for (int u = 0; u < TB; ++u) {
       float m = kMasked, l = 0.f, k = 0.f;
 #pragma unroll
-      for (int t = 0; t < kTA16; ++t)
+      for (int t = 0; t < TA; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][u][r]);
       if (two && power) {
 #pragma unroll
-        for (int t = 0; t < kTA16; ++t)
+        for (int t = 0; t < TA; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float x = fast_exp2((acc[t][u][r] - m) * exponent), x2 = x * x;
@@ -263,12 +265,12 @@ struct ObjEpilogue : ObjTile {
           }
       } else {
 #pragma unroll
-        for (int t = 0; t < kTA16; ++t)
+        for (int t = 0; t < TA; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
         if (two) {
 #pragma unroll
-          for (int t = 0; t < kTA16; ++t)
+          for (int t = 0; t < TA; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
         }
@@ -281,12 +283,12 @@ struct ObjEpilogue : ObjTile {
       // y of the label straight from the accumulator that holds it
       const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
       const int y = s_local < rows ? y_u[u] : -1;
-      const int rel = y - (v0 + wa * 128);
-      if (rel >= 0 && rel < 128 && y < V && (rel >> 5) == g) {
-        const int t_sel = (rel & 31) >> 2, r_sel = rel & 3;
+      const int rel = y - va;
+      if ((unsigned)rel < (unsigned)kPer && y < V) {
+        const int t_sel = rel >> 2, r_sel = rel & 3;
         float val = 0.f;
 #pragma unroll
-        for (int t = 0; t < kTA16; ++t)
+        for (int t = 0; t < TA; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             if (t == t_sel && r == r_sel) val = acc[t][u][r];
@@ -315,128 +317,12 @@ struct ObjEpilogue : ObjTile {
   }
 };
 
-// ---------------------------------------------------------------------------
-// forward of a few rows: W is read once, which is all that takes time.  A workgroup owns kFewV vocabulary entries, a wave 16 of
-// them and up to 16 TB rows; both operands come from memory straight into registers as MFMA fragments.  The contraction's
-// order is free, so a lane quarter g takes the 16 consecutive k = 16 g .. 16 g + 15 of every 64: 32 contiguous bytes a lane, a
-// whole line of each of the 16 rows for the wave.  kDepth such steps are loaded while the kDepth before them are multiplied.
-// ---------------------------------------------------------------------------
-constexpr int kFewWaves = 8, kFewV = 16 * kFewWaves, kFewDepth = 4;
-template <int TB>
-__global__ __launch_bounds__(64 * kFewWaves) void k_obj_few(const __bf16* __restrict__ H, const __bf16* __restrict__ W, int rows, int d, int V,
-                                                            ObjTile e) {
-  __shared__ float xch[kFewWaves][16 * TB][3];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-  const int vt = blockIdx.x, v0 = vt * kFewV + 16 * wave;
-  const int v_in = v0 + c < V ? v0 + c : V - 1;
-  const __bf16* const a_row = W + (size_t)v_in * d + 16 * g;
-  const __bf16* b_row[TB];
-#pragma unroll
-  for (int u = 0; u < TB; ++u) b_row[u] = H + (size_t)(16 * u + c < rows ? 16 * u + c : rows - 1) * d + 16 * g;
-  f32x4 acc[TB];
-#pragma unroll
-  for (int u = 0; u < TB; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-  struct Step { bf16x8 a[2], b[TB][2]; };
-  auto load = [&](Step& x, int k) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      x.a[h] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(a_row + k + 8 * h));
-#pragma unroll
-      for (int u = 0; u < TB; ++u) x.b[u][h] = *reinterpret_cast<const bf16x8*>(b_row[u] + k + 8 * h);
-    }
-  };
-  auto multiply = [&](const Step& x) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int u = 0; u < TB; ++u) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.a[h], x.b[u][h], acc[u], 0, 0, 0);
-  };
-  const int n_block = d / (64 * kFewDepth);
-  if (n_block) {
-    Step now[kFewDepth], next[kFewDepth];
-#pragma unroll
-    for (int i = 0; i < kFewDepth; ++i) load(now[i], 64 * i);
-    for (int b = 1; b < n_block; ++b) {
-#pragma unroll
-      for (int i = 0; i < kFewDepth; ++i) load(next[i], 64 * (b * kFewDepth + i));
-#pragma unroll
-      for (int i = 0; i < kFewDepth; ++i) multiply(now[i]);
-#pragma unroll
-      for (int i = 0; i < kFewDepth; ++i) now[i] = next[i];
-    }
-#pragma unroll
-    for (int i = 0; i < kFewDepth; ++i) multiply(now[i]);
-  }
-  for (int k = n_block * 64 * kFewDepth; k < d; k += 64) {             // the rest, eight k at a time inside or outside
-    Step x;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = k + 16 * g + 8 * h < d;
-      const bf16x8 zero = {};
-      x.a[h] = in ? *reinterpret_cast<const bf16x8*>(a_row + k + 8 * h) : zero;
-#pragma unroll
-      for (int u = 0; u < TB; ++u) x.b[u][h] = in ? *reinterpret_cast<const bf16x8*>(b_row[u] + k + 8 * h) : zero;
-    }
-    multiply(x);
-  }
-
-  typedef TileEntries<16 * TB, kFewV, 64 * kFewWaves> Found;
-  __shared__ __attribute__((aligned(16))) char found_sh[Found::kBytes];
-  const Found found = e.K ? Found(found_sh, e, 0, rows, vt * kFewV, V, vt == 0) : Found();
-
-  // as ObjEpilogue: a lane has, of row 16 u + c, the four entries from va on
-  const int va = v0 + 4 * g;
-  const bool two = e.part_label != nullptr;
-#pragma unroll
-  for (int u = 0; u < TB; ++u) {
-    const int s = 16 * u + c;
-    const bool in = s < rows;
-    const int s_in = in ? s : rows - 1;
-    float y[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = e.cap > 0.f ? capped(acc[u][r], e.cap, 2.f * kLog2e / e.cap) : acc[u][r];
-    if (e.labels_c && in) {
-      const int at = e.labels_c[s] - va;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (at == r && va + r < V) e.tgt[s] = y[r];
-    }
-    if (e.K) {
-      const unsigned mine = found.bits[s * Found::kWords + (va - vt * kFewV) / 32] >> ((va - vt * kFewV) & 31);
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if ((mine >> r) & 1u) {
-          e.entry_y[(size_t)s * e.K + found.place[s * kFewV + va - vt * kFewV + r]] = y[r];
-          y[r] = kMasked;
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (va + r >= V) y[r] = kMasked;
-    float m = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), l = 0.f, k = 0.f;
-    m = fmaxf(m, kMasked);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      l += fast_exp2((y[r] - m) * e.exponent);
-      if (two) k += fast_exp2((y[r] - m) * e.exponent_label);
-    }
-#pragma unroll
-    for (int o = 16; o <= 32; o <<= 1)
-      merge_sums(m, l, k, __shfl_xor(m, o), __shfl_xor(l, o), two ? __shfl_xor(k, o) : 0.f, e.exponent, e.exponent_label, two);
-    if (lane < 16) {
-      float* const at = xch[wave][16 * u + lane];
-      at[0] = m; at[1] = l; at[2] = k;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x >= 16 * TB || (int)threadIdx.x >= rows) return;
-  const int s = threadIdx.x;
-  float m = kMasked, l = 0.f, k = 0.f;
-#pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) merge_sums(m, l, k, xch[w][s][0], xch[w][s][1], xch[w][s][2], e.exponent, e.exponent_label, two);
-  e.part[(size_t)vt * e.part_stride + s] = make_float2(m, l);
-  if (two) e.part_label[(size_t)vt * e.part_stride + s] = k;
-}
+// Calls of up to 32 rows that have tiles of 256 vocabulary entries for half of the compute units or fewer: W is read once, which is
+// all that takes time, and a compute unit alone does not get its share of the memory's bandwidth.  Tiles of 64, two workgroups on a
+// compute unit where there are as many.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight stages) and these: d = 4096,
+// V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048, V = 4000 19.6, 15.8, 13.4.
+// (With both operands from memory straight into registers, a wave to 16 vocabulary entries: 57.8 for one row, 71.4 for 16.)
+typedef CfgSmall<2, 1, 6, 6, true> TileFew;
 
 // ---------------------------------------------------------------------------
 // The teacher's entries of a group of rows in ascending order.  A wave sorts a row, P entries a lane, with a bitonic network on

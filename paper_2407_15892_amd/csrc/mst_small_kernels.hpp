@@ -35,16 +35,16 @@ inline double small_launch_us(double tiles, double ksteps) {
 // ---------------------------------------------------------------------------
 // forward: 256 vocabulary entries x 32 TB rows per workgroup.  The vocabulary side stays 256 wide because the workspace
 // holds one (max, sum-exp) pair per row and 256 entries; every pair is formed in the same order as by k_fwd_gemm_lse, so
-// lse and loss keep their bits.
+// lse and loss keep their bits (E::kWhole; other objectives have narrower tiles too).
 // ---------------------------------------------------------------------------
 template <class C, class E>
 __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_lse_small(
     const __bf16* __restrict__ Hc, const __bf16* __restrict__ W, int rows, int d, int V, int n_st, int n_vt, E epilogue) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  static_assert(C::EA == kTile && C::TA == kTA16, "one pair per row and 256 vocabulary entries");
+  static_assert(!E::kWhole || (C::EA == kTile && C::TA == kTA16), "one pair per row and 256 vocabulary entries");
   int vt, st;
   if (!even_tile_of_block(blockIdx.x, n_vt, n_st, &vt, &st)) return;
-  const int v0 = vt * kTile, s0 = st * C::EB;
+  const int v0 = vt * C::EA, s0 = st * C::EB;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave / C::WB, wb = wave % C::WB;
