@@ -419,12 +419,15 @@ __device__ __forceinline__ void lse_epilogue(f32x4 (&acc)[kTA16][TB], const int*
 struct LseEpilogue {
   typedef LseEpilogue Small;           // that of the smaller tiles
   static constexpr bool kWhole = true; // tiles are 256 vocabulary entries wide
+  struct Early {};                     // what is loaded before a small tile's main loop
+  template <class C> __device__ __forceinline__ Early early(int, int) const { return {}; }
   const int* labels_c;
   float2* part;
   size_t part_stride;
   float* tgt;
   template <class C>                   // the tile
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[kTA16][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem,
+                                             Early = {}) const {
     lse_epilogue<C::TB>(acc, labels_c, rows, V, vt, s0, part, part_stride, tgt, wa, wb, lane, smem);
   }
 };

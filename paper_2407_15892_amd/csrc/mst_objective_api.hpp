@@ -12,8 +12,8 @@ struct ObjPlan {
   int K;
   bool few;              // the forward's tiles are TileFew, not the plain forward's
   int n_vt;              // vocabulary tiles of the forward
-  // forward workspace: the plain forward's (its nll: the rows' losses), then
-  size_t f_part_few, f_count, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
+  // forward workspace: the plain forward's, then
+  size_t f_part_few, f_row_loss, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
   size_t s_rows, s_rows2, s_index, s_at, s_total;      // of `saved`
 };
 
@@ -64,7 +64,7 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   size_t off = o->p.f_total;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
   o->f_part_few = o->few ? take((size_t)o->n_vt * rows * 8) : 0;
-  o->f_count = take((size_t)S * 4);
+  o->f_row_loss = take((size_t)S * 8);
   o->f_part_label = K ? take((size_t)o->n_vt * rows * 4) : 0;
   o->f_starts = K && !o->few ? take((size_t)(o->n_vt + 1) * rows * 2) : 0;
   o->f_index = K ? take(rows * k * 4) : 0;
@@ -161,24 +161,21 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   float* const logit = reinterpret_cast<float*>(ws + o.f_logit);
   int* const info = reinterpret_cast<int*>(ws + o.f_info);
   unsigned short* const starts = reinterpret_cast<unsigned short*>(ws + o.f_starts);
-  const bool sorted = o.K && !o.few && forward_tile_rows(p) == kTile;
+  const bool sorted = o.K && !o.few && forward_tile_rows(p) > 32;
   if (o.K) {
     e.starts = sorted ? starts : nullptr;
     e.index = index;
     e.entry_y = reinterpret_cast<float*>(ws + o.f_entry_y);
-    e.logit_bf16 = c.logits_bf16;
-    e.logit = logit;
     e.info = info;
   }
   ObjFinal f = {};
   f.part = e.part; f.part_label = e.part_label; f.part_stride = stride;
   f.n_vt = o.n_vt; f.V = (int)p.V; f.K = o.K;
   f.tgt = e.tgt; f.ignore_index = c.ignore_index;
-  f.index = index; f.logit = logit; f.entry_y = e.entry_y; f.info = info;
-  f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t = (float)(1.0 / (double)c.temperature);
+  f.index = index; f.logit = sorted ? logit : nullptr; f.logit_bf16 = c.logits_bf16; f.entry_y = e.entry_y; f.info = info;
+  f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t_64 = 1.0 / (double)c.temperature; f.inv_t = (float)f.inv_t_64;
   f.label_coef = c.label_coef; f.teacher_coef = c.teacher_coef; f.z_coef = c.z_coef; f.temperature = c.temperature;
-  float* const row_loss = reinterpret_cast<float*>(ws + p.f_nll);
-  int* const count = reinterpret_cast<int*>(ws + o.f_count);
+  float2* const row_loss = reinterpret_cast<float2*>(ws + o.f_row_loss);
 
   ObjLoss l = {};
   l.divisor = c.divisor;
@@ -195,7 +192,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   auto tile_of = [&](int64_t g0) {
     ObjTile of = e;
     of.labels_c = c.labels ? c.labels + g0 : nullptr;
-    if (o.K) of.index_in_c = c.index + (size_t)g0 * k, of.logit_in_c = logits_from(g0);
+    if (o.K) of.index_in_c = c.index + (size_t)g0 * k;
     return of;
   };
   auto before = [&](int64_t g0, int g_rows) {
@@ -208,6 +205,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   auto after = [&](int64_t g0, int g_rows) {
     ObjFinal of = f;
     of.rows = g_rows;
+    if (o.K) of.logit_in_c = logits_from(g0);
     of.labels_c = c.labels ? c.labels + g0 : nullptr;
     of.weights_c = c.weights ? c.weights + g0 : nullptr;
     of.teacher_lse_c = c.teacher_lse ? c.teacher_lse + g0 : nullptr;
@@ -215,7 +213,6 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
     of.kd_c = c.kd ? c.kd + g0 : nullptr;
     of.lse_c = c.lse ? c.lse + g0 : nullptr;
     of.row_loss_c = row_loss + g0;
-    of.count_c = count + g0;
     if (saved) {
       of.rows_c = reinterpret_cast<ObjRow*>(saved + o.s_rows) + g0;
       if (o.K) {
@@ -250,7 +247,7 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   }
   if (!one) {
     Scope sc(st, MST_K_LOSS_REDUCE);
-    hipLaunchKernelGGL(k_obj_loss, dim3(1), dim3(1024), 0, st, row_loss, count, (long long)p.S, l);
+    hipLaunchKernelGGL(k_obj_loss, dim3(1), dim3(1024), 0, st, row_loss, (long long)p.S, l);
   }
   return check_launch();
 }

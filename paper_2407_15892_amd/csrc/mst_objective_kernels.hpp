@@ -68,73 +68,85 @@ struct ObjTile {
   int* index;                          // [rows][K] the entries, kNoEntry where there is none
   float* entry_y;                      // [rows][K] their y
   const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile, with `index` ascending; null where the tile
-                                       // finds its entries among the caller's and writes `index`, `logit` and `info` (TileEntries)
+                                       // finds its entries among the caller's and writes `index` and `info` (TileEntries)
   const int* index_in_c;
-  const void* logit_in_c;
-  int logit_bf16;
-  float* logit;
   int* info;
   float cap, exponent, exponent_label;
   int power;                           // T where it is 2 or 4: the second exponential is a power of the first; else 0
 };
 
-// A tile's entries without a launch before it, for tiles that are all in one round of workgroups: its threads look through the
-// entries of its rows and note in LDS which of the tile's kWidth vocabulary entries are the teacher's (a bit each) and at which place
-// of the row's list (the first, where an index comes twice).  The tile that has an entry writes what the following kernel reads of
-// it, the first tile also what is no entry.  512 x 256 x 4096 with 20 entries: 8.6 us of a launch of sorting, 1 us here.
+// f(row, place in its list, index) for all entries of a tile's rows, [rows][K] from `index` on.  A thread's first ones can be loaded
+// long before (first_entries).
+constexpr int kEntriesAtOnce = 8;
+struct FirstEntries { int v[kEntriesAtOnce]; };
+template <int kThreadsOfTile>
+__device__ __forceinline__ FirstEntries load_entries(const int* __restrict__ index, int n, int i0) {
+  FirstEntries e;
+#pragma unroll
+  for (int b = 0; b < kEntriesAtOnce; ++b) e.v[b] = index[i0 + b * kThreadsOfTile < n ? i0 + b * kThreadsOfTile : n - 1];
+  return e;
+}
 template <int kThreadsOfTile, class F>
-__device__ __forceinline__ void each_entry(const int* __restrict__ index, int rows, int K, F f) {     // f(row, place in its list, index)
-  constexpr int kAtOnce = 8;
+__device__ __forceinline__ void each_entry(const FirstEntries& first, const int* __restrict__ index, int rows, int K, F f) {
   const int n = rows * K;
   const float by_k = 1.f / (float)K;
-  for (int i0 = threadIdx.x; i0 < n; i0 += kAtOnce * kThreadsOfTile) {
-    int v[kAtOnce];
+  FirstEntries e = first;
+  for (int i0 = threadIdx.x; i0 < n;) {
 #pragma unroll
-    for (int b = 0; b < kAtOnce; ++b) v[b] = index[i0 + b * kThreadsOfTile < n ? i0 + b * kThreadsOfTile : n - 1];
-#pragma unroll
-    for (int b = 0; b < kAtOnce; ++b) {
+    for (int b = 0; b < kEntriesAtOnce; ++b) {
       const int i = i0 + b * kThreadsOfTile;
       const int r = (int)(((float)i + 0.5f) * by_k);       // i / K: i < 2^15, K <= 2^8, half of 1 / K is more than the product is off by
-      if (i < n) f(r, i - r * K, v[b]);
+      if (i < n) f(r, i - r * K, e.v[b]);
     }
+    i0 += kEntriesAtOnce * kThreadsOfTile;
+    if (i0 < n) e = load_entries<kThreadsOfTile>(index, n, i0);
   }
 }
+
+// A tile's entries without a launch before it, for tiles of up to 32 rows, which are all in one round of workgroups: its threads look
+// through the entries of its rows and note in LDS which of the tile's kWidth vocabulary entries are the teacher's (a bit each) and at
+// which place of the row's list (the first, where an index comes twice).  The tile that has an entry writes what the following kernel
+// reads of it, the first tile also what is no entry.  512 x 256 x 4096 with 20 entries: 8.6 us of a launch of sorting, 3 us here.
 template <int kRows, int kWidth, int kThreadsOfTile>
 struct TileEntries {
   static constexpr int kWords = kWidth / 32;
-  static constexpr int kBytes = kRows * (kWords + kWidth) * 4;
+  static constexpr int kBytes = kRows * (kWords + 2 * kWidth) * 4;
   static_assert(kRows * kMaxEntries <= 1 << 15 && kBytes % 16 == 0, "each_entry");
   unsigned* bits;                      // [kRows][kWords]
   int* place;                          // [kRows][kWidth], where there is a bit
-  TileEntries() = default;
+  float* y;                            // [kRows][kWidth]: for the tile's y where there is a bit
   // smem: kBytes, 16-byte aligned, that nobody uses; all threads of the workgroup
-  __device__ __forceinline__ TileEntries(char* smem, const ObjTile& e, int s0, int rows, int v0, int V, bool first_tile) {
-    bits = reinterpret_cast<unsigned*>(smem);
-    place = reinterpret_cast<int*>(bits + kRows * kWords);
+  __device__ __forceinline__ TileEntries(char* smem, const ObjTile& e, const FirstEntries& first, int s0, int rows, int v0, int V, bool first_tile)
+      : bits(reinterpret_cast<unsigned*>(smem)), place(reinterpret_cast<int*>(bits + kRows * kWords)),
+        y(reinterpret_cast<float*>(place + kRows * kWidth)) {
     for (int i = threadIdx.x; i < kRows * kWords; i += kThreadsOfTile) bits[i] = 0;
     for (int i = threadIdx.x; i < kRows * kWidth / 4; i += kThreadsOfTile) reinterpret_cast<int4*>(place)[i] = make_int4(kNoEntry, kNoEntry, kNoEntry, kNoEntry);
     const int here = rows - s0 < kRows ? rows - s0 : kRows;
-    const size_t from = (size_t)s0 * e.K;
-    const int* const index_in = e.index_in_c + from;
-    auto in_tile = [&](int v) { return (unsigned)(v - v0) < (unsigned)kWidth && v < V; };
     if (first_tile)
       for (int r = threadIdx.x; r < here; r += kThreadsOfTile) e.info[s0 + r] = e.K;
     __syncthreads();
-    each_entry<kThreadsOfTile>(index_in, here, e.K, [&](int r, int k, int v) {
-      if (!in_tile(v)) return;
+    each_entry<kThreadsOfTile>(first, e.index_in_c + (size_t)s0 * e.K, here, e.K, [&](int r, int k, int v) {
+      if ((unsigned)(v - v0) >= (unsigned)kWidth || v >= V) return;
       atomicMin(place + r * kWidth + v - v0, k);
       atomicOr(bits + r * kWords + (v - v0) / 32, 1u << ((v - v0) & 31));
     });
     __syncthreads();
-    each_entry<kThreadsOfTile>(index_in, here, e.K, [&](int r, int k, int v) {
+  }
+  // behind the tile's y in LDS
+  __device__ __forceinline__ void write(const ObjTile& e, const FirstEntries& first, int s0, int rows, int v0, int V, bool first_tile) const {
+    __syncthreads();
+    const int here = rows - s0 < kRows ? rows - s0 : kRows;
+    const size_t from = (size_t)s0 * e.K;
+    each_entry<kThreadsOfTile>(first, e.index_in_c + from, here, e.K, [&](int r, int k, int v) {
       const size_t at = from + (size_t)r * e.K + k;
-      if (in_tile(v)) {
-        const bool kept = place[r * kWidth + v - v0] == k;
+      if ((unsigned)(v - v0) < (unsigned)kWidth && v < V) {
+        const int in = r * kWidth + v - v0;
+        const bool kept = place[in] == k;
         e.index[at] = kept ? v : kNoEntry;
-        if (kept) e.logit[at] = e.logit_bf16 ? (float)static_cast<const __bf16*>(e.logit_in_c)[at] : static_cast<const float*>(e.logit_in_c)[at];
+        if (kept) e.entry_y[at] = y[in];
       } else if (first_tile && (unsigned)v >= (unsigned)V) {
         e.index[at] = kNoEntry;
-        if (v >= V) e.info[s0 + r] = -1;             // behind e.K, with a barrier in between
+        if (v >= V) e.info[s0 + r] = -1;             // behind e.K, with barriers in between
       }
     });
   }
@@ -150,10 +162,21 @@ struct ObjEpilogue : ObjTile {
   ObjEpilogue() = default;
   explicit ObjEpilogue(const ObjTile& t) : ObjTile(t) {}
 
+  // what is on its way during a small tile's main loop
+  template <class C> static constexpr bool has_early() { return C::EB <= 32; }
+  typedef FirstEntries Early;
   template <class C>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[C::TA][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem) const {
+  __device__ __forceinline__ Early early(int rows, int s0) const {
+    if constexpr (has_early<C>())
+      if (K) return load_entries<C::kThreads>(index_in_c + (size_t)s0 * K, (rows - s0 < C::EB ? rows - s0 : C::EB) * K, threadIdx.x);
+    return Early();
+  }
+
+  template <class C>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[C::TA][C::TB], int rows, int V, int vt, int s0, int wa, int wb, int lane, char* smem,
+                                             const Early& first_entries = Early()) const {
     constexpr int TA = C::TA, TB = C::TB, kPer = 4 * TA, kWaveV = 16 * TA;    // vocabulary entries of a lane, of a wave
-    constexpr bool kSorted = C::EB == kTile;           // entries from k_entries
+    constexpr bool kSorted = !has_early<C>();          // entries from k_entries
     typedef TileEntries<C::EB, C::EA, C::kThreads> Found;
     const bool teacher = kWhat == kObjAny && K > 0, two = kWhat == kObjAny && part_label != nullptr;
     const int v0 = vt * C::EA;
@@ -177,10 +200,8 @@ struct ObjEpilogue : ObjTile {
           for (int r = 0; r < 4; ++r) acc[t][u][r] = capped(acc[t][u][r], cap, scale);
     }
     float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
-    // The entries' y out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's;
-    // place_of(i): its place in the row's list.
-    auto take = [&](int u, unsigned mine, auto place_of) {
-      const int s_local = s0 + wb * (16 * TB) + 16 * u + c;
+    // The entries' y out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's.
+    auto take = [&](int u, unsigned mine, auto put) {
       if (!__any(mine != 0)) return;
 #pragma unroll
       for (int t = 0; t < TA; ++t) {
@@ -188,7 +209,7 @@ struct ObjEpilogue : ObjTile {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if ((mine >> (4 * t + r)) & 1u) {
-            entry_y[(size_t)s_local * K + place_of(4 * t + r)] = acc[t][u][r];
+            put(4 * t + r, acc[t][u][r]);
             acc[t][u][r] = kMasked;
           }
       }
@@ -220,20 +241,28 @@ struct ObjEpilogue : ObjTile {
           };
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i) note(from[u] + i, entry[u][i]);
-          for (int e = from[u] + kAtOnce; e < to[u]; ++e) note(e, index[(size_t)s_local * K + e]);
-          take(u, mine, [&](int i) { return first + __builtin_popcount(mine & ((1u << i) - 1u)); });
+          for (int e0 = from[u] + kAtOnce; e0 < to[u]; e0 += kAtOnce) {
+            int more[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) more[i] = index[(size_t)s_local * K + (e0 + i < K ? e0 + i : K - 1)];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) note(e0 + i, more[i]);
+          }
+          float* out = entry_y + (size_t)(s_local < rows ? s_local : rows - 1) * K + first;      // a lane's entries follow each other
+          take(u, mine, [&](int, float y) { *out++ = y; });
         }
       } else {
         static_assert(Found::kBytes + 2 * C::EB * 12 <= C::kLds, "beside the triples");
-        const Found found(smem, *this, s0, rows, v0, V, vt == 0);
+        const Found found(smem, *this, first_entries, s0, rows, v0, V, vt == 0);
         xch = reinterpret_cast<float*>(smem + Found::kBytes);
 #pragma unroll
         for (int u = 0; u < TB; ++u) {
           const int r = wb * (16 * TB) + 16 * u + c;   // past the last row: no bits
-          const int* const at = found.place + r * C::EA + va - v0;
+          float* const out = found.y + r * C::EA + va - v0;
           const unsigned word = found.bits[r * Found::kWords + (va - v0) / 32];
-          take(u, (word >> ((va - v0) & 31)) & (0xffffffffu >> (32 - kPer)), [&](int i) { return at[i]; });
+          take(u, (word >> ((va - v0) & 31)) & (0xffffffffu >> (32 - kPer)), [&](int i, float y) { out[i] = y; });
         }
+        found.write(*this, first_entries, s0, rows, v0, V, vt == 0);
       }
     }
     if (v0 + C::EA > V) {
@@ -434,15 +463,17 @@ struct ObjFinal {
   const float* weights_c;
   int ignore_index;
   const int* index;                   // [rows][K] (kNoEntry: none), and the entries' logits and y
-  const float* logit;
+  const float* logit;                 // null: the caller's, in the order of its list
+  const void* logit_in_c;
+  int logit_bf16;
   const float* entry_y;
   const int* info;
   const float* teacher_lse_c;
   float cap, exponent, exponent_label, inv_t;
+  double inv_t_64;
   float label_coef, teacher_coef, z_coef, temperature;
   float *nll_c, *kd_c, *lse_c;        // outputs, each may be null
-  float* row_loss_c;
-  int* count_c;                       // 1: the row counts, -1: an index out of range
+  float2* row_loss_c;                 // the row's loss, and as an integer's bits 1: it counts, -1: an index out of range
   ObjRow* rows_c;                     // null: no backward follows
   ObjRow2* rows2_c;
   int* saved_index_c;
@@ -499,7 +530,8 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     const int e = lane + 16 * i, e_in = e < a.K ? e : a.K - 1;
     const int v = a.index[at0 + e_in];
     y_p[i] = a.entry_y[at0 + e_in];
-    t_p[i] = a.logit[at0 + e_in];
+    t_p[i] = a.logit ? a.logit[at0 + e_in] : a.logit_bf16 ? (float)static_cast<const __bf16*>(a.logit_in_c)[at0 + e_in]
+                                                          : static_cast<const float*>(a.logit_in_c)[at0 + e_in];
     v_p[i] = e < a.K ? v : kNoEntry;
   }
   const int y = a.labels_c ? a.labels_c[s_in] : a.ignore_index;
@@ -603,8 +635,9 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   double sum_q = 0.0;
   float kd = 0.f;
   entries([&](int i) {
-    // relative to the largest logits, so that equal distributions leave nothing
-    const float log_q = given ? t_p[i] * a.inv_t - lse_teacher : (t_p[i] - mt) * a.inv_t - logf(lt);
+    // relative to the largest logits, so that equal distributions leave nothing; to a log-sum-exp in 64 bits: half a step of a logit
+    // of 16 would be 1e-6 of a share, and all of them of the rest
+    const float log_q = given ? (float)((double)t_p[i] * a.inv_t_64 - (double)lse_teacher) : (t_p[i] - mt) * a.inv_t - logf(lt);
     const float log_p = (y_p[i] - m_all) * a.inv_t - log_all;
     const float q = expf(log_q);
     sum_q += (double)q;
@@ -636,8 +669,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
       sh_loss[r] = loss;
       sh_count[r] = count;
     } else {
-      a.row_loss_c[s] = loss;
-      a.count_c[s] = count;
+      a.row_loss_c[s] = make_float2(loss, __builtin_bit_cast(float, count));
     }
   }
   if constexpr (kAll) {
@@ -685,7 +717,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     float x = 0.f;
     if (v != kNoEntry) {
       const float ye = y_p[i];
-      const float log_q = given ? t_p[i] * a.inv_t - lse_teacher : (t_p[i] - mt) * a.inv_t - logf(lt);
+      const float log_q = given ? (float)((double)t_p[i] * a.inv_t_64 - (double)lse_teacher) : (t_p[i] - mt) * a.inv_t - logf(lt);
       if (on_kd != 0.f) x = on_kd * (expf((ye - m_all) * a.inv_t - log_all) * (total_q + rest) - expf(log_q));
       if (on_p != 0.f) x += on_p * expf((ye - m_all) - log_label);
       if (valid && v == y) x -= on_label;
@@ -717,25 +749,22 @@ __device__ __forceinline__ void reduce_obj_loss(const ObjLoss& o, double a, long
   for (int i = 0; i < 16; ++i) { a += sh[i]; n += sh_n[i]; bad |= sh_bad[i]; }
   write_loss(o, a, n, bad);
 }
-// One workgroup, bound by the latency of its loads: eight rounds of them at a time.
-__global__ __launch_bounds__(1024) void k_obj_loss(const float* __restrict__ row_loss, const int* __restrict__ count, long long S, ObjLoss o) {
+// One workgroup, bound by the latency of its loads: sixteen rounds of them at a time.
+__global__ __launch_bounds__(1024) void k_obj_loss(const float2* __restrict__ row_loss, long long S, ObjLoss o) {
   double a = 0.0;
   long long n = 0;
   int bad = 0;
-  for (long long i0 = threadIdx.x; i0 < S; i0 += 8 * 1024) {
-    float x[8];
-    int c[8];
+  constexpr int kAtOnce = 16;
+  for (long long i0 = threadIdx.x; i0 < S; i0 += kAtOnce * 1024) {
+    float2 x[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const long long i = i0 + k * 1024;
-      x[k] = i < S ? row_loss[i] : 0.f;
-      c[k] = i < S ? count[i] : 0;
-    }
+    for (int k = 0; k < kAtOnce; ++k) x[k] = i0 + k * 1024 < S ? row_loss[i0 + k * 1024] : make_float2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      a += (double)x[k];
-      n += c[k] > 0;
-      bad |= c[k] < 0;
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int count = __builtin_bit_cast(int, x[k].y);
+      a += (double)x[k].x;
+      n += count > 0;
+      bad |= count < 0;
     }
   }
   reduce_obj_loss(o, a, n, bad);
@@ -792,7 +821,7 @@ struct ObjGrad {
     if (!K) return;
     __syncthreads();
     const size_t from = (size_t)s0 * K;
-    each_entry<kThreadsOfTile>(index + from, n_rows, K, [&](int r, int k, int v) {
+    each_entry<kThreadsOfTile>(load_entries<kThreadsOfTile>(index + from, n_rows * K, threadIdx.x), index + from, n_rows, K, [&](int r, int k, int v) {
       if ((unsigned)(v - v0) < (unsigned)width && v < V)
         *reinterpret_cast<__bf16*>(staged + r * row_bytes + 2 * (v - v0)) = (__bf16)at[from + (size_t)r * K + k];
     });

@@ -49,6 +49,7 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_ls
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave / C::WB, wb = wave % C::WB;
 
+  const typename E::Early early = epilogue.template early<C>(rows, s0);
   f32x4 acc[C::TA][C::TB];
   zero_acc<C::TA, C::TB>(acc);
   {
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_fwd_gemm_ls
     pb.init(Hc + (size_t)s0 * d, d, rows - s0, d, wave, lane, wb);
     gemm_mainloop_small<C>(acc, pa, pb, smem, 0, d);
   }
-  epilogue.template operator()<C>(acc, rows, V, vt, s0, wa, wb, lane, smem);
+  epilogue.template operator()<C>(acc, rows, V, vt, s0, wa, wb, lane, smem, early);
 }
 
 // ---------------------------------------------------------------------------

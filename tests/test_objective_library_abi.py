@@ -31,7 +31,7 @@ def test_bytes(lib):
     import paper_2407_15892_amd as mst
     plain = mst.mst_workspace_bytes(8192, 4096, 128256, 8)
     fwd, bwd, saved = mst.mst_objective_bytes(8192, 4096, 128256, 8)
-    assert bwd == plain[1] and plain[0] < fwd <= plain[0] + 4 * 8192 + 512 and saved <= 16 * 8192 + 512
+    assert bwd == plain[1] and plain[0] < fwd <= plain[0] + 8 * 8192 + 512 and saved <= 16 * 8192 + 512
     fwd, bwd, saved = mst.mst_objective_bytes(8192, 4096, 128256, 8, 64)
     assert bwd == plain[1] and fwd < bwd and saved <= (24 + 8 * 64) * 8192 + 2048
     # M is the largest number of mini-sequences: fewer where one of them is less than 512 MiB of fp32 logits
