@@ -145,6 +145,10 @@ def bounds(p: Problem, r: dict, grad_loss=1.0):
     b["loss"] = np.sum(b["row_loss"] * np.ones(p.S)) * abs(r["gamma"] / grad_loss) + 4 * HALF_FP32 * abs(r["loss"])
     # the logits' gradient: its terms off by their shares' error (the rest's share of the others by the rest's own as well), then rounded
     share = 4 * arg + 8 * HALF_FP32
+    # the cap's slope 1 / cosh^2(z / cap), whose logarithm changes by at most 2 / cap for each unit of z: the logit's error, and the
+    # roundings of its exponential's argument 2 z / cap and of 2 z / cap in base 2
+    if cap:
+        share += 2 / cap * dz + 8 * HALF_FP32 * (2 * largest / cap + 1)
     if p.K and p.lse is not None:
         share += 8 * arg
     dG = HALF_BF16 * np.abs(r["G"]) + share * r["G_abs"]

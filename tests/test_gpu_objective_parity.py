@@ -68,7 +68,7 @@ def test_orders_of_the_backward_pass(schedule, o):
     print(check(p, run.outputs(), p.oracle()))
 
 
-@pytest.mark.parametrize("rows", [20, 100, 400, 1500])
+@pytest.mark.parametrize("rows", [20, 100, 200, 400, 1500])
 def test_tiles_of_the_forward_pass(rows):
     """Every height of the forward's tiles, with entries at the borders of tiles and lanes."""
     import paper_2407_15892_amd as mst
@@ -96,16 +96,18 @@ def test_a_few_rows(S, d):
         print(check(p, run.outputs(), p.oracle()))
 
 
+@pytest.mark.parametrize("S,d,V,mini_sequences", [(2300, 64, 150000, 3), (4196, 4096, 40960, 2)])
 @pytest.mark.parametrize("o", [dict(K=30, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=20.0, weights=True, z_coef=1e-3)])
-def test_several_mini_sequences(o):
-    """2300 x 150000 logits are 1.3 GB in float32, three mini-sequences: every row's outputs and gradient are those of a call of its
-    own rows (one mini-sequence), and the weights' gradient is the sum of these calls'."""
+def test_several_mini_sequences(S, d, V, mini_sequences, o):
+    """More than 512 MiB of float32 logits: every row's outputs and gradient are those of a call of its own rows (one mini-sequence),
+    and the weights' gradient is the sum of these calls'.  The forward of the second shape deals its tiles out of queues, the calls of
+    its parts do not."""
     import torch
     import paper_2407_15892_amd as mst
-    S, d, V = 2300, 64, 150000
+    assert (mst.mst_forward_launch(S, d, V, mini_sequences) == "queues") == (d == 4096)
     g = torch.Generator(device="cuda").manual_seed(5)
     H = torch.randn((S, d), generator=g, device="cuda").bfloat16()
-    W = (torch.randn((V, d), generator=g, device="cuda") / 4).bfloat16()
+    W = (torch.randn((V, d), generator=g, device="cuda") * 2 / d ** 0.5).bfloat16()
     labels = torch.randint(0, V, (S,), generator=g, device="cuda", dtype=torch.int32)
     labels[::7] = -100
     weights = torch.rand(S, generator=g, device="cuda") if o.get("weights") else None
@@ -133,7 +135,7 @@ def test_several_mini_sequences(o):
             mst.mst_lmhead_wce_bwd(H[rows], W, M, 1.0, saved, ws, dH, dW)
         return loss.double().item(), int(cnt), nll, other, dH, dW
 
-    assert mst.mst_objective_bytes(S, d, V, 5, K)[1] == -(-S // 3) * V * 4
+    assert mst.mst_objective_bytes(S, d, V, 5, K)[1] == -(-S // mini_sequences) * V * 4
     whole = call(slice(0, S), 5)
     parts = [call(slice(a, b), 1) for a, b in ((0, 300), (300, 1000), (1000, 1500), (1500, S))]
     assert whole[1] == sum(p[1] for p in parts)
