@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2407_15892_amd as mst
-from tests.objective_gpu_harness import HALF_BF16, Problem, Run, check
+from tests.objective_gpu_harness import HALF_BF16, HALF_FP32, Problem, Run, check
 
 pytestmark = pytest.mark.gpu
 
@@ -87,6 +87,30 @@ def test_confident_student():
     r, got = run_and_check(p)
     ref = p.oracle()
     assert ref["kd"].min() > 5 and np.abs(got["rows"] / ref["kd"] - 1).max() < 1e-5
+
+
+@pytest.mark.parametrize("S,d,V,K", [(1, 384, 20000, 6), (30, 80, 3000, 9), (400, 128, 14144, 9), (2000, 64, 12800, 100)])
+@pytest.mark.parametrize("tail", [False, True])
+def test_softened_distributions_that_are_nearly_the_same(S, d, V, K, tail):
+    """A divergence of shares that add up to 1 is off by (p - q) times what the logarithms of shares are off by, added up: no more than
+    the largest of these times sum |p - q|, which is at most sqrt(2 kd)."""
+    p = Problem(S, d, V, K=K, tail=tail, labels=False, temperature=4.0, sigma=1.5, short=0, empty=0)
+    if not tail:                                                     # entries that are nearly all of the student's distribution
+        p.W[:K, 0] = np.abs(p.W[:K, 0]) + 8.0
+        p.H[:, 0] = 16.0
+        p.index[:] = np.arange(K)
+        p.logits = np.float32(p.H @ p.W[:K].T + 0.1 * np.random.default_rng(3).standard_normal((S, K))).astype(np.float64)
+    run = Run(p)
+    run.forward()
+    run.backward()
+    got, ref = run.outputs(), p.oracle()
+    largest = max(np.abs(ref["Z"]).max(), np.abs(p.logits).max(), 1.0)
+    arg = (8 * np.sqrt(d) * HALF_FP32 * largest + 16 * HALF_FP32 * (largest + np.log(V))) / 4 + 16 * HALF_FP32
+    off = np.abs(got["rows"] - ref["kd"])
+    bound = arg * np.sqrt(2 * ref["kd"]) + 16 * HALF_FP32 * ref["kd"] + arg * arg
+    print(ref["kd"].min(), ref["kd"].max(), (off / ref["kd"]).max(), (off / bound).max())
+    assert (off <= bound).all()
+    print(check(p, got, ref))
 
 
 @pytest.mark.parametrize("S,d,V", SIZES)
