@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2407_15892_amd as mst
-from tests.objective_gpu_harness import HALF_BF16, HALF_FP32, Problem, Run, check
+from tests.objective_gpu_harness import HALF_BF16, HALF_FP32, Problem, Run, bf16, check
 
 pytestmark = pytest.mark.gpu
 
@@ -96,7 +96,7 @@ def test_softened_distributions_that_are_nearly_the_same(S, d, V, K, tail):
     the largest of these times sum |p - q|, which is at most sqrt(2 kd)."""
     p = Problem(S, d, V, K=K, tail=tail, labels=False, temperature=4.0, sigma=1.5, short=0, empty=0)
     if not tail:                                                     # entries that are nearly all of the student's distribution
-        p.W[:K, 0] = np.abs(p.W[:K, 0]) + 8.0
+        p.W[:K, 0] = bf16(np.abs(p.W[:K, 0]) + 8.0)                    # as the GPU holds it
         p.H[:, 0] = 16.0
         p.index[:] = np.arange(K)
         p.logits = np.float32(p.H @ p.W[:K].T + 0.1 * np.random.default_rng(3).standard_normal((S, K))).astype(np.float64)
