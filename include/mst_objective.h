@@ -30,8 +30,8 @@
  *   label terms          label_coef weight (softmax(y)_v - [v == label]), wce: + 2 z_coef weight lse softmax(y)_v
  *
  * Conventions: those of mst_lmhead.h (device pointers, streams, graphs, errors, M, shapes, alignment), and
- *   - labels equal to ignore_index have no loss; a row whose entries are all missing, or have a logit of -infinity all of them
- *     with teacher_lse NULL, has no teacher;
+ *   - labels equal to ignore_index have no loss; a row whose entries are all missing, or have a logit of -infinity (or one of
+ *     -5e29 or less, as masks of a type's lowest value) all of them with teacher_lse NULL, has no teacher;
  *   - an index below 0 is no entry (rows with fewer than K entries, in any place); an index that comes twice in a row counts
  *     once, with the logit it has first;
  *   - a label outside [0, V) that is not ignore_index, or an index of V or more, never causes an out-of-range access: *loss is
@@ -88,7 +88,7 @@ mst_status mst_lmhead_wce_bwd(const void* H, const void* W, int64_t S, int64_t d
 /*
  *   labels   int32 [S], or NULL: the teacher alone (label_coef 0, nll NULL)
  *   teacher_index  int32 [S, K];  teacher_logits [S, K] of teacher_type (0: bf16, 1: fp32);  teacher_lse fp32 [S] or NULL
- *   K        1 to MST_MAX_ENTRIES;  label_coef, teacher_coef finite;  temperature 0.01 to 100
+ *   K        1 to MST_MAX_ENTRIES, and S * max(K, 64) below 2^32;  label_coef, teacher_coef finite;  temperature 0.01 to 100
  *   nll, kd  out, fp32 [S] each, each may be NULL: 0 where the row has no label, no teacher
  *   n_valid  out, int64 scalar, may be NULL: rows with a label or a teacher
  */

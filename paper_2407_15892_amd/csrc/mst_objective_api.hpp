@@ -56,6 +56,7 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, V, M), &o->p, forced, 0, schedule);
   if (s != MST_OK) return s;
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
+  if (K && S * std::max(K, 64) >= int64_t(1) << 32) return MST_ERR_BAD_SHAPE;      // threads of a launch
   o->p.streamed = 0;      // that order stores no dlogits to put the entries into
   o->K = K;
   o->few = use_tile_few(o->p);
@@ -144,8 +145,8 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   char* const ws = static_cast<char*>(c.workspace);
   char* const saved = static_cast<char*>(c.saved);
   const size_t stride = (size_t)p.fwd_group_rows;
-  // both log-sum-exps, at 1 / T for the teacher and at 1 for the labels, only where they differ
-  const bool two = o.K && c.labels && c.temperature != 1.f;
+  // both log-sum-exps, at 1 / T for the teacher and at 1 for the labels, only where they differ and the second is asked for
+  const bool two = o.K && c.labels && (c.label_coef != 0.f || c.nll) && c.temperature != 1.f;
   const float exponent = (float)(1.4426950408889634 / (double)c.temperature);
   ObjTile e = {};
   e.part = reinterpret_cast<float2*>(ws + (o.few ? o.f_part_few : p.f_part));
@@ -156,7 +157,6 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   e.cap = c.softcap;
   e.exponent = exponent;
   e.exponent_label = kLog2e;
-  e.power = c.temperature == 2.f ? 2 : c.temperature == 4.f ? 4 : 0;
   int* const index = reinterpret_cast<int*>(ws + o.f_index);
   float* const logit = reinterpret_cast<float*>(ws + o.f_logit);
   int* const info = reinterpret_cast<int*>(ws + o.f_info);

@@ -6,7 +6,7 @@
 // the teacher gives, "others" the rest.
 //
 //   forward   k_entries        the teacher's entries of every row in ascending order, and where each vocabulary tile's begin (for
-//                              256-row tiles; calls with smaller tiles find them as they need them: TileEntries)
+//                              tiles of more than 32 rows; others find them as they need them: TileEntries)
 //             (logits)         ObjEpilogue: the label's y and the entries' y out of the accumulators; partial log-sum-exps of the
 //                              others alone, at 1 / T and, where a row needs both, at 1
 //             k_obj_finalize   log-sum-exps, losses, what the backward needs of each row and at each entry
@@ -72,7 +72,6 @@ struct ObjTile {
   const int* index_in_c;
   int* info;
   float cap, exponent, exponent_label;
-  int power;                           // T where it is 2 or 4: the second exponential is a power of the first; else 0
 };
 
 // f(row, place in its list, index) for all entries of a tile's rows, [rows][K] from `index` on.  A thread's first ones can be loaded
@@ -283,26 +282,15 @@ struct ObjEpilogue : ObjTile {
       for (int t = 0; t < TA; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][u][r]);
-      if (two && power) {
+#pragma unroll
+      for (int t = 0; t < TA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
+      if (two) {           // at T = 2 and 4 a power of the first, to no gain: 8192 x 4096 x 128256 5850 us with exponentials, 5888 with squares
 #pragma unroll
         for (int t = 0; t < TA; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float x = fast_exp2((acc[t][u][r] - m) * exponent), x2 = x * x;
-            l += x;
-            k = power == 2 ? k + x2 : __builtin_fmaf(x2, x2, k);
-          }
-      } else {
-#pragma unroll
-        for (int t = 0; t < TA; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) l += fast_exp2((acc[t][u][r] - m) * exponent);
-        if (two) {
-#pragma unroll
-          for (int t = 0; t < TA; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
-        }
+          for (int r = 0; r < 4; ++r) k += fast_exp2((acc[t][u][r] - m) * exponent_label);
       }
 #pragma unroll
       for (int o = 16; o <= 32; o <<= 1)
@@ -499,11 +487,14 @@ __device__ __forceinline__ double log_64(float x) {
 }
 // exp of a logarithm in 64 bits: that of its float32 part, and what that leaves as a factor
 __device__ __forceinline__ float exp_of(double x) {
+  if (!(__builtin_fabs(x) <= 1000.0)) return x < 0.0 ? 0.f : expf((float)x);      // NaN and infinities, and what float32 has no number for
   const float hi = (float)x, lo = (float)(x - (double)hi);
-  return lo == lo ? __builtin_fmaf(expf(hi), lo, expf(hi)) : expf(hi);       // infinities: their difference is no number
+  return __builtin_fmaf(expf(hi), lo, expf(hi));
 }
-// exp(w) - 1 - w: around 0 by its series, whose first term left out is 1 / 40320 w^8
-__device__ __forceinline__ float exp_less_tangent(float w) {
+// q (exp(w) - 1 - w) with q exp(w) = p: around 0 by the series of the bracket, whose first term left out is 1 / 40320 w^8; q (exp(w) - 1)
+// likewise.  Elsewhere by p, as exp(w) has no float32 where q is next to nothing.
+__device__ __forceinline__ float above_tangent(float q, float p, float w) {
+  if (q == 0.f) return p;
   if (__builtin_fabsf(w) < 0.25f) {
     float s = 1.f / 5040.f;
     s = __builtin_fmaf(s, w, 1.f / 720.f);
@@ -511,10 +502,11 @@ __device__ __forceinline__ float exp_less_tangent(float w) {
     s = __builtin_fmaf(s, w, 1.f / 24.f);
     s = __builtin_fmaf(s, w, 1.f / 6.f);
     s = __builtin_fmaf(s, w, 0.5f);
-    return s * w * w;
+    return q * (s * w * w);
   }
-  return (float)((double)expf(w) - 1.0 - (double)w);
+  return (float)((double)p - (double)q - (double)q * (double)w);
 }
+__device__ __forceinline__ float share_less(float q, float p, float w) { return __builtin_fabsf(w) < 1.f ? q * expm1f(w) : p - q; }
 
 // What the loss needs besides the rows'.
 struct ObjLoss {
@@ -686,15 +678,16 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   // distributions (T = 4, 9 of 14144 entries) leave a divergence of 0.002 of logarithms of 10, and float32 differences of these left 2e-4
   // of it.  The logarithms of shares are differences in 64 bits for the same reason.
   const double log_lt = given ? 0.0 : log_64(lt);
-  float q_p[P ? P : 1], w_p[P ? P : 1];
+  float q_p[P ? P : 1], p_p[P ? P : 1], w_p[P ? P : 1];         // shares, the teacher's and the student's, and w
   double sum_q = 0.0, kd_64 = 0.0;
   entries([&](int i) {
     const double log_q = given ? (double)t_p[i] * a.inv_t_64 - (double)given_lse : ((double)t_p[i] - (double)mt) * a.inv_t_64 - log_lt;
     const double log_p = ((double)y_p[i] - (double)m_all) * a.inv_t_64 - log_all;
     q_p[i] = exp_of(log_q);
+    p_p[i] = exp_of(log_p);
     w_p[i] = (float)(log_p - log_q);
     sum_q += (double)q_p[i];
-    kd_64 += q_p[i] == 0.f ? (double)exp_of(log_p) : (double)(q_p[i] * exp_less_tangent(w_p[i]));
+    kd_64 += (double)above_tangent(q_p[i], p_p[i], w_p[i]);
   });
   sum_q = sum16(sum_q);
   kd_64 = sum16(kd_64);
@@ -702,7 +695,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const float rest = rest_64 > 0.0 || rest_64 != rest_64 ? (float)rest_64 : 0.f;
   const float share = others ? exp_of(log_share) : 0.f;                  // the student's of the others
   const float w_rest = rest == 0.f ? 0.f : (float)(log_share - log_64(rest));
-  kd_64 += rest == 0.f ? (double)share : (double)(rest * exp_less_tangent(w_rest));
+  kd_64 += (double)above_tangent(rest, share, w_rest);
   const float over = given ? (float)(sum_q + (double)rest - 1.0) : 0.f;  // where the teacher's entries are more than 1 in all
   const float kd = taught ? (float)(kd_64 + (double)over) : 0.f;
   const float on_kd = taught && weight != 0.f ? weight * a.teacher_coef * a.temperature : 0.f;
@@ -742,7 +735,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   }
   if (!a.rows_c || !in) return;
   // (Q + rest) p - q and (Q + rest) p_rest - rest, whose Q + rest is 1 + over, as q (exp(w) - 1) + over p
-  const float kd_others = on_kd == 0.f ? 0.f : on_kd * ((rest == 0.f ? share : rest * expm1f(w_rest)) + over * share);
+  const float kd_others = on_kd == 0.f ? 0.f : on_kd * ((rest == 0.f ? share : share_less(rest, share, w_rest)) + over * share);
   if (lane == 0) {
     ObjRow row;
     ObjRow2 row2 = {__builtin_inff(), 0.f};
@@ -772,14 +765,11 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     float x = 0.f;
     if (v != kNoEntry) {
       const float ye = y_p[i];
-      if (on_kd != 0.f) {
-        const float p = exp_of(((double)ye - (double)m_all) * a.inv_t_64 - log_all);
-        x = on_kd * ((q_p[i] == 0.f ? p : q_p[i] * expm1f(w_p[i])) + over * p);
-      }
+      if (on_kd != 0.f) x = on_kd * ((q_p[i] == 0.f ? p_p[i] : share_less(q_p[i], p_p[i], w_p[i])) + over * p_p[i]);
       if (on_p != 0.f) x += on_p * expf((ye - m_all) - log_label);
       if (valid && v == y) x -= on_label;
       if (a.cap > 0.f) {
-        const float h = ye / a.cap;
+        const float h = ye / a.cap;                              // 1 - h is off by half a step of 1: 1e-6 of it at z = 2 c, all at 9 c
         x *= (1.f - h) * (1.f + h);
       }
     }

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2407_15892_amd as mst
+from oracle import objective_oracle as orc
 from tests.objective_gpu_harness import HALF_BF16, HALF_FP32, Problem, Run, bf16, check
 
 pytestmark = pytest.mark.gpu
@@ -46,6 +47,35 @@ def test_logits_of_minus_infinity(S, d, V, tail):
     p.logits[::2, 3:9] = -np.inf
     p.logits[::5] = -np.inf                                          # no teacher, or one that gives all to the others
     run_and_check(p)
+
+
+@pytest.mark.parametrize("S,d,V", SIZES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("temperature", [0.02, 1.0])
+def test_masks_of_the_lowest_value_and_shares_that_are_next_to_nothing(S, d, V, tail, temperature):
+    p = Problem(S, d, V, K=30, sigma=2.0 * temperature, tail=tail, temperature=temperature, empty=0)
+    p.logits *= temperature                                          # so that shares are what they are at temperature 1
+    if tail:
+        p.lse = np.float32([orc._lse(1.5 * h @ p.W.T / temperature) for h in p.H]).astype(np.float64)
+    top = p.lse if tail else (p.logits / temperature).max(1)         # exp(-95): float32 has it, but not its reciprocal
+    p.logits[:, 3] = np.float32((top - 95.0) * temperature)
+    p.logits[:, 4:8] = np.float32(-3.0e38)
+    run = Run(p)
+    run.forward()
+    run.backward()
+    p.logits[:, 4:8] = -np.inf                                       # what their shares come to, and the bounds count finite ones
+    print(check(p, run.outputs(), p.oracle()))
+
+
+@pytest.mark.parametrize("S,d,V", SIZES)
+def test_labels_that_only_count(S, d, V):
+    """A coefficient of 0 for the labels and no losses of theirs asked for: one log-sum-exp is enough."""
+    p = Problem(S, d, V, K=30, tail=True, temperature=2.5)
+    run = Run(p)
+    run.nll = None
+    run.forward()
+    run.backward()
+    print(check(p, run.outputs(), p.oracle()))
 
 
 @pytest.mark.parametrize("S,d,V", SIZES)

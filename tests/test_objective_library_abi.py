@@ -147,3 +147,8 @@ def test_binding_refuses_tensors_of_another_kind():
         with pytest.raises(mst.MstError) as e:
             mst.mst_lmhead_wce_bwd(t["H"], t["W"], M, 1.0, saved, t["workspace"], a["dH"], a["dW"])
         assert e.value.status == status, over
+
+
+@pytest.mark.parametrize("s,k,status", [(1 << 26, 1, SHAPE), ((1 << 26) - 1, 64, 0), (1 << 24, 256, SHAPE), ((1 << 24) - 1, 256, 0), (1 << 26, 0, 0)])
+def test_entries_of_more_rows_than_a_launch_has_threads(lib, s, k, status):
+    assert lib.mst_objective_bytes(s, 8, 8, 1, k, None, None, None) == status
