@@ -68,6 +68,28 @@ def test_masks_of_the_lowest_value_and_shares_that_are_next_to_nothing(S, d, V, 
 
 
 @pytest.mark.parametrize("S,d,V", SIZES)
+def test_what_is_not_asked_for_may_hold_anything(S, d, V):
+    """Logits of missing entries, the log-sum-exp of a row without a teacher, the weight of a row without a loss."""
+    for p in both(S, d, V):
+        ref = p.oracle()
+        nothing = p.labels == -100
+        if p.K:
+            p.logits[p.index < 0] = np.nan
+            p.lse[(p.index < 0).all(1)] = np.inf
+            nothing &= (p.index < 0).all(1)
+            nothing[3], p.labels[3], p.index[3] = True, -100, -1
+            ref = p.oracle()
+        p.weights[nothing] = np.nan
+        run = Run(p)
+        run.forward()
+        run.backward()
+        p.weights[nothing] = 1.0
+        if p.K:
+            p.logits[p.index < 0], p.lse[(p.index < 0).all(1)] = 0.0, 0.0
+        print(check(p, run.outputs(), ref))
+
+
+@pytest.mark.parametrize("S,d,V", SIZES)
 def test_labels_that_only_count(S, d, V):
     """A coefficient of 0 for the labels and no losses of theirs asked for: one log-sum-exp is enough."""
     p = Problem(S, d, V, K=30, tail=True, temperature=2.5)
