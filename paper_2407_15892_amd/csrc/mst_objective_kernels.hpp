@@ -917,7 +917,8 @@ struct ObjGrad {
   }
 };
 
-// The teacher's entries of `rows` rows that lie in a window of the vocabulary, into its dlogits.
+// The teacher's entries of some rows that lie in a window of the vocabulary, into its dlogits.  What bounds it are the scattered stores of
+// two bytes: 1.1 million of them, 32768 rows of 256 in one of 7.5 windows, 25 us, also with four entries a thread and 32-bit divisions.
 __global__ __launch_bounds__(256) void k_obj_entries(const int* __restrict__ index, const float* __restrict__ at, long long n, int K,
                                                      int v_base, int V, __bf16* __restrict__ G, int ldg) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
