@@ -62,7 +62,7 @@ extern "C" {
  * Bytes of the forward's and the backward's workspace and of `saved` (host, pure; each pointer may be NULL).  K: 0 for wce.
  * The backward's workspace is that of mst_lmhead_ce_bwd, one mini-sequence (see M above) of fp32 logits; the forward's that of
  * mst_lmhead_ce_fwd and 8 bytes a row, for distill also 6 bytes for each pair that is kept there and 12 K + 4 bytes for each row of
- * a group of mini-sequences.
+ * a group of mini-sequences; small calls up to 0.2 MB more.
  */
 mst_status mst_objective_bytes(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, size_t* fwd_bytes, size_t* bwd_bytes, size_t* saved_bytes);
 

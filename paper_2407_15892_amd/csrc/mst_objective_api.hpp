@@ -21,8 +21,28 @@ struct ObjPlan {
 // the entries of its rows.
 constexpr int kPatchEntries = 64;
 
-// See TileFew.
-bool use_tile_few(const Plan& p) { return p.S <= TileFew::EB && p.S <= p.fwd_group_rows && 2 * p.n_vt <= kNumCu; }
+// See TileFew.  Where tiles of 256 leave a row's pairs to one thread of k_obj_finalize_one and tiles of 64 do not, short hidden sizes are slower
+// with these: 128 rows, V = 4000: d = 128 8.0 us with tiles of 256, 9.3; 512 9.9, 10.3; 1536 16.7, 13.9; 4096 30.0, 21.0.
+int few_row_tiles(const Plan& p) { return (int)((p.S + TileFew::EB - 1) / TileFew::EB); }
+bool use_tile_few(const Plan& p, int K) {
+  if (p.S > p.fwd_group_rows || (p.S + TileFew::EB - 1) / TileFew::EB * p.n_vt > kNumCu / 2) return false;
+  return K || p.S <= kObjRows || p.d >= 1024 || p.n_vt > kFinOneTiles || p.V <= kFinOneTiles * TileFew::EA;
+}
+
+// One workgroup finishes a forward call without a teacher (k_obj_finalize_one).  Whole calls, us, with it and with the two launches of longer ones:
+// 256 rows, d = 512, 32 tiles of 64 9.4, 11.1; 63 tiles (16128 pairs) 12.1, 12.3; 1000 rows, d = 512, 20 tiles of 256 (20000) 17.8, 19.9.  Up to 32 pairs a row are one
+// thread's: split over two, and joined in LDS, 512 rows of 16 take 11.3 in place of 10.5.
+constexpr int64_t kPairsOfOne = 16384;
+int finalize_row_bits(int64_t S, int n_vt) {                       // of its threads, 2^row_bits have the first pair of a row each
+  if (n_vt <= kFinOneTiles) return 10;
+  int bits = 6;
+  while (S > int64_t(1) << bits) ++bits;
+  return bits;
+}
+bool one_finalizes(const ObjPlan& o) {
+  if (o.K || o.p.S > 1024 || o.p.S > o.p.fwd_group_rows || o.p.S * o.n_vt > kPairsOfOne) return false;
+  return o.n_vt <= kFinOneTiles << (10 - finalize_row_bits(o.p.S, o.n_vt));
+}
 
 // Byte ranges of a call's arguments: no output may overlap anything else.
 struct Ranges {
@@ -59,7 +79,7 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   if (K && S * std::max(K, 64) >= int64_t(1) << 32) return MST_ERR_BAD_SHAPE;      // threads of a launch
   o->p.streamed = 0;      // that order stores no dlogits to put the entries into
   o->K = K;
-  o->few = use_tile_few(o->p);
+  o->few = use_tile_few(o->p, K);
   o->n_vt = o->few ? (int)((V + TileFew::EA - 1) / TileFew::EA) : o->p.n_vt;
   const size_t rows = (size_t)o->p.fwd_group_rows, k = (size_t)K;
   size_t off = o->p.f_total;
@@ -187,7 +207,8 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   l.loss = c.loss;
   l.n_valid = reinterpret_cast<long long*>(c.n_valid);
   const bool one_group = p.S <= kObjRows && p.S <= p.fwd_group_rows;       // the call's rows are one workgroup of k_obj_finalize
-  const bool one = one_group || (!o.K && !o.few && finalize_in_one(p));    // the loss is formed with the rows' losses
+  const bool lone = !one_group && one_finalizes(o);
+  const bool one = lone || one_group;                                      // the loss is formed with the rows' losses
   auto logits_from = [&](int64_t g0) -> const void* { return static_cast<const char*>(c.logits) + (size_t)g0 * k * (c.logits_bf16 ? 2 : 4); };
   auto tile_of = [&](int64_t g0) {
     ObjTile of = e;
@@ -222,8 +243,8 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
       }
     }
     Scope sc(st, MST_K_LSE_FINALIZE);
-    if (one && !one_group) {
-      hipLaunchKernelGGL(k_obj_finalize_one, dim3(1), dim3(1024), 0, st, of, l);
+    if (lone) {
+      hipLaunchKernelGGL(k_obj_finalize_one, dim3(1), dim3(1024), 0, st, of, l, finalize_row_bits(p.S, o.n_vt));
       return;
     }
     hipLaunchKernelGGL(finalize_kernel(one, o.K), dim3((unsigned)((g_rows + kObjRows - 1) / kObjRows)), dim3(kObjRows * kObjGroups), 0, st, of, l);
@@ -232,8 +253,8 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   if (o.few) {
     {
       Scope sc(st, MST_K_FWD_GEMM_LSE);
-      hipLaunchKernelGGL((k_fwd_gemm_lse_small<TileFew, ObjEpilogue<kObjAny>>), dim3(even_grid(o.n_vt, 1)), dim3(TileFew::kThreads), TileFew::kLds,
-                         st, H, W, (int)p.S, (int)p.d, (int)p.V, 1, o.n_vt, ObjEpilogue<kObjAny>(tile_of(0)));
+      hipLaunchKernelGGL((k_fwd_gemm_lse_small<TileFew, ObjEpilogue<kObjAny>>), dim3(even_grid(o.n_vt, few_row_tiles(p))), dim3(TileFew::kThreads),
+                         TileFew::kLds, st, H, W, (int)p.S, (int)p.d, (int)p.V, few_row_tiles(p), o.n_vt, ObjEpilogue<kObjAny>(tile_of(0)));
     }
     after(0, (int)p.S);
   } else {

@@ -334,9 +334,10 @@ struct ObjEpilogue : ObjTile {
   }
 };
 
-// Calls of up to 32 rows that have tiles of 256 vocabulary entries for half of the compute units or fewer: W is read once, which is
-// all that takes time, and a compute unit alone does not get its share of the memory's bandwidth.  Tiles of 64, two workgroups on a
-// compute unit where there are as many.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight stages) and these: d = 4096,
+// Calls that have tiles of 32 rows and 256 vocabulary entries for half of the compute units or fewer: with up to 32 rows W is read once, which
+// is all that takes time, and a compute unit alone does not get its share of the memory's bandwidth; with more a few workgroups take
+// the K loop's steps one by one.  Tiles of 64, two workgroups on a compute unit where there are as many.  Whole calls, us, tiles of 256 and these:
+// 33 rows, V = 300: d = 512 9.8, 7.8; 4096 29.1, 17.2; 500 rows, V = 1000: 1536 16.3, 12.0; with 30 entries 23.9, 18.7.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight stages) and these: d = 4096,
 // V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048, V = 4000 19.6, 15.8, 13.4.
 // (With both operands from memory straight into registers, a wave to 16 vocabulary entries: 57.8 for one row, 71.4 for 16.)
 typedef CfgSmall<2, 1, 6, 6, true> TileFew;
@@ -817,20 +818,47 @@ __global__ __launch_bounds__(1024) void k_obj_loss(const float2* __restrict__ ro
   reduce_obj_loss(o, a, n, bad);
 }
 
-// k_obj_finalize and k_obj_loss of calls without a teacher that are few rows and vocabulary tiles (finalize_in_one), from one
-// workgroup: a thread has a row and all of its pairs in flight at once, as k_finalize_loss.
-__global__ __launch_bounds__(1024) void k_obj_finalize_one(ObjFinal a, ObjLoss o) {
-  const int s = threadIdx.x;
-  float loss = 0.f;
-  int count = 0;
-  if (s < a.rows) {
+// k_obj_finalize and k_obj_loss of calls without a teacher that are few rows and vocabulary tiles (one_finalizes), from one
+// workgroup: up to 16 threads, 2^row_bits apart, have a row and all of its pairs in flight at once, as k_finalize_loss.
+constexpr int kOneGroups = 16;
+__global__ __launch_bounds__(1024) void k_obj_finalize_one(ObjFinal a, ObjLoss o, int row_bits) {
+  __shared__ float2 sh[1024];
+  const int s = threadIdx.x & ((1 << row_bits) - 1), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> row_bits), groups = 1024 >> row_bits;
+  const bool in = s < a.rows;
+  int y = 0;
+  float z_y = 0.f, weight = 1.f, m = kMasked, l = 0.f;
+  if (in) {
     float2 p[kFinOneTiles];
 #pragma unroll
-    for (int vt = 0; vt < kFinOneTiles; ++vt) p[vt] = vt < a.n_vt ? a.part[(size_t)vt * a.part_stride + s] : make_float2(kMasked, 0.f);
-    const int y = a.labels_c[s];
-    const float z_y = a.tgt[s], weight = a.weights_c ? a.weights_c[s] : 1.f;
-    float m = kMasked, l = 0.f;
+    for (int i = 0; i < kFinOneTiles; ++i) {
+      const int vt = g + i * groups;
+      p[i] = vt < a.n_vt ? a.part[(size_t)vt * a.part_stride + s] : make_float2(kMasked, 0.f);
+    }
+    y = a.labels_c[s];
+    z_y = a.tgt[s];
+    if (a.weights_c) weight = a.weights_c[s];
     fold_lse(m, l, p);
+  }
+  if (groups > 1) {
+    sh[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (groups <= 4) {
+      for (int i = 1; i < groups; ++i) {
+        const float2 q = sh[(threadIdx.x + (i << row_bits)) & 1023];
+        merge_lse(m, l, q.x, q.y);
+      }
+    } else {
+      float2 q[kOneGroups];
+#pragma unroll
+      for (int i = 0; i < kOneGroups; ++i) q[i] = i < groups ? sh[(i << row_bits) | s] : make_float2(kMasked, 0.f);
+      m = kMasked;
+      l = 0.f;
+      fold_lse(m, l, q);
+    }
+  }
+  float loss = 0.f;
+  int count = 0;
+  if (in && g == 0) {
     const float log_l = logf(l), lse = m + log_l;
     const bool valid = y != a.ignore_index && (unsigned)y < (unsigned)a.V;
     const float nll = valid ? (m - z_y) + log_l : 0.f;

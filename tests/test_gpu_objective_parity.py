@@ -96,6 +96,18 @@ def test_a_few_rows(S, d):
         print(check(p, run.outputs(), p.oracle()))
 
 
+@pytest.mark.parametrize("S,d,V", [(17, 1032, 2049), (20, 8, 9000), (33, 1032, 4000), (100, 1032, 8000), (256, 1032, 4000), (400, 1032, 2100), (1000, 64, 700),
+                                   (2000, 64, 500)])
+def test_several_tiles_of_few_rows(S, d, V):
+    """Several row tiles of 64 vocabulary entries, their losses from one workgroup (one, two, four or sixteen threads a row) or from two launches."""
+    for o in (dict(K=33, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=4.0, z_coef=1e-3, weights=True)):
+        p = Problem(S, d, V, **o)
+        run = Run(p)
+        run.forward()
+        run.backward()
+        print(check(p, run.outputs(), p.oracle()))
+
+
 @pytest.mark.parametrize("S,d,V,mini_sequences", [(2300, 64, 150000, 3), (4196, 4096, 40960, 2)])
 @pytest.mark.parametrize("o", [dict(K=30, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=20.0, weights=True, z_coef=1e-3)])
 def test_several_mini_sequences(S, d, V, mini_sequences, o):
