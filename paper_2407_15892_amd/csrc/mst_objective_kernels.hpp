@@ -337,8 +337,9 @@ struct ObjEpilogue : ObjTile {
 // Calls that have tiles of 32 rows and 256 vocabulary entries for half of the compute units or fewer: with up to 32 rows W is read once, which
 // is all that takes time, and a compute unit alone does not get its share of the memory's bandwidth; with more a few workgroups take
 // the K loop's steps one by one.  Tiles of 64, two workgroups on a compute unit where there are as many.  Whole calls, us, tiles of 256 and these:
-// 33 rows, V = 300: d = 512 9.8, 7.8; 4096 29.1, 17.2; 500 rows, V = 1000: 1536 16.3, 12.0; with 30 entries 23.9, 18.7.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight stages) and these: d = 4096,
-// V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048, V = 4000 19.6, 15.8, 13.4.
+// 33 rows, V = 300: d = 512 9.8, 7.8; 4096 29.1, 17.2; 500 rows, V = 1000: 1536 16.3, 12.0; with 30 entries 23.9, 18.7; but where tiles of 256
+// are for all compute units, 512 rows, V = 4096, d = 1024 15.1, 22.2.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight
+// stages) and these: d = 4096, V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048, V = 4000 19.6, 15.8, 13.4.
 // (With both operands from memory straight into registers, a wave to 16 vocabulary entries: 57.8 for one row, 71.4 for 16.)
 typedef CfgSmall<2, 1, 6, 6, true> TileFew;
 
