@@ -44,6 +44,8 @@ struct Plan {
   int dh_ksteps;    // K steps (of kBK) per split
   // pair order: 64 x 64 tiles instead of 256 x 256 ones, per launch kind (mst_small_kernels.hpp)
   bool small_dlogits, small_dh, small_dw;
+  int dw_split, dw_per;   // other objectives, one chunk: parts of dW's contraction and their rows (0: one), partials in the free slot;
+  bool dw_split_small;    // in small tiles
   int small_dh_split, small_dh_ksteps;
   int joint;        // pair order: dH and dW from one launch, dlogits of a pair from another (MST_PAIR_* of the header)
   double joint_us;
@@ -514,6 +516,7 @@ mst_status make_plan(int64_t S, int64_t d, int64_t V, int32_t M, Plan* p, int fo
     p->small_dlogits = small_launch_us(tiles_of(C, V, 64), kd) < big_launch_us(tiles_of(C, V, 256), kd);
     const int64_t pair = p->n_chunks > 1 ? 2 * C : C;
     const double kw = (double)((pair + kBK - 1) / kBK);
+    p->dw_split = 0;
     p->small_dw = small_launch_us(tiles_of(V, d, 64), kw) < big_launch_us(tiles_of(V, d, 256), kw);
     auto reduce_us = [&](int s) { return s > 1 ? 4.0 + (double)s * (double)(C * d) * 8.0 / 4.6e6 : 0.0; };
     double t_best = big_launch_us((double)out_tiles * p->dh_split, (double)p->dh_ksteps) + reduce_us(p->dh_split);
@@ -605,6 +608,8 @@ bool set_kernel_attributes() {   // on the current device
   set((const void*)k_bwd_gemm_dh_small<Tile64Lone>);
   set((const void*)k_bwd_gemm_dw_small<Tile64>);
   set((const void*)k_bwd_gemm_dw_small<Tile64Lone>);
+  set((const void*)k_bwd_gemm_dw_split_small<Tile64>);
+  set((const void*)k_bwd_gemm_dw_split);
   set((const void*)k_bwd_gemm_dh_dw_small<TileKSplit32x16, Tile64>);
   set((const void*)k_bwd_gemm_dh_dw_small<TileKSplit64x16, Tile64>);
   set((const void*)k_bwd_gemm_dh_dw_small<TileKSplit64x32, Tile64>);
@@ -815,6 +820,21 @@ mst_status run_backward_orders(const Plan& p, const __bf16* Hb, const __bf16* Wb
   };
   auto grad_w = [&](int i_first, int i_last, int rows) {
     const int64_t r0 = (int64_t)i_first * p.C;
+    if (p.dw_split) {
+      float* const partial = reinterpret_cast<float*>(slot[1]);
+      const int edge = p.dw_split_small ? Tile64::EB : kTile;
+      const int n_v = (int)((p.V + edge - 1) / edge), n_j = (int)((p.d + edge - 1) / edge);
+      {
+        Scope sc(st, MST_K_BWD_GEMM_DW);
+        hipLaunchKernelGGL(p.dw_split_small ? k_bwd_gemm_dw_split_small<Tile64> : k_bwd_gemm_dw_split, dim3(even_grid(p.dw_split * n_v, n_j)),
+                           dim3(p.dw_split_small ? Tile64::kThreads : kThreads), p.dw_split_small ? Tile64::kLds : kLdsBytes, st, slot[0], p.ldg, Hb,
+                           rows, (int)p.d, (int)p.V, n_v, n_j, p.dw_split, p.dw_per, partial);
+      }
+      Scope sc(st, MST_K_BWD_DH_REDUCE);
+      const size_t n = (size_t)p.V * p.d;
+      hipLaunchKernelGGL(k_bwd_dw_reduce, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, partial, p.dw_split, n, nv, grad_loss, dW);
+      return;
+    }
     Scope sc(st, MST_K_BWD_GEMM_DW);
     if (p.small_dw) {
       const int n_vh = (int)((p.V + Tile64::EB - 1) / Tile64::EB), n_jh = (int)((p.d + Tile64::EA - 1) / Tile64::EA);

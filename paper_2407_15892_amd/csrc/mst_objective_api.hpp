@@ -72,12 +72,34 @@ int32_t fewer_mini_sequences(int64_t S, int64_t V, int32_t M) {
   return (int32_t)std::min<int64_t>(M, (S + rows - 1) / rows);
 }
 
+// dW of few vocabulary entries and many rows is a few tiles with a long contraction over the rows, which is split then.  The partials fit into
+// the half of the workspace that one mini-sequence's dlogits leave; the launch models are those that rank the tiles.  Backward, us, without and
+// with: 30000 rows, d = 128, V = 352 114, 46; 65536, 1024, 512 415, 246; 32768, 2048, 384 245, 217; 16384, 512, 1000 132, 94; where the models see less than
+// 15 % the launch stays whole (5000, 2048, 256: 53).
+void split_dw(Plan* p) {
+  if (p->blk_use || p->joint || p->n_chunks != 1) return;
+  const double ksteps = (double)((p->C + kBK - 1) / kBK), bytes = 4.0 * (double)(p->V * p->d);
+  const double t64 = tiles_of(p->V, p->d, 64), t256 = tiles_of(p->V, p->d, 256);
+  double best = 0.85 * (p->small_dw ? small_launch_us(t64, ksteps) : big_launch_us(t256, ksteps));
+  const int64_t room = (int64_t)((double)p->b_slot / bytes);
+  for (int s = 2; s <= 64 && s <= room && s <= ksteps; ++s) {
+    const double per = std::ceil(ksteps / s), sum = 4.0 + (s + 1) * bytes / 4.6e6;
+    const double small = small_launch_us(t64 * s, per) + sum, big = big_launch_us(t256 * s, per) + sum;
+    if (std::min(small, big) >= best) continue;
+    best = std::min(small, big);
+    p->dw_per = (int)per * kBK;
+    p->dw_split = (int)std::ceil(ksteps / per);
+    p->dw_split_small = small < big;
+  }
+}
+
 mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO, bool schedule = false) {
   const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, V, M), &o->p, forced, 0, schedule);
   if (s != MST_OK) return s;
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
   if (K && S * std::max(K, 64) >= int64_t(1) << 32) return MST_ERR_BAD_SHAPE;      // threads of a launch
   o->p.streamed = 0;      // that order stores no dlogits to put the entries into
+  if (schedule) split_dw(&o->p);
   o->K = K;
   o->few = use_tile_few(o->p, K);
   o->n_vt = o->few ? (int)((V + TileFew::EA - 1) / TileFew::EA) : o->p.n_vt;

@@ -255,6 +255,42 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dw
   dw_tile_small<C>(G, ldg, ldg, Hc, d, rows, d, V, vt, jt, accumulate != 0, scale, dW, d, smem);
 }
 
+// dW with its contraction over the rows in n_split parts of `per` rows, for a small matrix of many rows: sums of each part, for k_bwd_dw_reduce.
+template <class Tile>
+__device__ __forceinline__ void dw_split_tile(const __bf16* __restrict__ G, int ldg, const __bf16* __restrict__ H, int rows, int d, int V, int n_vt,
+                                              int n_jt, int n_split, int per, float* __restrict__ partial, Tile tile) {
+  int slow, jt;
+  if (!even_tile_of_block(blockIdx.x, n_split * n_vt, n_jt, &slow, &jt)) return;
+  const int sp = slow / n_vt, r0 = sp * per;
+  tile(G + (size_t)r0 * ldg, H + (size_t)r0 * d, rows - r0 < per ? rows - r0 : per, slow - sp * n_vt, jt, partial + (size_t)sp * V * d);
+}
+template <class C>
+__global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dw_split_small(
+    const __bf16* __restrict__ G, int ldg, const __bf16* __restrict__ H, int rows, int d, int V, int n_vt, int n_jt, int n_split, int per,
+    float* __restrict__ partial) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  dw_split_tile(G, ldg, H, rows, d, V, n_vt, n_jt, n_split, per, partial, [&](const __bf16* g, const __bf16* h, int n, int vt, int jt, float* out) {
+    dw_tile_small<C>(g, ldg, ldg, h, d, n, d, V, vt, jt, false, 1.f, out, d, smem);
+  });
+}
+__global__ __launch_bounds__(kThreads) void k_bwd_gemm_dw_split(
+    const __bf16* __restrict__ G, int ldg, const __bf16* __restrict__ H, int rows, int d, int V, int n_vt, int n_jt, int n_split, int per,
+    float* __restrict__ partial) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  dw_split_tile(G, ldg, H, rows, d, V, n_vt, n_jt, n_split, per, partial, [&](const __bf16* g, const __bf16* h, int n, int vt, int jt, float* out) {
+    dw_tile(g, ldg, ldg, h, d, n, d, V, vt, jt, 0, 0, 1.f, out, d, smem);
+  });
+}
+// gamma times the parts' sums in their order, four entries (of n = V d) a thread
+__global__ __launch_bounds__(256) void k_bwd_dw_reduce(const float* __restrict__ partial, int n_split, size_t n, const long long* __restrict__ n_valid,
+                                                       float grad_loss, float* __restrict__ dW) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  f32x4 a = *reinterpret_cast<const f32x4*>(partial + i);
+  for (int sp = 1; sp < n_split; ++sp) a += *reinterpret_cast<const f32x4*>(partial + sp * n + i);
+  *reinterpret_cast<f32x4*>(dW + i) = a * gamma_of(n_valid, grad_loss);
+}
+
 // ---------------------------------------------------------------------------
 // backward 2 and 3 from one launch: neither needs the other.  In the smallest problems a launch takes 4 to 6 us whatever
 // it does, and the pair order has seven of them per pair of chunks; these two kernels make two of them.

@@ -108,6 +108,20 @@ def test_several_tiles_of_few_rows(S, d, V):
         print(check(p, run.outputs(), p.oracle()))
 
 
+@pytest.mark.parametrize("S,d,V", [(5000, 72, 300), (9001, 264, 130), (20000, 64, 257), (6000, 1032, 40), (30001, 520, 8), (8191, 2048, 260)])
+def test_many_rows_of_a_small_vocabulary(S, d, V):
+    """The weights' gradient from parts of the rows; the same bits whatever M is."""
+    for o in (dict(K=7, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=4.0, z_coef=1e-3, weights=True)):
+        p = Problem(S, d, V, **o)
+        run = Run(p)
+        run.forward()
+        run.backward(M=S // 300)
+        first = run.dW.clone()
+        run.backward()
+        assert run.torch.equal(first, run.dW)
+        print(check(p, run.outputs(), p.oracle()))
+
+
 @pytest.mark.parametrize("S,d,V,mini_sequences", [(2300, 64, 150000, 3), (4196, 4096, 40960, 2)])
 @pytest.mark.parametrize("o", [dict(K=30, tail=True, label_coef=0.5, temperature=2.0, weights=True), dict(softcap=20.0, weights=True, z_coef=1e-3)])
 def test_several_mini_sequences(S, d, V, mini_sequences, o):
