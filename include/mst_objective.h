@@ -45,7 +45,9 @@
  *   - arithmetic: that of mst_lmhead.h; the loss and the rows' outputs float32 (sums over rows in 64 bits), the gradient of the
  *     logits without the factor grad_loss / n rounded to bf16 before the two products; everything in a fixed order, without
  *     atomics: repeated calls give the same bits.
- *   - No output and neither `saved` nor the workspace may overlap another argument (MST_ERR_BAD_ARGUMENT).
+ *   - no output and neither `saved` nor the workspace may overlap another argument (MST_ERR_BAD_ARGUMENT);
+ *   - mst_profile_collect counts the launches under the kinds of the plain calls' that they stand for: sorting a teacher's entries under the
+ *     label scan, putting them into the logits' gradient and adding up dW's parts under dH's reduce.
  */
 #ifndef MST_OBJECTIVE_H
 #define MST_OBJECTIVE_H

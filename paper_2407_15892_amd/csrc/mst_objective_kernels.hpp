@@ -10,7 +10,7 @@
 //             (logits)         ObjEpilogue: the label's y and the entries' y out of the accumulators; partial log-sum-exps of the
 //                              others alone, at 1 / T and, where a row needs both, at 1
 //             k_obj_finalize   log-sum-exps, losses, what the backward needs of each row and at each entry
-//             k_obj_loss       the loss, in a fixed order
+//             k_obj_loss       the loss, in a fixed order (small calls: with the rows' losses, by k_obj_finalize or k_obj_finalize_one)
 //   backward  (logits again)   ObjGrad: every entry of a row as two coefficients times exponentials
 //             k_obj_entries    the teacher's entries put into the block of dlogits
 //
