@@ -52,7 +52,7 @@
  *     tile maps are laid out for 8 XCDs of 32 compute units.
  *   - Requirements: d % 8 == 0; H, W, dH, dW 16-byte aligned; lse 4-byte
  *     aligned; workspace 256-byte aligned; 1 <= M <= S; d < 2^22;
- *     V * d < 2^31; ceil(S/M) * (V rounded up to 8) < 2^30.
+ *     V * d < 2^31; ceil(S/M) * (V rounded up to 8) < 2^30; ceil(S/M) * d < 2^30.
  *   - Arithmetic: bf16 operands, fp32 MFMA accumulation, fp32 log-sum-exp and
  *     softmax, dlogits = softmax - onehot rounded to bf16 (nearest even)
  *     before the two gradient GEMMs, grad_loss / N_valid applied in fp32 by

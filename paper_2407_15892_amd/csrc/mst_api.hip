@@ -1045,7 +1045,7 @@ const char* mst_strerror(mst_status s) {
   switch (s) {
     case MST_OK: return "ok";
     case MST_ERR_NULL_POINTER: return "a required pointer is NULL";
-    case MST_ERR_BAD_SHAPE: return "bad shape: S, d, V must be positive, d % 8 == 0, d < 2^22, V*d < 2^31, ceil(S/M)*V < 2^30";
+    case MST_ERR_BAD_SHAPE: return "bad shape: S, d, V must be positive, d % 8 == 0, d < 2^22, V*d < 2^31, ceil(S/M)*V and ceil(S/M)*d < 2^30";
     case MST_ERR_BAD_M: return "M must satisfy 1 <= M <= S";
     case MST_ERR_WORKSPACE: return "workspace is NULL or too small (see mst_workspace_bytes)";
     case MST_ERR_ALIGNMENT: return "pointer alignment: H, W, dH, dW 16 bytes; workspace 256 bytes; n_valid 8 bytes; labels, lse, loss 4 bytes";

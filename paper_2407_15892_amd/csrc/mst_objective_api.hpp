@@ -66,9 +66,10 @@ struct Ranges {
 // with 10, 1452 with 4, 1380 with 3, 1407 with 2, 1552 with 1 (610 MB); 8192, 4096, 128256: 19616 with 31 (129 MB), 19324 with 16, 18694
 // with 8, 18593 with 4 (1 GB); 20000, 520, 30000: 3927 with 57 (40 MB), 2300 with 16, 2245 with 4; 3000, 1024, 8000: 340 with 8, 152 with 1.
 constexpr int64_t kObjRoom = int64_t(512) << 20;
-int32_t fewer_mini_sequences(int64_t S, int64_t V, int32_t M) {
-  if (S < 1 || V < 1 || V >= (int64_t(1) << 31) || M < 1 || M > S) return M;      // refused by make_plan
-  const int64_t rows = std::max<int64_t>(1, kObjRoom / (4 * ((V + 7) / 8 * 8)));
+int32_t fewer_mini_sequences(int64_t S, int64_t d, int64_t V, int32_t M) {
+  if (S < 1 || d < 1 || V < 1 || V >= (int64_t(1) << 31) || M < 1 || M > S) return M;      // refused by make_plan
+  // never so long that a mini-sequence's rows x d reach 2^30, which make_plan refuses
+  const int64_t rows = std::max<int64_t>(1, std::min(kObjRoom / (4 * ((V + 7) / 8 * 8)), ((int64_t(1) << 30) - 1) / d));
   return (int32_t)std::min<int64_t>(M, (S + rows - 1) / rows);
 }
 
@@ -94,7 +95,7 @@ void split_dw(Plan* p) {
 }
 
 mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO, bool schedule = false) {
-  const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, V, M), &o->p, forced, 0, schedule);
+  const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, d, V, M), &o->p, forced, 0, schedule);
   if (s != MST_OK) return s;
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;
   if (K && S * std::max(K, 64) >= int64_t(1) << 32) return MST_ERR_BAD_SHAPE;      // threads of a launch
