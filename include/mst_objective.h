@@ -42,7 +42,8 @@
  *     it; H, W, S, d, V and K have to be those of the forward call, M need not be.  NULL where no backward call follows;
  *   - M is the largest number of mini-sequences: the calls make fewer, longer ones as long as the fp32 logits of one are at most
  *     512 MiB and its rows x d below 2^30, and their workspace is that of these;
- *   - arithmetic: that of mst_lmhead.h; the loss and the rows' outputs float32 (sums over rows in 64 bits), the gradient of the
+ *   - arithmetic: that of mst_lmhead.h; a capped logit within 8 half steps of float32 of its value, at any cap; the loss and the
+ *     rows' outputs float32 (sums over rows in 64 bits), the gradient of the
  *     logits without the factor grad_loss / n rounded to bf16 before the two products; everything in a fixed order, without
  *     atomics: repeated calls give the same bits.
  *   - no output and neither `saved` nor the workspace may overlap another argument (MST_ERR_BAD_ARGUMENT);

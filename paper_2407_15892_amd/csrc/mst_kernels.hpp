@@ -652,7 +652,8 @@ __global__ __launch_bounds__(1024) void k_finalize_loss(
 //
 // What an entry is, the objective's gradient E says:
 //   load(s)                 what it needs of a row;  settle(row): the same, ready for use (behind all loads)
-//   with(row, f)            calls f with a function of a logit that gives the entry, the label's own term left out
+//   with(row, top, f)       calls f with a function of a logit that gives the entry, the label's own term left out; top() is the largest
+//                           magnitude among the logits that f asks for
 //   label(row)              the row's label, -1 for none;  label_term(row, z): what its entry is less by
 //   kPatch, patch(...)      whether entries are put into a small tile behind all others (mst_objective_kernels.hpp)
 struct CeGrad {
@@ -671,8 +672,8 @@ struct CeGrad {
   // z - lse is formed first and scaled afterwards: where a class dominates (z close to lse) the difference is exact,
   // so p - 1 at a confidently predicted label keeps full precision, and a one-class vocabulary gives exactly 0.
   __device__ __forceinline__ static float entry(const Row& r, float z) { return fast_exp2((z - r.lse) * kLog2e); }
-  template <class F>
-  __device__ __forceinline__ void with(const Row& r, F f) const { f([&r](float z) { return entry(r, z); }); }
+  template <class Top, class F>
+  __device__ __forceinline__ void with(const Row& r, Top, F f) const { f([&r](float z) { return entry(r, z); }); }
   __device__ __forceinline__ int label(const Row& r) const { return r.y; }
   __device__ __forceinline__ float label_term(const Row&, float) const { return 1.0f; }
 };
@@ -729,7 +730,15 @@ __global__ __launch_bounds__(kThreads) void k_bwd_gemm_dlogits(
     const int y_abs = grad.label(of);
     const int y_lane = y_abs >= 0 ? y_abs - v_base - va : -1;   // the label's position among this lane's 32 entries, if it is there
     char* srow = smem + row * kStageRow + (wa * 128 + 32 * (lane >> 4)) * 2;
-    grad.with(of, [&](auto entry) {
+    auto top = [&]() {
+      float m = 0.f;
+#pragma unroll
+      for (int t = 0; t < kTA16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, __builtin_fabsf(acc[t][u][r]));
+      return m;
+    };
+    grad.with(of, top, [&](auto entry) {
 #pragma unroll
       for (int p = 0; p < kTA16 / 2; ++p) {            // tiles 2p and 2p + 1: entries va + 8p .. + 7
         bf16x8 o;
@@ -748,7 +757,9 @@ __global__ __launch_bounds__(kThreads) void k_bwd_gemm_dlogits(
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (4 * t + r == y_lane) z_y = acc[t][u][r];
-      grad.with(of, [&](auto entry) { *reinterpret_cast<__bf16*>(srow + 2 * y_lane) = (__bf16)(entry(z_y) - grad.label_term(of, z_y)); });
+      grad.with(of, [&]() { return z_y; }, [&](auto entry) {
+        *reinterpret_cast<__bf16*>(srow + 2 * y_lane) = (__bf16)(entry(z_y) - grad.label_term(of, z_y));
+      });
     }
   }
   __syncthreads();

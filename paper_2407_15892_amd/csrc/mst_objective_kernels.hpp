@@ -17,6 +17,8 @@
 // The others' log-sum-exp is formed without the entries, not as a difference: where the student gives nearly everything to the
 // entries a difference of float32 numbers would leave nothing of the share of the others.
 #pragma once
+#include <type_traits>
+
 #include "mst_small_kernels.hpp"
 
 namespace mst {
@@ -38,14 +40,40 @@ struct ObjHeader {
 struct ObjRow { float base, at, label_term; int label; };
 struct ObjRow2 { float base, at; };
 
-// y = c tanh(z / c) and dy/dz = 1 - tanh^2, by u = 1 / (1 + exp(2 |z| / c)), which is at most 1/2: tanh = sign(z) (1 - 2 u) and
-// 1 - tanh^2 = 4 u (1 - u), without cancellation in the second at any z.
-__device__ __forceinline__ float cap_u(float z, float scale /* 2 log2(e) / c */) {
-  return __builtin_amdgcn_rcpf(1.f + fast_exp2(__builtin_fabsf(z) * scale));
-}
-__device__ __forceinline__ float capped(float z, float cap, float scale) {
-  return __builtin_copysignf(cap - 2.f * cap * cap_u(z, scale), z);
-}
+// y = c tanh(z / c) and its slope 1 - tanh^2, x = z / c, without cancellation anywhere:
+//   |x| < 1/2   tanh x = x + x p, p = x^2 q(x^2), with q of degree 3 the polynomial whose largest relative error in tanh is least (1.5e-8, by
+//               weighted least squares until the errors' peaks are equal); 1 - tanh^2 as it stands, tanh^2 being at most 0.22.  1.3 half steps of y.
+//   elsewhere   by u = 1 / (1 + exp(2 |x|)) <= 0.27: tanh |x| = 1 - 2 u, slope 4 u (1 - u).  5 half steps of y.
+// Formed as 1 - 2 u throughout, y is half a step of the cap off whatever z is: 0.12 at a cap of 1e6.  The polynomial alone costs less than
+// exp2 and the reciprocal, both ways and a choice more; 8192 x 3584 x 128000, logits of 2.5, us, forward and backward: no cap 4950, 16300; as
+// 1 - 2 u 5125, 16600 at any cap; so 5080, 16600 at caps of 50 and 30, 5320, 17200 at 10 and 2.
+struct Cap {
+  float c, by_c, scale;                // 2 log2(e) / c
+  __device__ __forceinline__ explicit Cap(float cap) : c(cap), by_c(1.f / cap), scale(2.f * kLog2e / cap) {}
+  __device__ __forceinline__ bool near(float z) const { return __builtin_fabsf(z) < 0.5f * c; }
+  __device__ __forceinline__ float p(float x) const {
+    const float w = x * x;
+    float q = 1.724154502e-2f;
+    q = __builtin_fmaf(q, w, -5.304551497e-2f);
+    q = __builtin_fmaf(q, w, 1.332587898e-1f);
+    q = __builtin_fmaf(q, w, -3.333314359e-1f);
+    return w * q;
+  }
+  __device__ __forceinline__ float u(float z) const { return __builtin_amdgcn_rcpf(1.f + fast_exp2(__builtin_fabsf(z) * scale)); }
+  // kNear: |z| < c / 2 is known; else both ways, the same bits
+  template <bool kNear> __device__ __forceinline__ float y(float z) const {
+    const float at_0 = __builtin_fmaf(z, p(z * by_c), z);
+    if (kNear) return at_0;
+    const float far = __builtin_copysignf(c - 2.f * c * u(z), z);
+    return near(z) ? at_0 : far;
+  }
+  template <bool kNear> __device__ __forceinline__ float slope(float z) const {
+    const float x = z * by_c, t = __builtin_fmaf(x, p(x), x), at_0 = __builtin_fmaf(-t, t, 1.f);
+    if (kNear) return at_0;
+    const float v = u(z);
+    return near(z) ? at_0 : 4.f * v * (1.f - v);
+  }
+};
 
 // merge_lse for sums of exp2(exponent (y - m)), and a second sum beside the first at another exponent
 __device__ __forceinline__ void merge_sums(float& m, float& l, float& k, float m2, float l2, float k2, float exponent, float exponent_label, bool two) {
@@ -190,13 +218,22 @@ struct ObjEpilogue : ObjTile {
       to[u] = teacher && kSorted ? starts[(size_t)(vt + 1) * part_stride + s_in] : 0;
     }
     if (kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap) {
-      const float scale = 2.f * kLog2e / cap;
+      const Cap bend(cap);
 #pragma unroll
-      for (int t = 0; t < TA; ++t)
+      for (int t = 0; t < TA; ++t) {
+        float top = 0.f;               // 16 logits of a lane at a time: seldom is one of the wave's far from 0
 #pragma unroll
         for (int u = 0; u < TB; ++u)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[t][u][r] = capped(acc[t][u][r], cap, scale);
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, __builtin_fabsf(acc[t][u][r]));
+        auto all = [&](auto near) {
+#pragma unroll
+          for (int u = 0; u < TB; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[t][u][r] = bend.template y<decltype(near)::value>(acc[t][u][r]);
+        };
+        if (__any(!bend.near(top))) all(std::false_type()); else all(std::true_type());
+      }
     }
     float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
     // The entries' y out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's.
@@ -912,32 +949,24 @@ struct ObjGrad {
   __device__ __forceinline__ Row settle(const Row& r) const { return r; }
   __device__ __forceinline__ int label(const Row& r) const { return r.a.label; }
   __device__ __forceinline__ float label_term(const Row& r, float z) const {
-    if (!(head->cap > 0.f)) return r.a.label_term;
-    const float u = cap_u(z, 2.f * kLog2e / head->cap);
-    return r.a.label_term * (4.f * u * (1.f - u));
+    return head->cap > 0.f ? r.a.label_term * Cap(head->cap).slope<false>(z) : r.a.label_term;
   }
-  template <class F>
-  __device__ __forceinline__ void with(const Row& r, F f) const {
+  template <class Top, class F>
+  __device__ __forceinline__ void with(const Row& r, Top top, F f) const {
     const float c1 = head->exponent, c2 = head->exponent_label, cap = head->cap;
     if (cap > 0.f) {
-      const float scale = 2.f * kLog2e / cap;
-      auto split = [=](float z, float& y) {
-        const float u = cap_u(z, scale);
-        y = __builtin_copysignf(cap - 2.f * cap * u, z);
-        return 4.f * u * (1.f - u);
+      const Cap bend(cap);
+      auto capped = [&](auto near) {
+        constexpr bool kNear = decltype(near)::value;
+        if (head->two)
+          f([&](float z) {
+            const float y = bend.template y<kNear>(z);
+            return bend.template slope<kNear>(z) * (r.a.at * fast_exp2((y - r.a.base) * c1) + r.b.at * fast_exp2((y - r.b.base) * c2));
+          });
+        else
+          f([&](float z) { return bend.template slope<kNear>(z) * (r.a.at * fast_exp2((bend.template y<kNear>(z) - r.a.base) * c1)); });
       };
-      if (head->two)
-        f([&](float z) {
-          float y;
-          const float slope = split(z, y);
-          return slope * (r.a.at * fast_exp2((y - r.a.base) * c1) + r.b.at * fast_exp2((y - r.b.base) * c2));
-        });
-      else
-        f([&](float z) {
-          float y;
-          const float slope = split(z, y);
-          return slope * (r.a.at * fast_exp2((y - r.a.base) * c1));
-        });
+      if (__any(!bend.near(top()))) capped(std::false_type()); else capped(std::true_type());
     } else if (head->two) {
       f([&](float z) { return r.a.at * fast_exp2((z - r.a.base) * c1) + r.b.at * fast_exp2((z - r.b.base) * c2); });
     } else {

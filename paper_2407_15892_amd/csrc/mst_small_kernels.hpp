@@ -106,7 +106,15 @@ __global__ __launch_bounds__(C::kThreads, kSmallWavesPerSimd) void k_bwd_gemm_dl
     const int y_abs = grad.label(of);
     const int y_lane = y_abs >= 0 ? y_abs - va : -1;
     char* srow = smem + row * kStageRow + va_tile * 2;
-    grad.with(of, [&](auto entry) {
+    auto top = [&]() {
+      float m = 0.f;
+#pragma unroll
+      for (int t = 0; t < C::TA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, __builtin_fabsf(acc[t][u][r]));
+      return m;
+    };
+    grad.with(of, top, [&](auto entry) {
 #pragma unroll
       for (int p = 0; p < C::TA / 2; ++p) {
         bf16x8 o;
