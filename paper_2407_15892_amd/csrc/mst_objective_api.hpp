@@ -13,7 +13,7 @@ struct ObjPlan {
   bool few;              // the forward's tiles are TileFew, not the plain forward's
   int n_vt;              // vocabulary tiles of the forward
   // forward workspace: the plain forward's, then
-  size_t f_part_few, f_row_loss, f_part_label, f_starts, f_index, f_logit, f_entry_y, f_info, f_total;
+  size_t f_part_few, f_row_loss, f_part_label, f_starts, f_index, f_logit, f_entry_z, f_info, f_total;
   size_t s_rows, s_rows2, s_index, s_at, s_total;      // of `saved`
 };
 
@@ -113,7 +113,7 @@ mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, 
   o->f_starts = K && !o->few ? take((size_t)(o->n_vt + 1) * rows * 2) : 0;
   o->f_index = K ? take(rows * k * 4) : 0;
   o->f_logit = K ? take(rows * k * 4) : 0;
-  o->f_entry_y = K ? take(rows * k * 4) : 0;
+  o->f_entry_z = K ? take(rows * k * 4) : 0;
   o->f_info = K ? take(rows * 4) : 0;
   o->f_total = off;
   off = align_up(sizeof(ObjHeader), 256);
@@ -208,14 +208,14 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   if (o.K) {
     e.starts = sorted ? starts : nullptr;
     e.index = index;
-    e.entry_y = reinterpret_cast<float*>(ws + o.f_entry_y);
+    e.entry_z = reinterpret_cast<float*>(ws + o.f_entry_z);
     e.info = info;
   }
   ObjFinal f = {};
   f.part = e.part; f.part_label = e.part_label; f.part_stride = stride;
   f.n_vt = o.n_vt; f.V = (int)p.V; f.K = o.K;
   f.tgt = e.tgt; f.ignore_index = c.ignore_index;
-  f.index = index; f.logit = sorted ? logit : nullptr; f.logit_bf16 = c.logits_bf16; f.entry_y = e.entry_y; f.info = info;
+  f.index = index; f.logit = sorted ? logit : nullptr; f.logit_bf16 = c.logits_bf16; f.entry_z = e.entry_z; f.info = info;
   f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t_64 = 1.0 / (double)c.temperature; f.inv_t = (float)f.inv_t_64;
   f.label_coef = c.label_coef; f.teacher_coef = c.teacher_coef; f.z_coef = c.z_coef; f.temperature = c.temperature;
   float2* const row_loss = reinterpret_cast<float2*>(ws + o.f_row_loss);

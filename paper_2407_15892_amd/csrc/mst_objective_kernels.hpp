@@ -7,7 +7,7 @@
 //
 //   forward   k_entries        the teacher's entries of every row in ascending order, and where each vocabulary tile's begin (for
 //                              tiles of more than 32 rows; others find them as they need them: TileEntries)
-//             (logits)         ObjEpilogue: the label's y and the entries' y out of the accumulators; partial log-sum-exps of the
+//             (logits)         ObjEpilogue: the label's y and the entries' z out of the accumulators; partial log-sum-exps of the
 //                              others alone, at 1 / T and, where a row needs both, at 1
 //             k_obj_finalize   log-sum-exps, losses, what the backward needs of each row and at each entry
 //             k_obj_loss       the loss, in a fixed order (small calls: with the rows' losses, by k_obj_finalize or k_obj_finalize_one)
@@ -94,7 +94,7 @@ struct ObjTile {
   float* tgt;                          // y of the label, unless it is an entry
   int K;                               // 0: no teacher
   int* index;                          // [rows][K] the entries, kNoEntry where there is none
-  float* entry_y;                      // [rows][K] their y
+  float* entry_z;                      // [rows][K] their logits
   const unsigned short* starts;        // [n_vt + 1][part_stride]: entries before a tile, with `index` ascending; null where the tile
                                        // finds its entries among the caller's and writes `index` and `info` (TileEntries)
   const int* index_in_c;
@@ -141,11 +141,11 @@ struct TileEntries {
   static_assert(kRows * kMaxEntries <= 1 << 15 && kBytes % 16 == 0, "each_entry");
   unsigned* bits;                      // [kRows][kWords]
   int* place;                          // [kRows][kWidth], where there is a bit
-  float* y;                            // [kRows][kWidth]: for the tile's y where there is a bit
+  float* z;                            // [kRows][kWidth]: for the tile's logits where there is a bit
   // smem: kBytes, 16-byte aligned, that nobody uses; all threads of the workgroup
   __device__ __forceinline__ TileEntries(char* smem, const ObjTile& e, const FirstEntries& first, int s0, int rows, int v0, int V, bool first_tile)
       : bits(reinterpret_cast<unsigned*>(smem)), place(reinterpret_cast<int*>(bits + kRows * kWords)),
-        y(reinterpret_cast<float*>(place + kRows * kWidth)) {
+        z(reinterpret_cast<float*>(place + kRows * kWidth)) {
     for (int i = threadIdx.x; i < kRows * kWords; i += kThreadsOfTile) bits[i] = 0;
     for (int i = threadIdx.x; i < kRows * kWidth / 4; i += kThreadsOfTile) reinterpret_cast<int4*>(place)[i] = make_int4(kNoEntry, kNoEntry, kNoEntry, kNoEntry);
     const int here = rows - s0 < kRows ? rows - s0 : kRows;
@@ -159,7 +159,7 @@ struct TileEntries {
     });
     __syncthreads();
   }
-  // behind the tile's y in LDS
+  // behind the tile's logits in LDS
   __device__ __forceinline__ void write(const ObjTile& e, const FirstEntries& first, int s0, int rows, int v0, int V, bool first_tile) const {
     __syncthreads();
     const int here = rows - s0 < kRows ? rows - s0 : kRows;
@@ -170,7 +170,7 @@ struct TileEntries {
         const int in = r * kWidth + v - v0;
         const bool kept = place[in] == k;
         e.index[at] = kept ? v : kNoEntry;
-        if (kept) e.entry_y[at] = y[in];
+        if (kept) e.entry_z[at] = z[in];
       } else if (first_tile && (unsigned)v >= (unsigned)V) {
         e.index[at] = kNoEntry;
         if (v >= V) e.info[s0 + r] = -1;             // behind e.K, with barriers in between
@@ -217,26 +217,23 @@ struct ObjEpilogue : ObjTile {
       from[u] = teacher && kSorted ? starts[(size_t)vt * part_stride + s_in] : 0;
       to[u] = teacher && kSorted ? starts[(size_t)(vt + 1) * part_stride + s_in] : 0;
     }
-    if (kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap) {
+    float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
+    const bool bends = kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap;
+    // Bit t: some of the wave's logits acc[t] are far from 0 (seldom), before any is masked.
+    unsigned far = 0;
+    if (bends) {
       const Cap bend(cap);
 #pragma unroll
       for (int t = 0; t < TA; ++t) {
-        float top = 0.f;               // 16 logits of a lane at a time: seldom is one of the wave's far from 0
+        float top = 0.f;
 #pragma unroll
         for (int u = 0; u < TB; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) top = fmaxf(top, __builtin_fabsf(acc[t][u][r]));
-        auto all = [&](auto near) {
-#pragma unroll
-          for (int u = 0; u < TB; ++u)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][u][r] = bend.template y<decltype(near)::value>(acc[t][u][r]);
-        };
-        if (__any(!bend.near(top))) all(std::false_type()); else all(std::true_type());
+        if (__any(!bend.near(top))) far |= 1u << t;
       }
     }
-    float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
-    // The entries' y out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's.
+    // The entries' logits out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's.
     auto take = [&](int u, unsigned mine, auto put) {
       if (!__any(mine != 0)) return;
 #pragma unroll
@@ -284,8 +281,8 @@ struct ObjEpilogue : ObjTile {
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) note(e0 + i, more[i]);
           }
-          float* out = entry_y + (size_t)(s_local < rows ? s_local : rows - 1) * K + first;      // a lane's entries follow each other
-          take(u, mine, [&](int, float y) { *out++ = y; });
+          float* out = entry_z + (size_t)(s_local < rows ? s_local : rows - 1) * K + first;      // a lane's entries follow each other
+          take(u, mine, [&](int, float z) { *out++ = z; });
         }
       } else {
         static_assert(Found::kBytes + 2 * C::EB * 12 <= C::kLds, "beside the triples");
@@ -294,11 +291,28 @@ struct ObjEpilogue : ObjTile {
 #pragma unroll
         for (int u = 0; u < TB; ++u) {
           const int r = wb * (16 * TB) + 16 * u + c;   // past the last row: no bits
-          float* const out = found.y + r * C::EA + va - v0;
+          float* const out = found.z + r * C::EA + va - v0;
           const unsigned word = found.bits[r * Found::kWords + (va - v0) / 32];
-          take(u, (word >> ((va - v0) & 31)) & (0xffffffffu >> (32 - kPer)), [&](int i, float y) { out[i] = y; });
+          take(u, (word >> ((va - v0) & 31)) & (0xffffffffu >> (32 - kPer)), [&](int i, float z) { out[i] = z; });
         }
         found.write(*this, first_entries, s0, rows, v0, V, vt == 0);
+      }
+    }
+    if (bends) {                       // behind the entries, whose slopes need the logits themselves
+      const Cap bend(cap);
+#pragma unroll
+      for (int t = 0; t < TA; ++t) {
+        auto all = [&](auto near) {
+          constexpr bool kNear = decltype(near)::value;          // then the polynomial makes -infinity of kMasked, as good a mask
+#pragma unroll
+          for (int u = 0; u < TB; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float z = acc[t][u][r], y = bend.template y<kNear>(z);
+              acc[t][u][r] = !kNear && teacher && z == kMasked ? kMasked : y;
+            }
+        };
+        if ((far >> t) & 1u) all(std::false_type()); else all(std::true_type());
       }
     }
     if (v0 + C::EA > V) {
@@ -489,11 +503,11 @@ struct ObjFinal {
   const int* labels_c;
   const float* weights_c;
   int ignore_index;
-  const int* index;                   // [rows][K] (kNoEntry: none), and the entries' logits and y
+  const int* index;                   // [rows][K] (kNoEntry: none), and the entries' logits, the teacher's and the student's
   const float* logit;                 // null: the caller's, in the order of its list
   const void* logit_in_c;
   int logit_bf16;
-  const float* entry_y;
+  const float* entry_z;
   const int* info;
   const float* teacher_lse_c;
   float cap, exponent, exponent_label, inv_t;
@@ -605,12 +619,12 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const int s_in = in ? s : a.rows - 1;
   const size_t at0 = (size_t)s_in * a.K;
   int v_p[P ? P : 1];
-  float y_p[P ? P : 1], t_p[P ? P : 1];                          // of the row's entries lane, lane + 16, ...
+  float z_p[P ? P : 1], t_p[P ? P : 1];                          // of the row's entries lane, lane + 16, ...
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const int e = lane + 16 * i, e_in = e < a.K ? e : a.K - 1;
     const int v = a.index[at0 + e_in];
-    y_p[i] = a.entry_y[at0 + e_in];
+    z_p[i] = a.entry_z[at0 + e_in];
     t_p[i] = a.logit ? a.logit[at0 + e_in] : a.logit_bf16 ? (float)static_cast<const __bf16*>(a.logit_in_c)[at0 + e_in]
                                                           : static_cast<const float*>(a.logit_in_c)[at0 + e_in];
     v_p[i] = e < a.K ? v : kNoEntry;
@@ -666,6 +680,9 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     for (int i = 0; i < P; ++i)
       if (v_p[i] != kNoEntry) f(i);
   };
+  float y_p[P ? P : 1];
+#pragma unroll
+  for (int i = 0; i < P; ++i) y_p[i] = a.cap > 0.f ? Cap(a.cap).y<false>(z_p[i]) : z_p[i];
   float my = kMasked, mt = kMasked;
   int some = 0;
   entries([&](int i) {
@@ -803,14 +820,10 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
     if (e >= a.K) continue;
     float x = 0.f;
     if (v != kNoEntry) {
-      const float ye = y_p[i];
       if (on_kd != 0.f) x = on_kd * ((q_p[i] == 0.f ? p_p[i] : share_less(q_p[i], p_p[i], w_p[i])) + over * p_p[i]);
-      if (on_p != 0.f) x += on_p * expf((ye - m_all) - log_label);
+      if (on_p != 0.f) x += on_p * expf((y_p[i] - m_all) - log_label);
       if (valid && v == y) x -= on_label;
-      if (a.cap > 0.f) {
-        const float h = ye / a.cap;                              // 1 - h is off by half a step of 1: 1e-6 of it at z = 2 c, all at 9 c
-        x *= (1.f - h) * (1.f + h);
-      }
+      if (a.cap > 0.f) x *= Cap(a.cap).slope<false>(z_p[i]);
     }
     a.saved_index_c[at0 + e] = v;
     a.saved_at_c[at0 + e] = x;

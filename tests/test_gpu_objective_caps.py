@@ -3,7 +3,7 @@ the capped logits, and equal to the uncapped ones where the cap bends nothing.""
 import numpy as np
 import pytest
 
-from tests.objective_gpu_harness import HALF_FP32, Problem, Run
+from tests.objective_gpu_harness import HALF_FP32, Problem, Run, bf16
 from tests.objective_tight_bounds import check
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +56,25 @@ def test_logits_next_to_nothing(S, d, V):
     bound = 4 * np.sqrt(d) * HALF_FP32 * np.abs(r["Z"]).max() + 16 * HALF_FP32 * np.log(V)
     print((off / bound).max())
     assert (off <= bound).all()
+
+
+@pytest.mark.parametrize("S,d,V", [(64, 64, 300), (300, 64, 3000), (1500, 64, 12800)])
+@pytest.mark.parametrize("o", [dict(tail=True), dict(label_coef=0.5, temperature=2.0), dict(label_coef=0.5)], ids=str)
+def test_slope_at_the_entries_of_a_saturated_cap(S, d, V, o):
+    """Up to 13 caps from 0 the slope is 4 exp(-2 |z| / c), as at other vocabulary entries.  Row s is the s-th unit vector, so that an entry's
+    gradient stands alone in dW."""
+    p = Problem(S, d, V, K=30, softcap=4.0, short=0, empty=0, ignore=0, **o)
+    rng = np.random.default_rng(7)
+    p.H[:] = 0
+    p.H[np.arange(64), np.arange(64)] = 1.0
+    p.W[:30] = bf16(4.0 * rng.uniform(1.0, 13.0, (30, d)) * rng.choice([-1.0, 1.0], (30, d)))
+    p.index[:64] = np.argsort(rng.random((64, 30)), axis=1)
+    p.index[64:] = -1
+    p.logits = np.float32(rng.standard_normal((S, 30))).astype(np.float64)
+    p.labels = np.where(np.arange(S) < 64, rng.integers(0, 60, S), -100).astype(np.int32)
+    if p.lse is not None:
+        p.lse[:] = 5.0
+    run = Run(p)
+    run.forward()
+    run.backward()
+    print(check(p, run.outputs(), p.oracle()))
