@@ -31,7 +31,8 @@
  *
  * Conventions: those of mst_lmhead.h (device pointers, streams, graphs, errors, M, shapes, alignment), and
  *   - labels equal to ignore_index have no loss; a row whose entries are all missing, or have a logit of -infinity (or one of
- *     -5e29 or less, as masks of a type's lowest value) all of them with teacher_lse NULL, has no teacher;
+ *     -5e29 or less, as masks of a type's lowest value) all of them with teacher_lse NULL, has no teacher; one NaN among them makes kd
+ *     and the loss NaN;
  *   - an index below 0 is no entry (rows with fewer than K entries, in any place); an index that comes twice in a row counts
  *     once, with the logit it has first;
  *   - a label outside [0, V) that is not ignore_index, or an index of V or more, never causes an out-of-range access: *loss is

@@ -727,7 +727,7 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   const float nll = valid ? (m_all - (is_entry ? y_entry : tgt)) + log_label : 0.f;
 
   // the teacher's shares; `rest`: what it leaves to the others
-  const bool taught = some > 0 && (given || !(mt <= 0.5f * kMasked));          // true for NaN
+  const bool taught = some > 0 && (given || !(mt <= 0.5f * kMasked) || lt != lt);      // a maximum passes over NaN, a sum does not
   // The divergence is formed of parts that are 0 where a share is the teacher's and else positive: with w = log p - log q
   //   sum q (log q - log p) = sum q (exp(w) - 1 - w) + (sum q - sum p),
   // and the shares of both add up to 1.  What a log-sum-exp is off by changes a part by (p - q) times that and not by q times; softened
