@@ -8,7 +8,7 @@ from tests.objective_tight_bounds import check
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [(20, 64, 300), (300, 72, 3000), (1500, 64, 12800)]      # tiles of 64, of 256 x 32 and of 256 x 256
+SIZES = [(20, 64, 300), (130, 72, 9000), (200, 72, 12800), (400, 72, 12800), (1500, 64, 12800)]      # tiles of 64 x 32, of 256 x 32, 64, 128 and 256
 TEACHER = dict(K=30, tail=True, label_coef=0.5, temperature=2.0, weights=True)
 
 
@@ -58,7 +58,7 @@ def test_logits_next_to_nothing(S, d, V):
     assert (off <= bound).all()
 
 
-@pytest.mark.parametrize("S,d,V", [(64, 64, 300), (300, 64, 3000), (1500, 64, 12800)])
+@pytest.mark.parametrize("S,d,V", [(64, 64, 300), (130, 64, 9000), (400, 64, 12800), (1500, 64, 12800)])
 @pytest.mark.parametrize("o", [dict(tail=True), dict(label_coef=0.5, temperature=2.0), dict(label_coef=0.5)], ids=str)
 def test_slope_at_the_entries_of_a_saturated_cap(S, d, V, o):
     """Up to 13 caps from 0 the slope is 4 exp(-2 |z| / c), as at other vocabulary entries.  Row s is the s-th unit vector, so that an entry's

@@ -6,7 +6,7 @@ from tests.objective_gpu_harness import Problem, Run
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [(20, 64, 300), (300, 72, 3000), (1500, 64, 12800)]      # tiles of 64, of 256 x 32 and of 256 x 256
+SIZES = [(20, 64, 300), (130, 72, 9000), (200, 72, 12800), (400, 72, 12800), (1500, 64, 12800)]      # tiles of 64 x 32, of 256 x 32, 64, 128 and 256
 
 
 @pytest.mark.parametrize("S,d,V", SIZES)
