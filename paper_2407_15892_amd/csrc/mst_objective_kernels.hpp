@@ -219,18 +219,22 @@ struct ObjEpilogue : ObjTile {
     }
     float* xch = reinterpret_cast<float*>(smem);       // [wb][u][16] triples of the wa == 1 waves; the main loop ended with a barrier
     const bool bends = kWhat == kObjAny ? cap > 0.f : kWhat == kObjCap;
-    // Bit t: some of the wave's logits acc[t] are far from 0 (seldom), before any is masked.
+    // Bit t / kSame: some of the wave's logits acc[t] and of the next kSame - 1, 16 of a lane, are far from 0 (seldom), before any is masked.
+    constexpr int kSame = TB >= 4 ? 1 : TA * TB >= 4 ? 4 / TB : TA;
+    static_assert(TA % kSame == 0, "whole groups");
     unsigned far = 0;
     if (bends) {
       const Cap bend(cap);
 #pragma unroll
-      for (int t = 0; t < TA; ++t) {
+      for (int t0 = 0; t0 < TA; t0 += kSame) {
         float top = 0.f;
 #pragma unroll
-        for (int u = 0; u < TB; ++u)
+        for (int t = t0; t < t0 + kSame; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, __builtin_fabsf(acc[t][u][r]));
-        if (__any(!bend.near(top))) far |= 1u << t;
+          for (int u = 0; u < TB; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, __builtin_fabsf(acc[t][u][r]));
+        if (__any(!bend.near(top))) far |= 1u << (t0 / kSame);
       }
     }
     // The entries' logits out of the accumulators, in which they are masked then.  mine: bit i, entry va + i is the teacher's.
@@ -301,18 +305,20 @@ struct ObjEpilogue : ObjTile {
     if (bends) {                       // behind the entries, whose slopes need the logits themselves
       const Cap bend(cap);
 #pragma unroll
-      for (int t = 0; t < TA; ++t) {
+      for (int t0 = 0; t0 < TA; t0 += kSame) {
         auto all = [&](auto near) {
           constexpr bool kNear = decltype(near)::value;          // then the polynomial makes -infinity of kMasked, as good a mask
 #pragma unroll
-          for (int u = 0; u < TB; ++u)
+          for (int t = t0; t < t0 + kSame; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float z = acc[t][u][r], y = bend.template y<kNear>(z);
-              acc[t][u][r] = !kNear && teacher && z == kMasked ? kMasked : y;
-            }
+            for (int u = 0; u < TB; ++u)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float z = acc[t][u][r], y = bend.template y<kNear>(z);
+                acc[t][u][r] = !kNear && teacher && z == kMasked ? kMasked : y;
+              }
         };
-        if ((far >> t) & 1u) all(std::false_type()); else all(std::true_type());
+        if ((far >> (t0 / kSame)) & 1u) all(std::false_type()); else all(std::true_type());
       }
     }
     if (v0 + C::EA > V) {
