@@ -62,11 +62,13 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 
 // gamma = grad_loss / N_valid (Algorithm 4 lines 9-10 and the mean of the loss), 0 when nothing is valid.
 // A negative count is the forward's (or the label scan's) report of a label outside [0, V): the gradients
-// are then NaN throughout, like the loss.
+// are then NaN throughout, like the loss.  A count is below 2^52; a number from there on is the bits of a double (no normal one has
+// lower bits), what another objective divides by.
 __device__ __forceinline__ float gamma_of(const long long* __restrict__ n_valid, float grad_loss) {
   const long long nv = *n_valid;
   if (nv < 0) return __builtin_nanf("");
-  return nv > 0 ? (float)((double)grad_loss / (double)nv) : 0.f;
+  const double n = nv >= 1ll << 52 ? __builtin_bit_cast(double, nv) : (double)nv;
+  return nv > 0 ? (float)((double)grad_loss / n) : 0.f;
 }
 
 // XCD-aware remap of the linear workgroup id to a work item; returns -1 for padding workgroups.
@@ -650,7 +652,8 @@ __global__ __launch_bounds__(1024) void k_finalize_loss(
 // index and V_all the whole vocabulary (both only for the labels).  The row-chunk schedule passes the whole
 // vocabulary (v_base = 0, V = V_all).
 //
-// What an entry is, the objective's gradient E says:
+// An entry is rounded to bf16, the type that the matrix instructions of dH's and dW's products take: half a step, 2^-8 of it at most, of either
+// sign, against a second pair of products for what is lost.  What it is, the objective's gradient E says:
 //   load(s)                 what it needs of a row;  settle(row): the same, ready for use (behind all loads)
 //   with(row, top, f)       calls f with a function of a logit that gives the entry, the label's own term left out; top() is the largest
 //                           magnitude among the logits that f asks for

@@ -218,10 +218,18 @@ mst_status obj_forward(const ObjPlan& o, const ObjCall& c) {
   f.index = index; f.logit = sorted ? logit : nullptr; f.logit_bf16 = c.logits_bf16; f.entry_z = e.entry_z; f.info = info;
   f.cap = c.softcap; f.exponent = exponent; f.exponent_label = kLog2e; f.inv_t_64 = 1.0 / (double)c.temperature; f.inv_t = (float)f.inv_t_64;
   f.label_coef = c.label_coef; f.teacher_coef = c.teacher_coef; f.z_coef = c.z_coef; f.temperature = c.temperature;
+  // The logits' gradient is rounded to bf16, entry by entry, which errors of either sign survive and a common factor of all rows does not
+  // (a label's gradient is its coefficient times nearly -1: 0.3 is 0.3008 in bf16, a label's part of dH and dW 0.26 % too large).  The part of
+  // the labels' coefficient, or the teacher's alone, that has to be rounded, from 1 to 2, therefore goes into the divisor.
+  auto mantissa = [](double x) { int e; return x == 0.0 ? 1.0 : 2.0 * std::frexp(std::fabs(x), &e); };
+  const double slope = (double)c.teacher_coef * (double)c.temperature;
+  const double unit = c.labels && c.label_coef != 0.f ? mantissa(c.label_coef) : mantissa(slope);
+  f.label_slope = (float)((double)c.label_coef / unit); f.teacher_slope = (float)(slope / unit); f.z_slope = (float)((double)c.z_coef / unit);
   float2* const row_loss = reinterpret_cast<float2*>(ws + o.f_row_loss);
 
   ObjLoss l = {};
   l.divisor = c.divisor;
+  l.unit = unit;
   l.head.cap = c.softcap;
   l.head.exponent = exponent;
   l.head.exponent_label = kLog2e;

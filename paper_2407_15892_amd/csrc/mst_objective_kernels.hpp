@@ -29,7 +29,7 @@ constexpr int kNoEntry = 0x7fffffff;        // sorts behind every entry
 // What the backward call needs, at the front of the caller's `saved`.
 struct ObjHeader {
   long long n_valid;                        // rows that count; -1: an index out of range
-  long long n_divisor;                      // what the sums are divided by (-1 again, 0 where no row counts)
+  long long n_divisor;                      // what the gradient's sums are divided by, a double's bits (-1 again, 0 where no row counts)
   float cap, exponent, exponent_label;      // log2(e) / T of the (first) exponential, log2(e) of the second
   int two;                                  // rows have two exponentials
 };
@@ -519,6 +519,7 @@ struct ObjFinal {
   float cap, exponent, exponent_label, inv_t;
   double inv_t_64;
   float label_coef, teacher_coef, z_coef, temperature;
+  float label_slope, teacher_slope, z_slope;      // of the gradient, in units of ObjLoss::unit
   float *nll_c, *kd_c, *lse_c;        // outputs, each may be null
   float2* row_loss_c;                 // the row's loss, and as an integer's bits 1: it counts, -1: an index out of range
   ObjRow* rows_c;                     // null: no backward follows
@@ -570,6 +571,7 @@ __device__ __forceinline__ float share_less(float q, float p, float w) { return 
 // What the loss needs besides the rows'.
 struct ObjLoss {
   long long divisor;
+  double unit;                        // the gradient's: its rows, in bf16, are in units of it
   ObjHeader head;
   ObjHeader* saved;                   // null: no backward follows
   float* loss;
@@ -581,7 +583,7 @@ __device__ __forceinline__ void write_loss(const ObjLoss& o, double sum, long lo
   if (o.n_valid) *o.n_valid = bad ? -1 : n;
   if (!o.saved) return;
   o.saved->n_valid = bad ? -1 : n;
-  o.saved->n_divisor = divisor;
+  o.saved->n_divisor = divisor > 0 ? __builtin_bit_cast(long long, (double)divisor / o.unit) : divisor;
   o.saved->cap = o.head.cap;
   o.saved->exponent = o.head.exponent;
   o.saved->exponent_label = o.head.exponent_label;
@@ -760,9 +762,9 @@ __global__ __launch_bounds__(kObjRows * kObjGroups) void k_obj_finalize(ObjFinal
   kd_64 += (double)above_tangent(rest, share, w_rest);
   const float over = given ? (float)(sum_q + (double)rest - 1.0) : 0.f;  // where the teacher's entries are more than 1 in all
   const float kd = taught ? (float)(kd_64 + (double)over) : 0.f;
-  const float on_kd = taught && weight != 0.f ? weight * a.teacher_coef * a.temperature : 0.f;
-  const float on_label = valid && weight != 0.f ? weight * a.label_coef : 0.f;
-  const float on_p = on_label + (valid && weight != 0.f ? 2.f * weight * a.z_coef * lse : 0.f);
+  const float on_kd = taught && weight != 0.f ? weight * a.teacher_slope : 0.f;
+  const float on_label = valid && weight != 0.f ? weight * a.label_slope : 0.f;
+  const float on_p = on_label + (valid && weight != 0.f ? 2.f * weight * a.z_slope * lse : 0.f);
   __shared__ float sh_loss[kObjRows];
   __shared__ int sh_count[kObjRows];
   if (in && lane == 0) {
@@ -927,8 +929,8 @@ __global__ __launch_bounds__(1024) void k_obj_finalize_one(ObjFinal a, ObjLoss o
     if (a.rows_c) {
       ObjRow row;
       row.label = on ? y : -1;
-      row.label_term = on ? weight * a.label_coef : 0.f;
-      row.at = on ? row.label_term + 2.f * weight * a.z_coef * lse : 0.f;
+      row.label_term = on ? weight * a.label_slope : 0.f;
+      row.at = on ? row.label_term + 2.f * weight * a.z_slope * lse : 0.f;
       row.base = row.at == 0.f ? __builtin_inff() : lse;
       a.rows_c[s] = row;
     }
@@ -939,6 +941,9 @@ __global__ __launch_bounds__(1024) void k_obj_finalize_one(ObjFinal a, ObjLoss o
 // ---------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------
+// Every entry is rounded to bf16, here and in k_obj_entries too, as the matrix instructions of both products take it: dH and dW, themselves
+// in bf16, are 2.2e-3 off in place of 1.7e-3, errors of either sign (ObjLoss::unit keeps it so); two bf16 parts an entry would double
+// the products, three quarters of a step.
 struct ObjGrad {
   const ObjHeader* head;
   const ObjRow* rows;
