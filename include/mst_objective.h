@@ -42,7 +42,7 @@
  *     8 for each of K entries.  The backward call takes softcap, temperature, coefficients, weights, labels and the teacher from
  *     it; H, W, S, d, V and K have to be those of the forward call, M need not be.  NULL where no backward call follows;
  *   - M is the largest number of mini-sequences: the calls make fewer, longer ones as long as the fp32 logits of one are at most
- *     512 MiB and its rows x d below 2^30, and their workspace is that of these;
+ *     512 MiB and its rows x d below 2^30, and their workspace is that of these, whatever larger M is given;
  *   - arithmetic: that of mst_lmhead.h; a capped logit within 8 half steps of float32 of its value, at any cap; the loss and the
  *     rows' outputs float32 (sums over rows in 64 bits); the gradient of the logits rounded to bf16 before the two products, without
  *     grad_loss / n and without what all rows have in common: the labels' coefficient but for a power of 2, with label_coef 0 or no

@@ -21,16 +21,16 @@ struct ObjPlan {
 // the entries of its rows.
 constexpr int kPatchEntries = 64;
 
-// See TileFew.  Where tiles of 256 leave a row's pairs to one thread of k_obj_finalize_one and tiles of 64 do not, short hidden sizes are slower
-// with these: 128 rows, V = 4000: d = 128 8.0 us with tiles of 256, 9.3; 512 9.9, 10.3; 1536 16.7, 13.9; 4096 30.0, 21.0.
+// See TileFew.  Where tiles of 256 leave a row's pairs to one thread of k_obj_finalize_one and tiles of 64 do not, short hidden sizes are
+// slower with these: 128 rows, V = 4000: d = 128 8.0 us with tiles of 256, 9.3; 512 9.9, 10.3; 1536 16.7, 13.9; 4096 30.0, 21.0.
 int few_row_tiles(const Plan& p) { return (int)((p.S + TileFew::EB - 1) / TileFew::EB); }
 bool use_tile_few(const Plan& p, int K) {
   if (p.S > p.fwd_group_rows || (p.S + TileFew::EB - 1) / TileFew::EB * p.n_vt > kNumCu / 2) return false;
   return K || p.S <= kObjRows || p.d >= 1024 || p.n_vt > kFinOneTiles || p.V <= kFinOneTiles * TileFew::EA;
 }
 
-// One workgroup finishes a forward call without a teacher (k_obj_finalize_one).  Whole calls, us, with it and with the two launches of longer ones:
-// 256 rows, d = 512, 32 tiles of 64 9.4, 11.1; 63 tiles (16128 pairs) 12.1, 12.3; 1000 rows, d = 512, 20 tiles of 256 (20000) 17.8, 19.9.  Up to 32 pairs a row are one
+// One workgroup finishes a forward call without a teacher (k_obj_finalize_one).  Whole calls, us, with it and with the two launches of
+// longer ones: 256 rows, d = 512, 32 tiles of 64 11.5, 14.3; d = 1024, 63 tiles (16128 pairs) 14.2, 15.9.  Up to 32 pairs a row are one
 // thread's: split over two, and joined in LDS, 512 rows of 16 take 11.3 in place of 10.5.
 constexpr int64_t kPairsOfOne = 16384;
 int finalize_row_bits(int64_t S, int n_vt) {                       // of its threads, 2^row_bits have the first pair of a row each
@@ -73,10 +73,10 @@ int32_t fewer_mini_sequences(int64_t S, int64_t d, int64_t V, int32_t M) {
   return (int32_t)std::min<int64_t>(M, (S + rows - 1) / rows);
 }
 
-// dW of few vocabulary entries and many rows is a few tiles with a long contraction over the rows, which is split then.  The partials fit into
-// the half of the workspace that one mini-sequence's dlogits leave; the launch models are those that rank the tiles.  Backward, us, without and
-// with: 30000 rows, d = 128, V = 352 114, 46; 65536, 1024, 512 415, 246; 32768, 2048, 384 245, 217; 16384, 512, 1000 132, 94; where the models see less than
-// 15 % the launch stays whole (5000, 2048, 256: 53).
+// dW of few vocabulary entries and many rows is a few tiles with a long contraction over the rows, which is split then.  The partials
+// fit into the half of the workspace that one mini-sequence's dlogits leave; the launch models are those that rank the tiles.  Backward,
+// us, without and with: 30000 rows, d = 128, V = 352 114, 46; 65536, 1024, 512 415, 246; 32768, 2048, 384 245, 217; 16384, 512, 1000 132,
+// 94; where the models see less than 15 % the launch stays whole (5000, 2048, 256: 53).
 void split_dw(Plan* p) {
   if (p->blk_use || p->joint || p->n_chunks != 1) return;
   const double ksteps = (double)((p->C + kBK - 1) / kBK), bytes = 4.0 * (double)(p->V * p->d);
@@ -94,7 +94,8 @@ void split_dw(Plan* p) {
   }
 }
 
-mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO, bool schedule = false) {
+mst_status make_obj_plan(int64_t S, int64_t d, int64_t V, int32_t M, int32_t K, ObjPlan* o, int forced = MST_BWD_SCHEDULE_AUTO,
+                         bool schedule = false) {
   const mst_status s = make_plan(S, d, V, fewer_mini_sequences(S, d, V, M), &o->p, forced, 0, schedule);
   if (s != MST_OK) return s;
   if (K < 0 || K > MST_MAX_ENTRIES) return MST_ERR_BAD_SHAPE;

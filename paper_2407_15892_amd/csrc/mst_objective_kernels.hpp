@@ -76,7 +76,8 @@ struct Cap {
 };
 
 // merge_lse for sums of exp2(exponent (y - m)), and a second sum beside the first at another exponent
-__device__ __forceinline__ void merge_sums(float& m, float& l, float& k, float m2, float l2, float k2, float exponent, float exponent_label, bool two) {
+__device__ __forceinline__ void merge_sums(float& m, float& l, float& k, float m2, float l2, float k2, float exponent, float exponent_label,
+                                           bool two) {
   const float mm = fmaxf(m, m2), a = m - mm, b = m2 - mm;
   l = __builtin_fmaf(l, fast_exp2(a * exponent), l2 * fast_exp2(b * exponent));
   if (two) k = __builtin_fmaf(k, fast_exp2(a * exponent_label), k2 * fast_exp2(b * exponent_label));
@@ -147,7 +148,8 @@ struct TileEntries {
       : bits(reinterpret_cast<unsigned*>(smem)), place(reinterpret_cast<int*>(bits + kRows * kWords)),
         z(reinterpret_cast<float*>(place + kRows * kWidth)) {
     for (int i = threadIdx.x; i < kRows * kWords; i += kThreadsOfTile) bits[i] = 0;
-    for (int i = threadIdx.x; i < kRows * kWidth / 4; i += kThreadsOfTile) reinterpret_cast<int4*>(place)[i] = make_int4(kNoEntry, kNoEntry, kNoEntry, kNoEntry);
+    for (int i = threadIdx.x; i < kRows * kWidth / 4; i += kThreadsOfTile)
+      reinterpret_cast<int4*>(place)[i] = make_int4(kNoEntry, kNoEntry, kNoEntry, kNoEntry);
     const int here = rows - s0 < kRows ? rows - s0 : kRows;
     if (first_tile)
       for (int r = threadIdx.x; r < here; r += kThreadsOfTile) e.info[s0 + r] = e.K;
@@ -391,12 +393,13 @@ struct ObjEpilogue : ObjTile {
   }
 };
 
-// Calls that have tiles of 32 rows and 256 vocabulary entries for half of the compute units or fewer: with up to 32 rows W is read once, which
-// is all that takes time, and a compute unit alone does not get its share of the memory's bandwidth; with more a few workgroups take
-// the K loop's steps one by one.  Tiles of 64, two workgroups on a compute unit where there are as many.  Whole calls, us, tiles of 256 and these:
-// 33 rows, V = 300: d = 512 9.8, 7.8; 4096 29.1, 17.2; 500 rows, V = 1000: 1536 16.3, 12.0; with 30 entries 23.9, 18.7; but where tiles of 256
-// are for all compute units, 512 rows, V = 4096, d = 1024 15.1, 22.2.  Forward of 16 rows, us, with tiles of 256, of 128 (lone ones, eight
-// stages) and these: d = 4096, V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048, V = 4000 19.6, 15.8, 13.4.
+// Calls that have tiles of 32 rows and 256 vocabulary entries for half of the compute units or fewer: with up to 32 rows W is read once,
+// which is all that takes time, and a compute unit alone does not get its share of the memory's bandwidth; with more a few workgroups take
+// the K loop's steps one by one.  Tiles of 64, two workgroups on a compute unit where there are as many.  Whole calls, us, tiles of 256
+// and these: 33 rows, V = 300: d = 512 9.8, 7.8; 4096 29.1, 17.2; 500 rows, V = 1000: 1536 16.3, 12.0; with 30 entries 23.9, 18.7; but where
+// tiles of 256 are for all compute units, 512 rows, V = 4096, d = 1024 15.1, 22.2.  Forward of 16 rows, us, with tiles of 256, of 128 (lone
+// ones, eight stages) and these: d = 4096, V = 32768 68.2, 64.6, 58.1 (4.6 TB/s); 16000 54.3, 38.0, 33.0; 8000 30.7, 22.1, 19.2; d = 2048,
+// V = 4000 19.6, 15.8, 13.4.
 // (With both operands from memory straight into registers, a wave to 16 vocabulary entries: 57.8 for one row, 71.4 for 16.)
 typedef CfgSmall<2, 1, 6, 6, true> TileFew;
 
@@ -958,7 +961,8 @@ struct ObjGrad {
     if (!K) return;
     __syncthreads();
     const size_t from = (size_t)s0 * K;
-    each_entry<kThreadsOfTile>(load_entries<kThreadsOfTile>(index + from, n_rows * K, threadIdx.x), index + from, n_rows, K, [&](int r, int k, int v) {
+    const FirstEntries first = load_entries<kThreadsOfTile>(index + from, n_rows * K, threadIdx.x);
+    each_entry<kThreadsOfTile>(first, index + from, n_rows, K, [&](int r, int k, int v) {
       if ((unsigned)(v - v0) < (unsigned)width && v < V)
         *reinterpret_cast<__bf16*>(staged + r * row_bytes + 2 * (v - v0)) = (__bf16)at[from + (size_t)r * K + k];
     });
