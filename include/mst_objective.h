@@ -46,7 +46,8 @@
  *   - arithmetic: that of mst_lmhead.h; a capped logit within 8 half steps of float32 of its value, at any cap; the loss and the
  *     rows' outputs float32 (sums over rows in 64 bits); the gradient of the logits rounded to bf16 before the two products, without
  *     grad_loss / n and without what all rows have in common: the labels' coefficient but for a power of 2, with label_coef 0 or no
- *     labels teacher_coef * temperature.  Everything in a fixed order, without atomics: repeated calls give the same bits;
+ *     labels teacher_coef * temperature (a factor that all weights have is better given as grad_loss).  Everything in a fixed order,
+ *     without atomics: repeated calls give the same bits;
  *   - no output and neither `saved` nor the workspace may overlap another argument (MST_ERR_BAD_ARGUMENT);
  *   - mst_profile_collect counts the launches under the kinds of the plain calls' that they stand for: sorting a teacher's entries under the
  *     label scan, putting them into the logits' gradient and adding up dW's parts under dH's reduce.
